@@ -258,7 +258,7 @@ def _buffers(s, km):
         b["top_id"], b["top_logp"] = _empty(T, top, dtype=torch.int32), _empty(T, top)
         b["ws"] = _empty(km.kmp_token_logprobs_workspace_bytes(T, c["V"], top), dtype=torch.uint8)
         if c["kind"] == "loss_step":
-            b["lse"], b["dx"] = _empty(T), _empty(T, c["V"], dtype=dtype)
+            b["stats"], b["dx"] = _empty(T, 2), _empty(T, c["V"], dtype=dtype)
     return b
 
 
@@ -287,9 +287,9 @@ def _own_run(s):
         km.kmp_token_logprobs(s["logits"], s["tokens"], b["logp"], entropy=b["entropy"], top_id=b["top_id"],
                               top_logp=b["top_logp"], workspace=b["ws"])
         return b["logp"], b["entropy"], b["top_id"], b["top_logp"]
-    km.kmp_token_logprobs(s["logits"], s["tokens"], b["logp"], entropy=b["entropy"], lse=b["lse"],
+    km.kmp_token_logprobs(s["logits"], s["tokens"], b["logp"], entropy=b["entropy"], stats=b["stats"],
                           workspace=b["ws"])
-    km.kmp_token_logprobs_backward(s["logits"], s["tokens"], b["lse"], s["dlogp"], b["dx"],
+    km.kmp_token_logprobs_backward(s["logits"], s["tokens"], b["stats"], s["dlogp"], b["dx"],
                                    entropy=b["entropy"], dentropy=s["dentropy"])
     return b["logp"], b["entropy"], b["dx"]
 
