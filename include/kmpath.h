@@ -1,6 +1,7 @@
 /*
  * kmpath -- cross-validated regularisation paths of RBF kernel machines on
- * one AMD Instinct MI355X (gfx950), fp64 throughout.
+ * one AMD Instinct MI355X (gfx950), fp64 throughout; and the operators at a
+ * language model's end that its features come from, in 8 to 32 bits (last part).
  *
  * Problem (Appendix A.1, eq. (kernelsvm); Appendix A.2, fold-restricted
  * form). For every kernel bandwidth sigma_s, quantile level tau_q (check
@@ -325,6 +326,114 @@ int kmp_path_step(void* stream, int32_t loss, double delta, const double* K, int
  * (overwritten; zero when K = 0). G <= 65535. Synchronises `stream`.       */
 int kmp_dgemm_grouped(void* stream, int32_t G, int32_t M, int32_t N, int32_t K,
                       const double* A, const double* B, double* C);
+
+/* ------------------------------------------------------------------------
+ * Operators at a language model's end: the layer norm of its hidden states,
+ * the 8-bit product with its vocabulary head, and the log probabilities of its
+ * tokens. A kernel machine's features often come from there (hidden states;
+ * log probability and entropy of an answer's tokens), and the gradients go
+ * back through them. Unlike the entry points above they work in 16 or 32 bits
+ * (sums and statistics in 32, or 64 for doubles), never allocate, never wait
+ * for the device and may be captured into a HIP graph. Element types:       */
+#define KMP_F64 0
+#define KMP_F32 1
+#define KMP_BF16 2
+#define KMP_F16 3
+#define KMP_I8 4
+/* All matrices are row-major with a leading dimension in elements; no
+ * alignment beyond one element is needed (16-byte aligned rows are faster).
+ * Outputs must not overlap inputs unless stated.                            */
+
+/* Layer norm of each row of x (DEVICE, rows x d): y = (x - mu) r gamma + beta,
+ * mu the row's mean, r = 1 / sqrt(variance + eps), the variance the mean of
+ * (x - mu)^2.
+ *   xtype      KMP_F64, KMP_F32, KMP_BF16 or KMP_F16
+ *   gamma, beta DEVICE [d] of type wtype (xtype, or KMP_F32 for 16-bit x);
+ *              either may be NULL (ones, zeros)
+ *   y          DEVICE, of type ytype = xtype, or KMP_I8 (not for KMP_F64): the
+ *              row quantised as by kmp_quantize_rows, from its 32-bit values
+ *   mean, rstd DEVICE [rows], 32 bits (64 for KMP_F64); may be NULL; what the
+ *              backward pass reads
+ *   scale      DEVICE [rows], the rows' scales with KMP_I8, else ignored      */
+int kmp_layer_norm(void* stream, int32_t xtype, const void* x, int64_t rows, int64_t d, int64_t ldx,
+                   int32_t wtype, const void* gamma, const void* beta, double eps, int32_t ytype,
+                   void* y, int64_t ldy, void* mean, void* rstd, float* scale);
+
+/* Bytes of DEVICE workspace of kmp_layer_norm_backward; 0: bad arguments.   */
+size_t kmp_layer_norm_workspace_bytes(int32_t xtype, int64_t rows, int64_t d);
+
+/* Gradients of the layer norm from dy (DEVICE, rows x d, xtype): with
+ * xh = (x - mu) r and w = dy gamma,
+ *   dx = r (w - mean_j(w) - xh mean_j(w xh))   (rows x d, xtype)
+ *   dgamma = sum over rows of dy xh, dbeta = sum over rows of dy  ([d], wtype)
+ * x, gamma, mean and rstd as in the forward call. dx, dgamma and dbeta may
+ * each be NULL; the workspace (16-byte aligned) is needed for the latter two.
+ * The sums over the rows are taken in a fixed order: the same call gives the
+ * same bits. With rows = 0 dgamma and dbeta are set to zero.                */
+int kmp_layer_norm_backward(void* stream, int32_t xtype, const void* dy, int64_t lddy, const void* x,
+                            int64_t ldx, int64_t rows, int64_t d, int32_t wtype, const void* gamma,
+                            const void* mean, const void* rstd, void* dx, int64_t lddx, void* dgamma,
+                            void* dbeta, void* workspace, size_t workspace_bytes);
+
+/* Rows of x (DEVICE, rows x d; KMP_F32, KMP_BF16 or KMP_F16) in 8 bits:
+ * q = rint(x (127 / a)), scale = a / 127, a the row's largest |x| (DEVICE,
+ * q rows x d, scale [rows]). A zero row has q = 0 and scale 0; a row with a
+ * NaN or an infinity q = 0 and scale NaN, so that products with it are NaN and
+ * other rows are not touched.                                               */
+int kmp_quantize_rows(void* stream, int32_t xtype, const void* x, int64_t rows, int64_t d, int64_t ldx,
+                      int8_t* q, int64_t ldq, float* scale);
+
+/* Product in 8-bit integers with a scale per token and per channel:
+ *   out[m][n] = xscale[m] wscale[n] sum_k x[m][k] w[n][k] + bias[n]
+ * x DEVICE M x K with scales [M], w DEVICE N x K (one row per output channel)
+ * with scales [N], bias DEVICE [N] or NULL, out DEVICE M x N of type otype
+ * (KMP_F32, KMP_BF16 or KMP_F16). The sums are exact in 32-bit integers:
+ * K <= 131071 (KMP_EINVAL above). K = 0 gives the bias. Rows that start at
+ * multiples of 16 bytes (ldx, ldw multiples of 16) are read fastest; K itself
+ * may be any number.                                                        */
+int kmp_quantized_product(void* stream, const int8_t* x, int64_t ldx, const float* xscale, int64_t M,
+                          const int8_t* w, int64_t ldw, const float* wscale, int64_t N, int64_t K,
+                          const float* bias, int32_t otype, void* out, int64_t ldo);
+
+/* Most alternatives per token. */
+#define KMP_MAX_TOP 64
+
+/* Bytes of DEVICE workspace of kmp_token_logprobs; 0: bad arguments.        */
+size_t kmp_token_logprobs_workspace_bytes(int64_t T, int64_t V, int32_t top);
+
+/* Log probabilities of given tokens under the rows of logits (DEVICE, T x V;
+ * KMP_F32, KMP_BF16 or KMP_F16), p = softmax of a row:
+ *   tokens   DEVICE [T], int32 or int64 (token_bits 32 or 64). A negative
+ *            token stands for none; a token >= V makes its logp NaN
+ *   logp     log p[token]; 0 for none. May be NULL (then tokens may be, too)
+ *   entropy  -sum p log p; may be NULL
+ *   stats    DEVICE [T][2], the row's maximum m and log sum exp(x - m) (their
+ *            sum is log sum exp x; apart they hold it at any size of m); may be
+ *            NULL; what the backward pass reads
+ *   top_id, top_logp  DEVICE [T][top], the `top` most likely tokens and their
+ *            log probabilities, equal logits by the lowest index first; each
+ *            may be NULL; top <= min(V, KMP_MAX_TOP)
+ *   workspace DEVICE, 16-byte aligned
+ * Outputs are 32 bits. A logit of -inf (a token ruled out) has p = 0 and adds
+ * nothing to the entropy; a row of nothing but -inf has stats and every log
+ * probability -inf, entropy 0. A row with a NaN or +inf has NaN results.    */
+int kmp_token_logprobs(void* stream, int32_t type, const void* logits, int64_t T, int64_t V, int64_t ldl,
+                       int32_t token_bits, const void* tokens, float* logp, float* entropy, float* stats,
+                       int32_t top, int32_t* top_id, float* top_logp, void* workspace,
+                       size_t workspace_bytes);
+
+/* Gradient of sum_t dlogp[t] logp[t] + dentropy[t] entropy[t] with respect to
+ * the logits (DEVICE, T x V, type; dlogits == logits with ldd == ldl is
+ * allowed):
+ *   dlogits_j = dlogp (1[j = token] - p_j) - dentropy p_j (log p_j + entropy)
+ * logits, tokens, stats and entropy as of the forward call; dlogp and dentropy
+ * DEVICE [T], either may be NULL (with dentropy, entropy may be, too; with
+ * dlogp, tokens). Rows without a token have no dlogp term; rows of nothing but
+ * -inf have gradient 0; rows with a token >= V or NaN stats have gradient NaN. */
+int kmp_token_logprobs_backward(void* stream, int32_t type, const void* logits, int64_t T, int64_t V,
+                                int64_t ldl, int32_t token_bits, const void* tokens, const float* stats,
+                                const float* entropy, const float* dlogp, const float* dentropy,
+                                void* dlogits, int64_t ldd);
 
 /* Message for a return code, or the last HIP error text for KMP_EHIP. */
 const char* kmp_strerror(int code);

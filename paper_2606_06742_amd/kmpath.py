@@ -28,6 +28,8 @@ KMP_FLAG_SHARED_FACTOR = 8
 KMP_FLAG_EXACT_HINGE = 16
 KMP_FLAG_EAGER = 32
 KMP_WNOTEXACT = 2
+KMP_F64, KMP_F32, KMP_BF16, KMP_F16, KMP_I8 = 0, 1, 2, 3, 4
+KMP_MAX_TOP = 64
 KMP_NKC = 10
 KERNEL_CLASSES = ("gram", "panel", "panel_wy", "trail_update", "q_form", "precompute", "gemm_f",
                   "gemm_zhat", "update", "finalize")
@@ -114,6 +116,28 @@ def lib():
         L.kmp_dgemm_grouped.argtypes = [_VP, C.c_int32, C.c_int32, C.c_int32, C.c_int32, _VP, _VP,
                                         _VP]
         L.kmp_dgemm_grouped.restype = C.c_int
+        I32, I64 = C.c_int32, C.c_int64
+        L.kmp_layer_norm.argtypes = [_VP, I32, _VP, I64, I64, I64, I32, _VP, _VP, C.c_double, I32,
+                                     _VP, I64, _VP, _VP, _VP]
+        L.kmp_layer_norm.restype = C.c_int
+        L.kmp_layer_norm_workspace_bytes.argtypes = [I32, I64, I64]
+        L.kmp_layer_norm_workspace_bytes.restype = C.c_size_t
+        L.kmp_layer_norm_backward.argtypes = [_VP, I32, _VP, I64, _VP, I64, I64, I64, I32, _VP, _VP,
+                                              _VP, _VP, I64, _VP, _VP, _VP, C.c_size_t]
+        L.kmp_layer_norm_backward.restype = C.c_int
+        L.kmp_quantize_rows.argtypes = [_VP, I32, _VP, I64, I64, I64, _VP, I64, _VP]
+        L.kmp_quantize_rows.restype = C.c_int
+        L.kmp_quantized_product.argtypes = [_VP, _VP, I64, _VP, I64, _VP, I64, _VP, I64, I64, _VP,
+                                            I32, _VP, I64]
+        L.kmp_quantized_product.restype = C.c_int
+        L.kmp_token_logprobs_workspace_bytes.argtypes = [I64, I64, I32]
+        L.kmp_token_logprobs_workspace_bytes.restype = C.c_size_t
+        L.kmp_token_logprobs.argtypes = [_VP, I32, _VP, I64, I64, I64, I32, _VP, _VP, _VP, _VP, I32,
+                                         _VP, _VP, _VP, C.c_size_t]
+        L.kmp_token_logprobs.restype = C.c_int
+        L.kmp_token_logprobs_backward.argtypes = [_VP, I32, _VP, I64, I64, I64, I32, _VP, _VP, _VP,
+                                                  _VP, _VP, _VP, I64]
+        L.kmp_token_logprobs_backward.restype = C.c_int
         L.kmp_strerror.argtypes = [C.c_int]
         L.kmp_strerror.restype = C.c_char_p
         L.kmp_version.argtypes = []
@@ -127,7 +151,10 @@ def lib():
 EXPORTED = ("kmp_default_spec", "kmp_workspace_bytes", "kmp_fit_path", "kmp_make_folds",
             "kmp_rbf_gram", "kmp_rbf_gram_noalloc", "kmp_tridiag", "kmp_band_reduce",
             "kmp_path_step",
-            "kmp_dgemm_grouped", "kmp_strerror", "kmp_version", "kmp_kernel_class_name")
+            "kmp_dgemm_grouped", "kmp_layer_norm", "kmp_layer_norm_workspace_bytes",
+            "kmp_layer_norm_backward", "kmp_quantize_rows", "kmp_quantized_product",
+            "kmp_token_logprobs", "kmp_token_logprobs_workspace_bytes",
+            "kmp_token_logprobs_backward", "kmp_strerror", "kmp_version", "kmp_kernel_class_name")
 KMP_BAND = 16
 
 
@@ -232,6 +259,187 @@ def kmp_dgemm_grouped(A, B, C, stream=None) -> None:
     N = B.shape[2]
     _check(lib().kmp_dgemm_grouped(_stream_ptr(stream), G, M, N, K, A.data_ptr(), B.data_ptr(),
                                    C.data_ptr()), allow_maxiter=False)
+
+
+# ------------------------------------------ operators at a language model's end
+# Tensors are on the current device; matrices are 2-D with consecutive elements
+# in a row and any row stride, vectors are contiguous. Nothing waits for the
+# device: `stream` (the current stream if None) carries the work, and tensors
+# made on another stream are the caller's to order.
+_TYPES: dict = {}
+
+
+def _type(t, name: str) -> int:
+    """KMP_* code of a tensor's (or torch) type."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float64: KMP_F64, torch.float32: KMP_F32, torch.bfloat16: KMP_BF16,
+                       torch.float16: KMP_F16, torch.int8: KMP_I8})
+    dtype = getattr(t, "dtype", t)
+    if dtype not in _TYPES:
+        raise KmpError(KMP_EINVAL, f"{name}: type {dtype} is not supported")
+    return _TYPES[dtype]
+
+
+def _refuse(what: str):
+    raise KmpError(KMP_EINVAL, what)
+
+
+def _matrix(t, name: str, rows=None, cols=None, dtype=None):
+    """(pointer, rows, columns, row stride) of a 2-D device tensor."""
+    if t.dim() != 2 or not t.is_cuda:
+        _refuse(f"{name} must be a 2-D device tensor")
+    (r, c), (sr, sc) = t.shape, t.stride()
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        _refuse(f"{name} has shape {r} x {c}, not {rows} x {cols}")
+    if dtype is not None and t.dtype != dtype:
+        _refuse(f"{name} has type {t.dtype}, not {dtype}")
+    if (sc != 1 and c > 1) or (r > 1 and sr < c):
+        _refuse(f"{name} must have consecutive elements in a row and rows that do not overlap")
+    return t.data_ptr(), r, c, sr if r > 1 else max(c, 1)
+
+
+def _vector(t, name: str, n: int, dtype=None):
+    """Pointer of a contiguous device tensor of n elements; None stays None."""
+    if t is None:
+        return None
+    if t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous device tensor of {n} elements")
+    if dtype is not None and t.dtype != dtype:
+        _refuse(f"{name} has type {t.dtype}, not {dtype}")
+    return t.data_ptr()
+
+
+def _tokens(t, n: int):
+    """(bits, pointer) of the tokens; None stays None."""
+    if t is None:
+        return 32, None
+    bits = t.element_size() * 8
+    if t.is_floating_point() or bits not in (32, 64):
+        _refuse(f"tokens have type {t.dtype}, not int32 or int64")
+    return bits, _vector(t, "tokens", n)
+
+
+def _workspace(t):
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        _refuse("workspace must be a contiguous device tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def kmp_layer_norm(x, gamma, beta, eps, y, mean=None, rstd=None, scale=None, stream=None) -> None:
+    """Layer norm of the rows of x (rows, d) into y: of x's type, or int8 with
+    the rows' scales in `scale`. gamma and beta (d) are of x's type or float32
+    (None: ones, zeros); mean and rstd (rows) take what the backward reads."""
+    xp, rows, d, ldx = _matrix(x, "x")
+    yp, _, _, ldy = _matrix(y, "y", rows, d)
+    xt = _type(x, "x")
+    w = gamma if gamma is not None else beta
+    wt = _type(w, "gamma") if w is not None else xt
+    wd = w.dtype if w is not None else None
+    sd = rd = None
+    if mean is not None or rstd is not None or scale is not None:
+        import torch
+        sd, rd = torch.float64 if xt == KMP_F64 else torch.float32, torch.float32
+    _check(lib().kmp_layer_norm(
+        _stream_ptr(stream), xt, xp, rows, d, ldx, wt, _vector(gamma, "gamma", d, wd),
+        _vector(beta, "beta", d, wd), float(eps), _type(y, "y"), yp, ldy,
+        _vector(mean, "mean", rows, sd), _vector(rstd, "rstd", rows, sd),
+        _vector(scale, "scale", rows, rd)), allow_maxiter=False)
+
+
+def kmp_layer_norm_workspace_bytes(rows: int, d: int, dtype) -> int:
+    return int(lib().kmp_layer_norm_workspace_bytes(_type(dtype, "x"), int(rows), int(d)))
+
+
+def kmp_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=None) -> None:
+    """Gradients of kmp_layer_norm from dy (rows, d): dx (rows, d) of x's type,
+    dgamma and dbeta (d) of gamma's; each may be None. The workspace has
+    kmp_layer_norm_workspace_bytes(rows, d, x.dtype) bytes."""
+    import torch
+    xp, rows, d, ldx = _matrix(x, "x")
+    dyp, _, _, lddy = _matrix(dy, "dy", rows, d, x.dtype)
+    dxp, lddx = None, d
+    if dx is not None:
+        dxp, _, _, lddx = _matrix(dx, "dx", rows, d, x.dtype)
+    xt = _type(x, "x")
+    w = next((t for t in (gamma, dgamma, dbeta) if t is not None), None)
+    wt = _type(w, "gamma") if w is not None else xt
+    wd = w.dtype if w is not None else None
+    sd = torch.float64 if xt == KMP_F64 else torch.float32
+    wsp, wsb = _workspace(workspace)
+    _check(lib().kmp_layer_norm_backward(
+        _stream_ptr(stream), xt, dyp, lddy, xp, ldx, rows, d, wt, _vector(gamma, "gamma", d, wd),
+        _vector(mean, "mean", rows, sd), _vector(rstd, "rstd", rows, sd), dxp, lddx,
+        _vector(dgamma, "dgamma", d, wd), _vector(dbeta, "dbeta", d, wd), wsp, wsb),
+        allow_maxiter=False)
+
+
+def kmp_quantize_rows(x, q, scale, stream=None) -> None:
+    """Rows of x (rows, d) in 8 bits: q (rows, d) int8, scale (rows) float32."""
+    import torch
+    xp, rows, d, ldx = _matrix(x, "x")
+    qp, _, _, ldq = _matrix(q, "q", rows, d, torch.int8)
+    _check(lib().kmp_quantize_rows(_stream_ptr(stream), _type(x, "x"), xp, rows, d, ldx, qp, ldq,
+                                   _vector(scale, "scale", rows, torch.float32)), allow_maxiter=False)
+
+
+def kmp_quantized_product(xq, xscale, wq, wscale, out, bias=None, stream=None) -> None:
+    """out (M, N) = xscale[m] wscale[n] sum_k xq[m, k] wq[n, k] + bias[n] for
+    int8 xq (M, K) and wq (N, K), float32 scales and bias, out of any of the
+    floating types up to 32 bits."""
+    import torch
+    xp, M, K, ldx = _matrix(xq, "xq", dtype=torch.int8)
+    wp, N, _, ldw = _matrix(wq, "wq", None, K, torch.int8)
+    op, _, _, ldo = _matrix(out, "out", M, N)
+    f = torch.float32
+    _check(lib().kmp_quantized_product(
+        _stream_ptr(stream), xp, ldx, _vector(xscale, "xscale", M, f), M, wp, ldw,
+        _vector(wscale, "wscale", N, f), N, K, _vector(bias, "bias", N, f), _type(out, "out"), op,
+        ldo), allow_maxiter=False)
+
+
+def kmp_token_logprobs_workspace_bytes(T: int, V: int, top: int = 0) -> int:
+    return int(lib().kmp_token_logprobs_workspace_bytes(int(T), int(V), int(top)))
+
+
+def kmp_token_logprobs(logits, tokens, logp, entropy=None, stats=None, top_id=None, top_logp=None,
+                       workspace=None, stream=None) -> None:
+    """Log probabilities of tokens (T; int32 or int64, negative: none) under the
+    rows of logits (T, V): logp and entropy (T) float32, stats (T, 2) float32
+    (maximum m, log sum exp(x - m); what the backward reads), the most likely
+    tokens top_id (T, k) int32 and their top_logp (T, k) float32; each output
+    may be None. The workspace has kmp_token_logprobs_workspace_bytes(T, V, k)
+    bytes."""
+    import torch
+    lp, T, V, ldl = _matrix(logits, "logits")
+    bits, tp = _tokens(tokens, T)
+    tops = [t.shape[-1] for t in (top_id, top_logp) if t is not None]
+    top = tops[0] if tops else 0
+    f = torch.float32
+    wsp, wsb = _workspace(workspace)
+    _check(lib().kmp_token_logprobs(
+        _stream_ptr(stream), _type(logits, "logits"), lp, T, V, ldl, bits, tp,
+        _vector(logp, "logp", T, f), _vector(entropy, "entropy", T, f), _vector(stats, "stats", 2 * T, f), top,
+        _vector(top_id, "top_id", T * top, torch.int32), _vector(top_logp, "top_logp", T * top, f),
+        wsp, wsb), allow_maxiter=False)
+
+
+def kmp_token_logprobs_backward(logits, tokens, stats, dlogp, dlogits, entropy=None, dentropy=None,
+                                stream=None) -> None:
+    """Gradient dlogits (T, V) of sum dlogp logp + dentropy entropy, from the
+    forward call's logits, tokens, stats and entropy; dlogp or dentropy may be
+    None. dlogits may be logits itself."""
+    import torch
+    lp, T, V, ldl = _matrix(logits, "logits")
+    dp, _, _, ldd = _matrix(dlogits, "dlogits", T, V, logits.dtype)
+    bits, tp = _tokens(tokens, T)
+    f = torch.float32
+    _check(lib().kmp_token_logprobs_backward(
+        _stream_ptr(stream), _type(logits, "logits"), lp, T, V, ldl, bits, tp,
+        _vector(stats, "stats", 2 * T, f), _vector(entropy, "entropy", T, f), _vector(dlogp, "dlogp", T, f),
+        _vector(dentropy, "dentropy", T, f), dp, ldd), allow_maxiter=False)
 
 
 def kmp_fit_path(stream, spec, X, y, sigmas, taus, lambdas, fold_id, V, workspace, ws_bytes,
