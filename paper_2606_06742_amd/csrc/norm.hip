@@ -11,6 +11,8 @@ namespace kmp {
 namespace {
 
 constexpr int BT = 256;                // threads of a workgroup
+// what is written: the norm in x's type or in 8 bits, or x itself in 8 bits
+enum { kNorm, kNormBytes, kBytesOfX };
 
 template <typename A>
 __device__ __forceinline__ A block_total(A v, A* red) {
@@ -43,6 +45,9 @@ __device__ __forceinline__ float block_most(float v, float* red) {
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 __device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
 
+// The larger, or NaN where either is NaN.
+__device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }
+
 // The factor 127 / a that takes a row into 8 bits, and its scale a / 127.
 // Below 2^-100 the factor would overflow: such rows are brought up by 2^100
 // first. A row with an infinity or NaN gets factor 0 and scale NaN.
@@ -60,11 +65,12 @@ struct ByteScale {
   }
 };
 
-// One workgroup per row, any length: a pass for the mean, one for the
+// One workgroup per row, any length (rows too long for the registers): a pass for the mean, one for the
 // variance, one for the largest |y| of the 8-bit form, one to write.
-template <typename T, typename W, bool BYTES, bool PLAIN>
+template <typename T, typename W, int MODE>
 __global__ __launch_bounds__(BT) void norm_row_kernel(NormArgs a) {
   typedef typename acc_of<T>::type A;
+  constexpr bool BYTES = MODE != kNorm, PLAIN = MODE == kBytesOfX;
   __shared__ A red[BT / 64];
   __shared__ float fred[BT / 64];
   const W* gamma = static_cast<const W*>(a.gamma);
@@ -111,6 +117,149 @@ __global__ __launch_bounds__(BT) void norm_row_kernel(NormArgs a) {
   }
 }
 
+// Rows that fit the registers of TPR threads, NV 16-byte vectors each: x is read
+// once. A thread's vectors are TPR apart, so a wavefront reads whole lines. The
+// sum over a row is a butterfly, then for TPR > 64 one exchange in LDS (slots
+// alternate between the sums, so one barrier each is enough). gamma and beta
+// stay in registers over the rows of a workgroup.
+constexpr int threads_of(int tpr) { return tpr > BT ? tpr : BT; }
+template <typename A, int TPR>
+__device__ __forceinline__ A row_total(A v, A (*red)[threads_of(TPR) / 64], int& slot) {
+#pragma unroll
+  for (int off = (TPR < 64 ? TPR : 64) / 2; off >= 1; off >>= 1) v += __shfl_xor(v, off, kWave);
+  if constexpr (TPR > 64) {
+    A* r = red[slot];
+    slot ^= 1;
+    if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = r[0];
+#pragma unroll
+    for (int i = 1; i < TPR / 64; ++i) v += r[i];
+  }
+  return v;
+}
+template <int TPR>
+__device__ __forceinline__ float row_most(float v, float (*red)[threads_of(TPR) / 64], int& slot) {
+#pragma unroll
+  for (int off = (TPR < 64 ? TPR : 64) / 2; off >= 1; off >>= 1) v = larger(v, __shfl_xor(v, off, kWave));
+  if constexpr (TPR > 64) {
+    float* r = red[slot];
+    slot ^= 1;
+    if ((threadIdx.x & 63) == 0) r[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = r[0];
+#pragma unroll
+    for (int i = 1; i < TPR / 64; ++i) v = larger(v, r[i]);
+  }
+  return v;
+}
+
+// Elements j .. j + N - 1 of a row of d, `fill` past its end.
+template <typename T, int N, typename A>
+__device__ __forceinline__ void load_part(const T* p, int j, int d, A fill, A (&v)[N]) {
+  if (j + N <= d) {
+    load_n(p + j, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = j + e < d ? (A)p[j + e] : fill;
+  }
+}
+template <typename T, int N, typename A>
+__device__ __forceinline__ void store_part(T* p, int j, int d, const A (&v)[N]) {
+  if (j + N <= d) {
+    store_n(p + j, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (j + e < d) p[j + e] = (T)v[e];
+  }
+}
+
+template <typename T, typename W, int MODE, int TPR, int NV>   // MODE: below
+__global__ __launch_bounds__(threads_of(TPR)) void norm_reg_kernel(NormArgs a) {
+  typedef typename acc_of<T>::type A;
+  constexpr int VEC = vec_of<T>(), RPB = threads_of(TPR) / TPR;
+  __shared__ A red[2][threads_of(TPR) / 64];
+  __shared__ float fred[2][threads_of(TPR) / 64];
+  int slot = 0, fslot = 0;
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
+  A g[NV][VEC], b[NV][VEC];
+  if constexpr (MODE != kBytesOfX) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = (t + i * TPR) * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) g[i][e] = 1, b[i][e] = 0;
+      if (a.gamma) load_part(static_cast<const W*>(a.gamma), j, d, (A)0, g[i]);
+      if (a.beta) load_part(static_cast<const W*>(a.beta), j, d, (A)0, b[i]);
+    }
+  }
+  // a workgroup's rows: every thread takes part in every round (the barriers)
+  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += (int64_t)gridDim.x * RPB) {
+    const bool live = r0 + sub < a.rows;
+    const int64_t r = live ? r0 + sub : a.rows - 1;
+    const T* x = static_cast<const T*>(a.x) + r * a.ldx;
+    A v[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_part(x, (t + i * TPR) * VEC, d, (A)0, v[i]);
+    if constexpr (MODE != kBytesOfX) {
+      A s = 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s += v[i][e];
+      const A mu = row_total<A, TPR>(s, red, slot) / (A)d;
+      A q = 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int j = (t + i * TPR) * VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[i][e] -= mu;
+        if (j + VEC > d) {                        // past the end: no deviation
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[i][e] = j + e < d ? v[i][e] : (A)0;
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) q += v[i][e] * v[i][e];
+      }
+      const A rs = inv_sqrt(row_total<A, TPR>(q, red, slot) / (A)d + (A)a.eps);
+      if (t == 0 && live) {
+        if (a.mean) static_cast<A*>(a.mean)[r] = mu;
+        if (a.rstd) static_cast<A*>(a.rstd)[r] = rs;
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[i][e] = v[i][e] * rs * g[i][e] + b[i][e];
+    }
+    if constexpr (MODE == kNorm) {
+      T* y = static_cast<T*>(a.y) + r * a.ldy;
+      if (live) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) store_part(y, (t + i * TPR) * VEC, d, v[i]);
+      }
+    } else {
+      float m = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) m = larger(m, fabsf((float)v[i][e]));
+      const ByteScale bs(row_most<TPR>(m, fred, fslot));
+      int8_t* y = static_cast<int8_t*>(a.y) + r * a.ldy;
+      if (live) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          int8_t q[VEC];
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) q[e] = bs((float)v[i][e]);
+          store_part(y, (t + i * TPR) * VEC, d, q);
+        }
+        if (t == 0) a.scale[r] = bs.scale;
+      }
+    }
+  }
+}
+
 // dx of one row per workgroup, any length.
 template <typename T, typename W>
 __global__ __launch_bounds__(BT) void norm_back_row_kernel(NormBackArgs a) {
@@ -137,6 +286,119 @@ __global__ __launch_bounds__(BT) void norm_back_row_kernel(NormBackArgs a) {
   }
 }
 
+// dx and the column sums in one pass over x and dy, rows in registers as in
+// norm_reg_kernel: workgroup b takes rows b, b + gridDim.x, .. (RPB at a time),
+// keeps its threads' columns of the two sums in registers, adds its RPB row
+// groups in LDS and writes partial[b]. The next rows' loads are in flight
+// during the current ones' sums.
+template <typename T, typename W, int TPR, int NV>
+__global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBackArgs a) {
+  typedef typename acc_of<T>::type A;
+  constexpr int VEC = vec_of<T>(), RPB = threads_of(TPR) / TPR;
+  __shared__ A red[2][threads_of(TPR) / 64];
+  __shared__ A sums[RPB > 1 ? TPR * NV * VEC : 1];
+  int slot = 0;
+  const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
+  A g[NV][VEC], dg[NV][VEC], db[NV][VEC], x[NV][VEC], w[NV][VEC];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) g[i][e] = 1, dg[i][e] = 0, db[i][e] = 0;
+  if (a.gamma) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) load_part(static_cast<const W*>(a.gamma), (t + i * TPR) * VEC, d, (A)0, g[i]);
+  }
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  const auto fetch = [&](int64_t r, T (&rx)[NV][VEC], T (&rd)[NV][VEC]) {
+    const T* px = static_cast<const T*>(a.x) + r * a.ldx;
+    const T* pd = static_cast<const T*>(a.dy) + r * a.lddy;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      load_part(px, (t + i * TPR) * VEC, d, (T)0.0f, rx[i]);
+      load_part(pd, (t + i * TPR) * VEC, d, (T)0.0f, rd[i]);
+    }
+  };
+  T nx[NV][VEC], nd[NV][VEC];
+  A nmu, nrs;
+  const auto next = [&](int64_t r) {
+    r = min(r, a.rows - 1);
+    fetch(r, nx, nd);
+    nmu = static_cast<const A*>(a.mean)[r];
+    nrs = static_cast<const A*>(a.rstd)[r];
+  };
+  int64_t r0 = (int64_t)blockIdx.x * RPB;
+  next(r0 + sub);
+  for (; r0 < a.rows; r0 += step) {
+    const int64_t r = r0 + sub;
+    const bool live = r < a.rows;
+    const A mu = nmu, rs = nrs;
+    A s1 = 0, s2 = 0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[i][e] = ((A)nx[i][e] - mu) * rs, w[i][e] = (A)nd[i][e];
+    }
+    if (r0 + step < a.rows) next(r + step);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        if (live) {                               // past the end: w = 0
+          dg[i][e] += w[i][e] * x[i][e];
+          db[i][e] += w[i][e];
+        }
+        w[i][e] *= g[i][e];
+        s1 += w[i][e];
+        s2 += w[i][e] * x[i][e];
+      }
+    }
+    if (a.dx) {
+      s1 = row_total<A, TPR>(s1, red, slot) / (A)d;
+      s2 = row_total<A, TPR>(s2, red, slot) / (A)d;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[i][e] = rs * (w[i][e] - s1 - x[i][e] * s2);
+      if (live) {
+        T* dx = static_cast<T*>(a.dx) + r * a.lddx;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) store_part(dx, (t + i * TPR) * VEC, d, w[i]);
+      }
+    }
+  }
+  if (!a.dgamma && !a.dbeta) return;
+  A* p = static_cast<A*>(a.partial) + (int64_t)blockIdx.x * 2 * a.d;
+  const auto write = [&](A (&v)[NV][VEC], A* out) {
+    if constexpr (RPB > 1) {
+      for (int q = RPB - 1; q > 0; --q) {         // row group q adds to what those above it left
+        if (sub == q) {
+#pragma unroll
+          for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              const int at = (i * VEC + e) * TPR + t;
+              sums[at] = q == RPB - 1 ? v[i][e] : sums[at] + v[i][e];
+            }
+        }
+        __syncthreads();
+      }
+      if (sub == 0) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[i][e] += sums[(i * VEC + e) * TPR + t];
+      }
+      __syncthreads();
+    }
+    if (sub == 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) store_part(out, (t + i * TPR) * VEC, d, v[i]);
+    }
+  };
+  write(dg, p);
+  write(db, p + a.d);
+}
+
 // Column sums of dy xh and dy over the strip blockIdx.y of rows, a thread per
 // column: partial[strip][0 or 1][column].
 template <typename T>
@@ -158,53 +420,99 @@ __global__ __launch_bounds__(BT) void norm_back_columns_kernel(NormBackArgs a, i
   p[a.d + j] = db;
 }
 
-// Adds the partial sums in a fixed order: 64 columns a workgroup, each
-// wavefront every fourth part, then the four.
+// Adds the partial sums in a fixed order: 64 columns a workgroup, each of its 16
+// wavefronts every sixteenth part, then the sixteen.
 template <typename A, typename W>
-__global__ __launch_bounds__(BT) void norm_back_join_kernel(const A* partial, int64_t parts, int64_t d,
-                                                            W* dgamma, W* dbeta) {
-  __shared__ A red[BT];
+__global__ __launch_bounds__(1024) void norm_back_join_kernel(const A* partial, int64_t parts, int64_t d,
+                                                              W* dgamma, W* dbeta) {
+  __shared__ A red[16][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t j = (int64_t)blockIdx.x * 64 + lane;
   W* out = blockIdx.y == 0 ? dgamma : dbeta;
   A s = 0;
-  if (j < d)
-    for (int64_t p = w; p < parts; p += BT / 64) s += partial[(p * 2 + blockIdx.y) * d + j];
-  red[threadIdx.x] = s;
+  if (j < d && out) {
+#pragma unroll 8
+    for (int64_t p = w; p < parts; p += 16) s += partial[(p * 2 + blockIdx.y) * d + j];
+  }
+  red[w][lane] = s;
   __syncthreads();
-  if (w == 0 && j < d && out) out[j] = (W)((red[lane] + red[64 + lane]) + (red[128 + lane] + red[192 + lane]));
+  if (w == 0 && j < d && out) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) s += red[i][lane];
+    out[j] = (W)s;
+  }
 }
 
-template <typename T, typename W>
-int forward_as(hipStream_t s, const NormArgs& a) {
-  const dim3 grid((unsigned)std::min<int64_t>(a.rows, 1 << 20)), block(BT);
-  if (!a.bytes)
-    hipLaunchKernelGGL((norm_row_kernel<T, W, false, false>), grid, block, 0, s, a);
-  else if (a.plain)
-    hipLaunchKernelGGL((norm_row_kernel<T, W, true, true>), grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((norm_row_kernel<T, W, true, false>), grid, block, 0, s, a);
+template <typename T, typename W, int MODE>
+int forward_mode(hipStream_t s, const NormArgs& a) {
+  const int64_t nv = ceil_div(a.d, vec_of<T>());
+  const auto grid = [&](int rpb) { return dim3((unsigned)std::min<int64_t>(ceil_div(a.rows, rpb), 2048)); };
+#define KMP_NORM_CASE(TPR, NV)                                                                   \
+  if (nv <= TPR * NV) {                                                                          \
+    hipLaunchKernelGGL((norm_reg_kernel<T, W, MODE, TPR, NV>), grid(threads_of(TPR) / TPR),      \
+                       dim3(threads_of(TPR)), 0, s, a);                                          \
+    KMP_LAUNCH_CHECK();                                                                          \
+    return 0;                                                                                    \
+  }
+  KMP_NORM_CASE(32, 1)
+  KMP_NORM_CASE(64, 1)
+  KMP_NORM_CASE(64, 2)
+  KMP_NORM_CASE(256, 1)
+  KMP_NORM_CASE(256, 2)
+  KMP_NORM_CASE(256, 4)
+  KMP_NORM_CASE(1024, 2)
+#undef KMP_NORM_CASE
+  hipLaunchKernelGGL((norm_row_kernel<T, W, MODE>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
+                     dim3(BT), 0, s, a);
   KMP_LAUNCH_CHECK();
   return 0;
 }
 
 template <typename T, typename W>
+int forward_as(hipStream_t s, const NormArgs& a) {
+  if (!a.bytes) return forward_mode<T, W, kNorm>(s, a);
+  if constexpr (sizeof(T) <= 4) {
+    if (!a.plain) return forward_mode<T, W, kNormBytes>(s, a);
+    if constexpr (sizeof(T) == sizeof(W)) return forward_mode<T, W, kBytesOfX>(s, a);
+  }
+  return KMP_EINVAL;                              // refused before
+}
+
+template <typename T, typename W>
 int backward_as(hipStream_t s, const NormBackArgs& a) {
   typedef typename acc_of<T>::type A;
-  const int64_t parts = norm_partials(a.xtype, a.rows, a.d);
-  if (a.rows > 0 && a.dx) {
-    hipLaunchKernelGGL((norm_back_row_kernel<T, W>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
-                       dim3(BT), 0, s, a);
+  const int64_t parts = norm_partials(a.xtype, a.rows, a.d), nv = ceil_div(a.d, vec_of<T>());
+  const bool weights = a.dgamma || a.dbeta;
+#define KMP_NORM_CASE(TPR, NV)                                                                             \
+  if (nv <= TPR * NV) {                                                                                    \
+    hipLaunchKernelGGL((norm_back_reg_kernel<T, W, TPR, NV>), dim3((unsigned)parts),                       \
+                       dim3(threads_of(TPR)), 0, s, a);                                                    \
+  } else
+  if (a.rows > 0) {
+    KMP_NORM_CASE(32, 1)
+    KMP_NORM_CASE(64, 1)
+    KMP_NORM_CASE(64, 2)
+    KMP_NORM_CASE(256, 1)
+    KMP_NORM_CASE(256, 2)
+    KMP_NORM_CASE(1024, 1)
+    // (two vectors of eight elements need more registers than 1024 threads have)
+    if (sizeof(T) >= 4 && nv <= 2048) {
+      hipLaunchKernelGGL((norm_back_reg_kernel<T, W, 1024, sizeof(T) >= 4 ? 2 : 1>), dim3((unsigned)parts),
+                         dim3(1024), 0, s, a);
+    } else {
+      if (a.dx)
+        hipLaunchKernelGGL((norm_back_row_kernel<T, W>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
+                           dim3(BT), 0, s, a);
+      if (weights)
+        hipLaunchKernelGGL((norm_back_columns_kernel<T>), dim3((unsigned)ceil_div(a.d, BT), (unsigned)parts),
+                           dim3(BT), 0, s, a, ceil_div(a.rows, parts));
+    }
     KMP_LAUNCH_CHECK();
   }
-  if (!a.dgamma && !a.dbeta) return 0;
-  if (parts > 0) {
-    hipLaunchKernelGGL((norm_back_columns_kernel<T>), dim3((unsigned)ceil_div(a.d, BT), (unsigned)parts),
-                       dim3(BT), 0, s, a, ceil_div(a.rows, parts));
-    KMP_LAUNCH_CHECK();
-  }
-  hipLaunchKernelGGL((norm_back_join_kernel<A, W>), dim3((unsigned)ceil_div(a.d, 64), 2), dim3(BT), 0, s,
-                     static_cast<const A*>(a.partial), parts, a.d, static_cast<W*>(a.dgamma),
+#undef KMP_NORM_CASE
+  if (!weights) return 0;
+  hipLaunchKernelGGL((norm_back_join_kernel<A, W>), dim3((unsigned)ceil_div(a.d, 64), 2), dim3(1024), 0, s,
+                     static_cast<const A*>(a.partial), a.rows > 0 ? parts : 0, a.d, static_cast<W*>(a.dgamma),
                      static_cast<W*>(a.dbeta));
   KMP_LAUNCH_CHECK();
   return 0;
@@ -212,8 +520,13 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
 
 }  // namespace
 
-// Strips of rows whose column sums are kept apart.
-int64_t norm_partials(int, int64_t rows, int64_t) { return std::min<int64_t>(ceil_div(rows, 32), 512); }
+// Workgroups of the backward pass, each with its own column sums: at least
+// four rounds of rows each, at most 512.
+int64_t norm_partials(int xtype, int64_t rows, int64_t d) {
+  const int64_t nv = ceil_div(d, 16 / (xtype == KMP_F64 ? 8 : xtype == KMP_F32 ? 4 : 2));
+  const int64_t rpb = nv <= 32 ? 8 : nv <= 128 ? 4 : 1;
+  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, 4 * rpb), 512));
+}
 
 int norm_forward(hipStream_t s, const NormArgs& a) {
   switch (a.xtype * 8 + a.wtype) {
