@@ -42,8 +42,8 @@ KernelClock* current_clock();
 void kc_begin(int cls, hipStream_t s);
 void kc_end(int cls, hipStream_t s, double bytes, double flops);
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
 
 // ---------------------------------------------------- MFMA f64 16x16x4 layout
 // v_mfma_f64_16x16x4_f64 on gfx950, per lane l of the wave: the A operand is

@@ -14,37 +14,37 @@
 namespace kmp {
 namespace {
 
-constexpr int BT = 256;
+constexpr int BT = 256;                // threads of a workgroup
+constexpr int CAP = 1024;              // candidates in LDS at a time
+constexpr int kMaxSegs = 64;           // segments of a row at most
 constexpr float kLog2e = 1.44269504088896340736f;
 
-// Largest value with NaN above all (so that it is never lost).
-__device__ __forceinline__ float most(float a, float b) { return a > b || a != a ? a : b; }
+// Differences to the maximum are held at -256, where exp is 0 in 32 bits: a
+// logit of -inf then adds 0 to s and to u. The maximum is NaN where any logit
+// is, which marks the row (s and u then hold nothing of use).
+__device__ __forceinline__ float most(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+__device__ __forceinline__ float held(float d) { return fmaxf(d, -256.0f); }
 
-// m = max, s and u of a part of a row (see above); s = 0 for an empty part or
-// one of nothing but -inf.
+// m, s and u of a part of a row; of an empty part, or one of nothing but -inf,
+// -inf, 0 and 0.
 struct Part { float m, s, u; };
 __device__ __forceinline__ Part join(const Part& a, const Part& b) {
   Part r;
   r.m = most(a.m, b.m);
-  if (!(r.m > -INFINITY)) {                 // both empty, or NaN
-    r.s = r.m != r.m ? r.m : 0.0f;
-    r.u = r.s;
-    return r;
-  }
-  const float da = a.s != 0.0f ? a.m - r.m : 0.0f, db = b.s != 0.0f ? b.m - r.m : 0.0f;
-  const float fa = a.s != 0.0f ? exp2f(da * kLog2e) : 0.0f, fb = b.s != 0.0f ? exp2f(db * kLog2e) : 0.0f;
-  // a part far below the maximum: its factor is 0, its distance unbounded
-  const float ua = fa > 0.0f ? fa * (a.u + da * a.s) : 0.0f, ub = fb > 0.0f ? fb * (b.u + db * b.s) : 0.0f;
+  const float da = held(a.m - r.m), db = held(b.m - r.m), fa = exp_of(da), fb = exp_of(db);
   r.s = fa * a.s + fb * b.s;
-  r.u = ua + ub;
+  r.u = fa * (a.u + da * a.s) + fb * (b.u + db * b.s);
   return r;
 }
-__device__ __forceinline__ Part shuffle_xor(const Part& p, int off) {
-  return Part{__shfl_xor(p.m, off, kWave), __shfl_xor(p.s, off, kWave), __shfl_xor(p.u, off, kWave)};
+__device__ __forceinline__ Part wave_join(Part p) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1)
+    p = join(p, Part{__shfl_xor(p.m, off, kWave), __shfl_xor(p.s, off, kWave), __shfl_xor(p.u, off, kWave)});
+  return p;
 }
 __device__ __forceinline__ Part block_join(Part p, Part* red) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) p = join(p, shuffle_xor(p, off));
+  p = wave_join(p);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = p;
   __syncthreads();
@@ -54,8 +54,28 @@ __device__ __forceinline__ Part block_join(Part p, Part* red) {
   return t;
 }
 
+// Adds N logits to a part: its maximum first, so that one rescaling serves all N.
+template <int N>
+__device__ __forceinline__ void absorb(Part& p, const float (&v)[N]) {
+  float c = p.m;
+#pragma unroll
+  for (int i = 0; i < N; ++i) c = most(c, v[i]);
+  const float dm = held(p.m - c), f = exp_of(dm);
+  p.u = f * (p.u + dm * p.s);
+  p.s *= f;
+  p.m = c;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = held(v[i] - c), e = exp_of(d);
+    p.s += e;
+    p.u += e * d;
+  }
+}
+
 // Order of the alternatives as one unsigned number: the value's bits mapped to
-// increasing order (NaN highest, -0 as 0) above the complemented index.
+// increasing order (NaN highest, -0 as 0) above the complemented index. No
+// value has key 0.
+typedef unsigned long long key_t;
 __device__ __forceinline__ uint32_t value_key(float v) {
   if (v != v) return 0xFFFFFFFFu;
   const uint32_t b = __float_as_uint(v + 0.0f);
@@ -64,9 +84,85 @@ __device__ __forceinline__ uint32_t value_key(float v) {
 __device__ __forceinline__ float key_value(uint32_t k) {
   return k == 0xFFFFFFFFu ? __builtin_nanf("") : __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
+__device__ __forceinline__ key_t key_of(float v, uint32_t index) { return (key_t)value_key(v) << 32 | (uint32_t)~index; }
 
-__device__ __forceinline__ int64_t token_at(const LogprobArgs& a, int64_t t) {
-  return a.wide ? static_cast<const int64_t*>(a.tokens)[t] : static_cast<const int32_t*>(a.tokens)[t];
+struct TopShared {
+  key_t keys[BT];                      // largest key of each thread
+  key_t list[CAP];
+  key_t bound;
+  int count, flagged;
+  uint8_t flag[BT];
+};
+
+// The k-th largest of the n different keys in `list` (k <= n), by counting the
+// larger ones of each. Ends with a barrier.
+__device__ __forceinline__ key_t kth_largest(const key_t* list, int n, int k, key_t* result) {
+  for (int i = threadIdx.x; i < n; i += BT) {
+    const key_t mine = list[i];
+    int larger = 0;
+    for (int j = 0; j < n; ++j) larger += list[j] > mine;
+    if (larger == k - 1) *result = mine;
+  }
+  __syncthreads();
+  return *result;
+}
+
+// The k largest of the keys that the threads hold: thread t's are visited by
+// visit(t, i) for i < per, each a call add(key); `mine` is the largest of this
+// thread's (0: it has none); its lower half need only make it different from
+// other threads'. Any k threads' largest values are those of k different keys,
+// so the k-th largest of the 256 bounds the k-th largest of all from below, and
+// only the threads at or above it (k, and those equal in value) need a second
+// look: their visits are spread over the workgroup. More candidates than the list holds (many equal values, or
+// the best ones all with one thread) raise the bound to the k-th largest of those
+// that were kept, and the visits are repeated. Writes the keys in order through
+// put(rank, key), 0 for ranks past the last key.
+template <typename Visit, typename Put>
+__device__ __forceinline__ void select_top(TopShared& sh, int k, key_t mine, int per, Visit visit, Put put) {
+  const int t = threadIdx.x;
+  __syncthreads();
+  sh.keys[t] = mine;
+  if (t == 0) sh.flagged = 0;
+  if (t < k) put(t, (key_t)0);
+  __syncthreads();
+  int larger = 0, last = 0;
+  for (int j = 0; j < BT; ++j) {
+    const key_t o = sh.keys[j];
+    larger += o > mine;
+    last += o == 0;
+  }
+  // the k-th largest, or 0 where fewer than k threads have a key
+  if (mine != 0 && larger == k - 1) sh.bound = mine;
+  if (t == 0 && BT - last < k) sh.bound = 0;
+  __syncthreads();
+  key_t bound = sh.bound >> 32 << 32;
+  if (mine != 0 && mine >= bound) sh.flag[atomicAdd(&sh.flagged, 1)] = (uint8_t)t;
+  int n;
+  for (;;) {
+    if (t == 0) sh.count = 0;
+    __syncthreads();
+    const int flagged = sh.flagged, items = flagged * per;
+    for (int i = t; i < items; i += BT)
+      visit((int)sh.flag[i % flagged], i / flagged, [&](key_t key) {
+        if (key < bound) return;
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < CAP) sh.list[at] = key;
+      });
+    __syncthreads();
+    n = sh.count;
+    if (n <= CAP) break;
+    bound = kth_largest(sh.list, CAP, k, &sh.bound);
+  }
+  for (int i = t; i < n; i += BT) {
+    const key_t key = sh.list[i];
+    int rank = 0;
+    for (int j = 0; j < n; ++j) rank += sh.list[j] > key;
+    if (rank < k) put(rank, key);
+  }
+}
+
+__device__ __forceinline__ int64_t token_at(const void* tokens, bool wide, int64_t t) {
+  return wide ? static_cast<const int64_t*>(tokens)[t] : static_cast<const int32_t*>(tokens)[t];
 }
 
 // A row's results from m, s, u: log p_j = (x_j - m) - log s, which keeps its
@@ -74,111 +170,223 @@ __device__ __forceinline__ int64_t token_at(const LogprobArgs& a, int64_t t) {
 struct Row { float m, logs; };
 template <typename T>
 __device__ __forceinline__ Row finish_row(const LogprobArgs& a, int64_t t, const Part& p) {
-  // s = 0 (all -inf): -inf; NaN or an infinite maximum: NaN
-  const Row r{p.m == INFINITY ? __builtin_nanf("") : p.m, p.m == INFINITY ? __builtin_nanf("") : logf(p.s)};
+  // a NaN or +inf: NaN; nothing but -inf: -inf
+  const bool nan = p.m != p.m || p.m == INFINITY, none = p.m == -INFINITY;
+  const float x = nan ? __builtin_nanf("") : -INFINITY;
+  const Row r{nan || none ? x : p.m, nan || none ? x : logf(p.s)};
   if (threadIdx.x == 0) {
     if (a.stats) {
       a.stats[2 * t] = r.m;
       a.stats[2 * t + 1] = r.logs;
     }
-    if (a.entropy)
-      a.entropy[t] = p.s == 0.0f ? 0.0f : r.logs != r.logs ? r.logs : fmaxf(r.logs - p.u / p.s, 0.0f);
+    if (a.entropy) a.entropy[t] = nan ? x : none ? 0.0f : fmaxf(r.logs - p.u / p.s, 0.0f);
     if (a.logp) {
-      const int64_t id = token_at(a, t);
+      const int64_t id = token_at(a.tokens, a.wide, t);
       float v = 0.0f;
       if (id >= a.V) v = __builtin_nanf("");
       else if (id >= 0)
-        v = p.s == 0.0f ? -INFINITY : ((float)static_cast<const T*>(a.logits)[t * a.ld + id] - r.m) - r.logs;
+        v = none ? -INFINITY : ((float)static_cast<const T*>(a.logits)[t * a.ld + id] - r.m) - r.logs;
       a.logp[t] = v;
     }
   }
   return r;
 }
+__device__ __forceinline__ void put_top(const LogprobArgs& a, int64_t t, const Row& row, int rank, key_t key) {
+  if (a.top_id) a.top_id[t * a.top + rank] = (int32_t)~(uint32_t)key;
+  if (a.top_logp)
+    a.top_logp[t * a.top + rank] =
+        row.m == -INFINITY ? -INFINITY : (key_value((uint32_t)(key >> 32)) - row.m) - row.logs;
+}
 
-// One workgroup per row; the alternatives one after another, each the largest
-// key below the last.
+// Partial results of segment g of row t, in the workspace: the parts, then the
+// keys of the segment's k best.
+__device__ __forceinline__ Part* parts_of(const LogprobArgs& a) { return static_cast<Part*>(a.workspace); }
+__device__ __forceinline__ key_t* keys_of(const LogprobArgs& a, int segs) {
+  return reinterpret_cast<key_t*>(static_cast<char*>(a.workspace) + round_up(a.T * segs * (int64_t)sizeof(Part), 16));
+}
+
+// One workgroup per segment of a row (segs of them, span elements each): one
+// pass of 16-byte loads, U in flight, every thread with its own maximum and
+// sums; then, where alternatives are asked for, a second look at the few threads
+// that can hold them. With one segment the row is finished here.
 template <typename T>
-__global__ __launch_bounds__(BT) void logprob_row_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(BT) void logprob_span_kernel(LogprobArgs a, int segs, int64_t span) {
+  constexpr int VEC = vec_of<T>(), U = 16 / VEC;
   __shared__ Part red[BT / 64];
-  __shared__ unsigned long long kred[BT / 64];
-  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
-    const T* x = static_cast<const T*>(a.logits) + t * a.ld;
-    Part p{-INFINITY, 0.0f, 0.0f};
-    for (int64_t j = threadIdx.x; j < a.V; j += BT) {
-      const float v = (float)x[j];
-      p = join(p, Part{v, v > -INFINITY || v != v ? 1.0f : 0.0f, 0.0f});
-    }
-    p = block_join(p, red);
-    const Row row = finish_row<T>(a, t, p);
-    unsigned long long last = ~0ull;
-    for (int k = 0; k < a.top; ++k) {
-      unsigned long long best = 0;
-      for (int64_t j = threadIdx.x; j < a.V; j += BT) {
-        const unsigned long long key = (unsigned long long)value_key((float)x[j]) << 32 | (uint32_t)~(uint32_t)j;
-        if (key < last && key > best) best = key;
-      }
+  __shared__ TopShared sh;
+  const int64_t units = a.T * segs;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int64_t t = unit / segs, e0 = (unit % segs) * span;
+    const int64_t len = min(span, a.V - e0);
+    const T* x = static_cast<const T*>(a.logits) + t * a.ld + e0;
+    const auto load = [&](int64_t j, float (&v)[VEC]) {    // -inf past the end
+      if (j + VEC <= len) {
+        load_n(x + j, v);
+      } else {
 #pragma unroll
-      for (int off = 32; off >= 1; off >>= 1) {
-        const unsigned long long o = __shfl_xor(best, off, kWave);
-        best = o > best ? o : best;
+        for (int e = 0; e < VEC; ++e) v[e] = j + e < len ? (float)x[j + e] : -INFINITY;
       }
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) kred[threadIdx.x >> 6] = best;
-      __syncthreads();
-      for (int i = 0; i < BT / 64; ++i) best = kred[i] > best ? kred[i] : best;
-      last = best;
-      if (threadIdx.x == 0) {
-        if (a.top_id) a.top_id[t * a.top + k] = (int32_t)~(uint32_t)best;
-        if (a.top_logp)
-          a.top_logp[t * a.top + k] = p.s == 0.0f ? -INFINITY : (key_value((uint32_t)(best >> 32)) - row.m) - row.logs;
+    };
+    Part p{-INFINITY, 0.0f, 0.0f};
+    int64_t j = threadIdx.x * VEC;
+    for (; j + (U - 1) * BT * VEC + VEC <= len; j += U * BT * VEC) {
+      float v[U * VEC];
+#pragma unroll
+      for (int i = 0; i < U; ++i) load_n(x + j + i * BT * VEC, reinterpret_cast<float(&)[VEC]>(v[i * VEC]));
+      absorb(p, v);
+    }
+    for (; j < len; j += BT * VEC) {
+      float v[VEC];
+      load(j, v);
+      absorb(p, v);
+    }
+    const float own = p.m;
+    p = block_join(p, red);
+    Row row{0.0f, 0.0f};
+    if (segs == 1)
+      row = finish_row<T>(a, t, p);
+    else if (threadIdx.x == 0)
+      parts_of(a)[unit] = p;
+    if (a.top > 0) {
+      // a thread's largest key with the index left out: at least its real ones
+      const key_t mine = threadIdx.x * VEC < len ? (key_t)value_key(own) << 32 | threadIdx.x : 0;
+      select_top(
+          sh, a.top, mine, (int)ceil_div(len, BT * VEC),
+          [&](int owner, int i, auto add) {
+            const int64_t at = ((int64_t)i * BT + owner) * VEC;
+            if (at >= len) return;
+            float v[VEC];
+            load(at, v);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+              if (at + e < len) add(key_of(v[e], (uint32_t)(e0 + at + e)));
+          },
+          [&](int rank, key_t key) {
+            if (segs > 1) keys_of(a, segs)[unit * a.top + rank] = key;
+            else if (key != 0) put_top(a, t, row, rank, key);
+          });
+    }
+  }
+}
+
+// Joins the segments of one row per workgroup.
+template <typename T>
+__global__ __launch_bounds__(BT) void logprob_join_kernel(LogprobArgs a, int segs) {
+  __shared__ TopShared sh;
+  const int lane = threadIdx.x & 63;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+    // every wavefront joins all parts (at most 64 of them) for itself
+    const Part none{-INFINITY, 0.0f, 0.0f};
+    const Row row = finish_row<T>(a, t, wave_join(lane < segs ? parts_of(a)[t * segs + lane] : none));
+    if (a.top > 0) {
+      const key_t* keys = keys_of(a, segs) + t * segs * a.top;
+      const int n = segs * a.top;
+      key_t mine = 0;
+      for (int i = threadIdx.x; i < n; i += BT) mine = max(mine, keys[i]);
+      select_top(
+          sh, a.top, mine, (n + BT - 1) / BT,
+          [&](int owner, int i, auto add) {
+            const int at = i * BT + owner;
+            if (at < n && keys[at] != 0) add(keys[at]);
+          },
+          [&](int rank, key_t key) {
+            if (key != 0) put_top(a, t, row, rank, key);
+          });
+    }
+  }
+}
+
+// The gradient, one workgroup per 4 vectors of its threads: reads a logit,
+// writes its gradient, an exponential between.
+template <typename T>
+__global__ __launch_bounds__(BT) void logprob_back_kernel(LogprobBackArgs a, int64_t chunks) {
+  constexpr int VEC = vec_of<T>(), U = 4;
+  const int64_t units = a.T * chunks;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int64_t t = unit / chunks, j0 = (unit % chunks) * (U * BT * VEC) + threadIdx.x * VEC;
+    const T* x = static_cast<const T*>(a.logits) + t * a.ld;
+    T* dx = static_cast<T*>(a.dlogits) + t * a.ldd;
+    const float m = a.stats[2 * t], logs = a.stats[2 * t + 1];
+    const float h = a.dentropy ? a.dentropy[t] : 0.0f, H = a.dentropy ? a.entropy[t] : 0.0f;
+    int64_t id = a.dlogp ? token_at(a.tokens, a.wide, t) : -1;
+    float g = id >= 0 ? a.dlogp[t] : 0.0f;
+    if (id >= a.V || logs != logs) g = __builtin_nanf("");
+    if (m == -INFINITY) id = -1;
+    float v[U][VEC];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int64_t j = j0 + i * BT * VEC;
+      if (j + VEC <= a.V) {
+        load_n(x + j, v[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) v[i][e] = j + e < a.V ? (float)x[j + e] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int64_t j = j0 + i * BT * VEC;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        const float lp = held((v[i][e] - m) - logs);       // -inf: p = 0, no term
+        v[i][e] = -exp_of(lp) * (g + h * (lp + H));
+      }
+      if (id >= j && id < j + VEC) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (j + e == id) v[i][e] += g;
+      }
+      if (j + VEC <= a.V) {
+        store_n(dx + j, v[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (j + e < a.V) dx[j + e] = (T)v[i][e];
       }
     }
   }
 }
 
-// The gradient of one row, elements blockIdx.x .. of it.
-template <typename T>
-__global__ __launch_bounds__(BT) void logprob_back_kernel(LogprobBackArgs a) {
-  for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
-    const T* x = static_cast<const T*>(a.logits) + t * a.ld;
-    T* dx = static_cast<T*>(a.dlogits) + t * a.ldd;
-    int64_t id = -1;
-    if (a.tokens && a.dlogp)
-      id = a.wide ? static_cast<const int64_t*>(a.tokens)[t] : static_cast<const int32_t*>(a.tokens)[t];
-    const float m = a.stats[2 * t], logs = a.stats[2 * t + 1];
-    const float g = id < 0 ? 0.0f : id >= a.V ? __builtin_nanf("") : a.dlogp[t];
-    const float h = a.dentropy ? a.dentropy[t] : 0.0f;
-    const float H = a.dentropy ? a.entropy[t] : 0.0f;
-    const bool none = m == -INFINITY && g == g;
-    for (int64_t j = (int64_t)blockIdx.x * BT + threadIdx.x; j < a.V; j += (int64_t)gridDim.x * BT) {
-      const float v = (float)x[j];
-      const float lp = (v - m) - logs;
-      // -inf: no probability and no term (unless the row is NaN)
-      float r = none || (v == -INFINITY && logs == logs) ? (g != g ? g : 0.0f) : -exp2f(lp * kLog2e) * (g + h * (lp + H));
-      if (j == id && !none) r += g;
-      dx[j] = (T)r;
-    }
-  }
+// Segments of a row: one where there are rows enough for the chip (four
+// workgroups a compute unit), else as many as make them so, of at least 4096
+// elements.
+struct Split { int segs; int64_t span; };
+Split split(int64_t T, int64_t V) {
+  const int64_t segs = std::min<int64_t>({1024 / std::max<int64_t>(T, 1), ceil_div(V, 4096), kMaxSegs});
+  if (segs <= 1) return {1, V};
+  const int64_t span = round_up(ceil_div(V, segs), 1024);
+  return {(int)ceil_div(V, span), span};
 }
 
 template <typename T>
 int forward_as(hipStream_t s, const LogprobArgs& a) {
-  hipLaunchKernelGGL(logprob_row_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T, 1 << 20)), dim3(BT), 0, s, a);
+  const auto [segs, span] = split(a.T, a.V);
+  const int64_t units = a.T * segs;
+  hipLaunchKernelGGL(logprob_span_kernel<T>, dim3((unsigned)std::min<int64_t>(units, 1 << 20)), dim3(BT), 0, s, a,
+                     segs, span);
   KMP_LAUNCH_CHECK();
+  if (segs > 1) {
+    hipLaunchKernelGGL(logprob_join_kernel<T>, dim3((unsigned)a.T), dim3(BT), 0, s, a, segs);
+    KMP_LAUNCH_CHECK();
+  }
   return 0;
 }
 template <typename T>
 int backward_as(hipStream_t s, const LogprobBackArgs& a) {
-  hipLaunchKernelGGL(logprob_back_kernel<T>,
-                     dim3((unsigned)std::min<int64_t>(ceil_div(a.V, BT), 1024), (unsigned)std::min<int64_t>(a.T, 65535)),
-                     dim3(BT), 0, s, a);
+  const int64_t chunks = ceil_div(a.V, 4 * BT * vec_of<T>());
+  hipLaunchKernelGGL(logprob_back_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T * chunks, 1 << 20)), dim3(BT), 0, s,
+                     a, chunks);
   KMP_LAUNCH_CHECK();
   return 0;
 }
 
 }  // namespace
 
-size_t logprob_workspace(int64_t, int64_t, int) { return 256; }
+size_t logprob_workspace(int64_t T, int64_t V, int top) {
+  const int segs = split(T, V).segs;
+  if (segs == 1) return 256;
+  return (size_t)(round_up(T * segs * (int64_t)sizeof(Part), 16) + T * segs * top * (int64_t)sizeof(key_t));
+}
 
 int token_logprobs(hipStream_t s, const LogprobArgs& a) {
   switch (a.type) {
