@@ -15,7 +15,7 @@ namespace kmp {
 namespace {
 
 constexpr int BT = 256;                // threads of a workgroup
-constexpr int CAP = 1024;              // candidates in LDS at a time
+constexpr int CAP = 512;               // candidates in LDS at a time
 constexpr int kMaxSegs = 64;           // segments of a row at most
 constexpr float kLog2e = 1.44269504088896340736f;
 
@@ -54,18 +54,35 @@ __device__ __forceinline__ Part block_join(Part p, Part* red) {
   return t;
 }
 
-// Adds N logits to a part: its maximum first, so that one rescaling serves all N.
-template <int N>
-__device__ __forceinline__ void absorb(Part& p, const float (&v)[N]) {
-  float c = p.m;
+// Adds U vectors of N logits to a part: their maximum first, so that one
+// rescaling serves all. With TOP, `at` follows the first vector that holds the
+// part's maximum (NaN, too): j + i * step for vector i.
+template <bool TOP, int U, int N>
+__device__ __forceinline__ void absorb(Part& p, const float (&w)[U][N], uint32_t& at, uint32_t j, uint32_t step) {
+  float c = p.m, one[U];
+  const float(&v)[U * N] = reinterpret_cast<const float(&)[U * N]>(w);
 #pragma unroll
-  for (int i = 0; i < N; ++i) c = most(c, v[i]);
+  for (int i = 0; i < U; ++i) {
+    one[i] = w[i][0];
+#pragma unroll
+    for (int e = 1; e < N; ++e) one[i] = most(one[i], w[i][e]);
+  }
+  if constexpr (TOP) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (one[i] > c || (one[i] != one[i] && c == c)) at = j + i * step;
+      c = most(c, one[i]);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < U; ++i) c = most(c, one[i]);
+  }
   const float dm = held(p.m - c), f = exp_of(dm);
   p.u = f * (p.u + dm * p.s);
   p.s *= f;
   p.m = c;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
+  for (int i = 0; i < U * N; ++i) {
     const float d = held(v[i] - c), e = exp_of(d);
     p.s += e;
     p.u += e * d;
@@ -87,61 +104,55 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 __device__ __forceinline__ key_t key_of(float v, uint32_t index) { return (key_t)value_key(v) << 32 | (uint32_t)~index; }
 
 struct TopShared {
-  key_t keys[BT];                      // largest key of each thread
-  key_t list[CAP];
+  key_t groups[64];
+  key_t list[CAP], few[CAP];
   key_t bound;
   int count, flagged;
   uint8_t flag[BT];
 };
 
-// The k-th largest of the n different keys in `list` (k <= n), by counting the
-// larger ones of each. Ends with a barrier.
-__device__ __forceinline__ key_t kth_largest(const key_t* list, int n, int k, key_t* result) {
-  for (int i = threadIdx.x; i < n; i += BT) {
-    const key_t mine = list[i];
-    int larger = 0;
-    for (int j = 0; j < n; ++j) larger += list[j] > mine;
-    if (larger == k - 1) *result = mine;
-  }
+// The k-th largest of the 64 groups' maxima, a group being four neighbouring
+// threads, or 0 where fewer than k <= 64 groups have a key. Every lane counts the
+// larger ones of one group's; all wavefronts do the same. Starts and ends with a
+// barrier.
+__device__ __forceinline__ key_t kth_of_groups(TopShared& sh, int k, key_t mine) {
+  mine = max(mine, (key_t)__shfl_xor(mine, 1, kWave));
+  mine = max(mine, (key_t)__shfl_xor(mine, 2, kWave));
   __syncthreads();
-  return *result;
+  if ((threadIdx.x & 3) == 0) sh.groups[threadIdx.x >> 2] = mine;
+  if (threadIdx.x == 0) sh.bound = 0;
+  __syncthreads();
+  const key_t own = sh.groups[threadIdx.x & 63];
+  int larger = 0;
+#pragma unroll
+  for (int j = 0; j < 64; ++j) larger += sh.groups[j] > own;
+  if (threadIdx.x < 64 && own != 0 && larger == k - 1) sh.bound = own;
+  __syncthreads();
+  return sh.bound;
 }
 
 // The k largest of the keys that the threads hold: thread t's are visited by
-// visit(t, i) for i < per, each a call add(key); `mine` is the largest of this
-// thread's (0: it has none); its lower half need only make it different from
-// other threads'. Any k threads' largest values are those of k different keys,
-// so the k-th largest of the 256 bounds the k-th largest of all from below, and
-// only the threads at or above it (k, and those equal in value) need a second
-// look: their visits are spread over the workgroup. More candidates than the list holds (many equal values, or
-// the best ones all with one thread) raise the bound to the k-th largest of those
-// that were kept, and the visits are repeated. Writes the keys in order through
-// put(rank, key), 0 for ranks past the last key.
+// visit(t, i) for i < per, each a call add(key); its largest lies in [lower,
+// upper] (0: it has none; different threads' lowers differ). The largest keys of
+// any k groups are k different ones, so the k-th largest lower bounds the k-th
+// largest key from below, and only threads whose upper reaches it (24 on average
+// for k = 20) need a second look: their visits are spread over the workgroup.
+// More candidates than the list holds (the best ones all with one thread, say)
+// raise the bound by those that were kept, in the same way, and the visits are
+// repeated: as the keys all differ, the bound grows every time. Writes the keys
+// in order through put(rank, key), 0 for ranks past the last key.
 template <typename Visit, typename Put>
-__device__ __forceinline__ void select_top(TopShared& sh, int k, key_t mine, int per, Visit visit, Put put) {
+__device__ __forceinline__ void select_top(TopShared& sh, int k, key_t lower, key_t upper, int per, Visit visit, Put put) {
   const int t = threadIdx.x;
-  __syncthreads();
-  sh.keys[t] = mine;
-  if (t == 0) sh.flagged = 0;
+  key_t bound = kth_of_groups(sh, k, lower);
   if (t < k) put(t, (key_t)0);
+  if (t == 0) sh.flagged = sh.count = 0;
   __syncthreads();
-  int larger = 0, last = 0;
-  for (int j = 0; j < BT; ++j) {
-    const key_t o = sh.keys[j];
-    larger += o > mine;
-    last += o == 0;
-  }
-  // the k-th largest, or 0 where fewer than k threads have a key
-  if (mine != 0 && larger == k - 1) sh.bound = mine;
-  if (t == 0 && BT - last < k) sh.bound = 0;
+  if (lower != 0 && upper >= bound) sh.flag[atomicAdd(&sh.flagged, 1)] = (uint8_t)t;
   __syncthreads();
-  key_t bound = sh.bound >> 32 << 32;
-  if (mine != 0 && mine >= bound) sh.flag[atomicAdd(&sh.flagged, 1)] = (uint8_t)t;
+  const int flagged = sh.flagged, items = flagged * per;
   int n;
   for (;;) {
-    if (t == 0) sh.count = 0;
-    __syncthreads();
-    const int flagged = sh.flagged, items = flagged * per;
     for (int i = t; i < items; i += BT)
       visit((int)sh.flag[i % flagged], i / flagged, [&](key_t key) {
         if (key < bound) return;
@@ -151,12 +162,28 @@ __device__ __forceinline__ void select_top(TopShared& sh, int k, key_t mine, int
     __syncthreads();
     n = sh.count;
     if (n <= CAP) break;
-    bound = kth_largest(sh.list, CAP, k, &sh.bound);
+    bound = kth_of_groups(sh, k, max(sh.list[t], sh.list[t + BT]));
+    if (t == 0) sh.count = 0;
+    __syncthreads();
+  }
+  // a long list (equal values below a bound of the value alone) once more by its
+  // own bound, then every key's place is the number of larger ones
+  const key_t* list = sh.list;
+  if (n > 96) {
+    bound = kth_of_groups(sh, k, max(t < n ? sh.list[t] : (key_t)0, t + BT < n ? sh.list[t + BT] : (key_t)0));
+    if (t == 0) sh.count = 0;
+    __syncthreads();
+    for (int i = t; i < n; i += BT)
+      if (sh.list[i] >= bound) sh.few[atomicAdd(&sh.count, 1)] = sh.list[i];
+    __syncthreads();
+    n = sh.count;
+    list = sh.few;
   }
   for (int i = t; i < n; i += BT) {
-    const key_t key = sh.list[i];
+    const key_t key = list[i];
     int rank = 0;
-    for (int j = 0; j < n; ++j) rank += sh.list[j] > key;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += list[j] > key;
     if (rank < k) put(rank, key);
   }
 }
@@ -205,21 +232,22 @@ __device__ __forceinline__ key_t* keys_of(const LogprobArgs& a, int segs) {
   return reinterpret_cast<key_t*>(static_cast<char*>(a.workspace) + round_up(a.T * segs * (int64_t)sizeof(Part), 16));
 }
 
-// One workgroup per segment of a row (segs of them, span elements each): one
-// pass of 16-byte loads, U in flight, every thread with its own maximum and
-// sums; then, where alternatives are asked for, a second look at the few threads
-// that can hold them. With one segment the row is finished here.
-template <typename T>
-__global__ __launch_bounds__(BT) void logprob_span_kernel(LogprobArgs a, int segs, int64_t span) {
+// One workgroup per segment of a row (gridDim.x of them, span elements each): one
+// pass of 16-byte loads, U in flight, every thread with its own maximum and sums;
+// with TOP a second look at the few threads that can hold the alternatives. With
+// one segment the row is finished here.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(BT, 8) void logprob_span_kernel(LogprobArgs a, int64_t span) {
   constexpr int VEC = vec_of<T>(), U = 16 / VEC;
+  constexpr uint32_t STEP = BT * VEC;
   __shared__ Part red[BT / 64];
   __shared__ TopShared sh;
-  const int64_t units = a.T * segs;
-  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t t = unit / segs, e0 = (unit % segs) * span;
-    const int64_t len = min(span, a.V - e0);
+  const int segs = gridDim.x;
+  for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
+    const int64_t unit = t * segs + blockIdx.x, e0 = blockIdx.x * span;
+    const uint32_t len = (uint32_t)min(span, a.V - e0);
     const T* x = static_cast<const T*>(a.logits) + t * a.ld + e0;
-    const auto load = [&](int64_t j, float (&v)[VEC]) {    // -inf past the end
+    const auto load = [&](uint32_t j, float (&v)[VEC]) {   // -inf past the end
       if (j + VEC <= len) {
         load_n(x + j, v);
       } else {
@@ -228,17 +256,17 @@ __global__ __launch_bounds__(BT) void logprob_span_kernel(LogprobArgs a, int seg
       }
     };
     Part p{-INFINITY, 0.0f, 0.0f};
-    int64_t j = threadIdx.x * VEC;
-    for (; j + (U - 1) * BT * VEC + VEC <= len; j += U * BT * VEC) {
-      float v[U * VEC];
+    uint32_t j = threadIdx.x * VEC, at = j;       // (a first vector of nothing but -inf is at j)
+    for (; j + (U - 1) * STEP + VEC <= len; j += U * STEP) {
+      float v[U][VEC];
 #pragma unroll
-      for (int i = 0; i < U; ++i) load_n(x + j + i * BT * VEC, reinterpret_cast<float(&)[VEC]>(v[i * VEC]));
-      absorb(p, v);
+      for (int i = 0; i < U; ++i) load_n(x + j + i * STEP, v[i]);
+      absorb<TOP>(p, v, at, j, STEP);
     }
-    for (; j < len; j += BT * VEC) {
-      float v[VEC];
-      load(j, v);
-      absorb(p, v);
+    for (; j < len; j += STEP) {
+      float v[1][VEC];
+      load(j, v[0]);
+      absorb<TOP>(p, v, at, j, STEP);
     }
     const float own = p.m;
     p = block_join(p, red);
@@ -247,19 +275,21 @@ __global__ __launch_bounds__(BT) void logprob_span_kernel(LogprobArgs a, int seg
       row = finish_row<T>(a, t, p);
     else if (threadIdx.x == 0)
       parts_of(a)[unit] = p;
-    if (a.top > 0) {
-      // a thread's largest key with the index left out: at least its real ones
-      const key_t mine = threadIdx.x * VEC < len ? (key_t)value_key(own) << 32 | threadIdx.x : 0;
+    if constexpr (TOP) {
+      // this thread's best key lies between these two: its vector is known, not
+      // the place in it
+      const bool any = threadIdx.x * VEC < len;
+      const key_t lower = any ? key_of(own, (uint32_t)e0 + at + (VEC - 1)) : 0, upper = any ? key_of(own, (uint32_t)e0 + at) : 0;
       select_top(
-          sh, a.top, mine, (int)ceil_div(len, BT * VEC),
+          sh, a.top, lower, upper, (int)((len + STEP - 1) / STEP),
           [&](int owner, int i, auto add) {
-            const int64_t at = ((int64_t)i * BT + owner) * VEC;
+            const uint32_t at = i * STEP + owner * VEC;
             if (at >= len) return;
             float v[VEC];
             load(at, v);
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-              if (at + e < len) add(key_of(v[e], (uint32_t)(e0 + at + e)));
+              if (at + e < len) add(key_of(v[e], (uint32_t)e0 + at + e));
           },
           [&](int rank, key_t key) {
             if (segs > 1) keys_of(a, segs)[unit * a.top + rank] = key;
@@ -284,7 +314,7 @@ __global__ __launch_bounds__(BT) void logprob_join_kernel(LogprobArgs a, int seg
       key_t mine = 0;
       for (int i = threadIdx.x; i < n; i += BT) mine = max(mine, keys[i]);
       select_top(
-          sh, a.top, mine, (n + BT - 1) / BT,
+          sh, a.top, mine, mine, (n + BT - 1) / BT,
           [&](int owner, int i, auto add) {
             const int at = i * BT + owner;
             if (at < n && keys[at] != 0) add(keys[at]);
@@ -297,52 +327,55 @@ __global__ __launch_bounds__(BT) void logprob_join_kernel(LogprobArgs a, int seg
 }
 
 // The gradient, one workgroup per 4 vectors of its threads: reads a logit,
-// writes its gradient, an exponential between.
+// writes its gradient, an exponential between. The last rows come first: the
+// forward call read them last, so that the last-level cache still has them.
 template <typename T>
-__global__ __launch_bounds__(BT) void logprob_back_kernel(LogprobBackArgs a, int64_t chunks) {
-  constexpr int VEC = vec_of<T>(), U = 4;
-  const int64_t units = a.T * chunks;
-  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t t = unit / chunks, j0 = (unit % chunks) * (U * BT * VEC) + threadIdx.x * VEC;
-    const T* x = static_cast<const T*>(a.logits) + t * a.ld;
-    T* dx = static_cast<T*>(a.dlogits) + t * a.ldd;
-    const float m = a.stats[2 * t], logs = a.stats[2 * t + 1];
-    const float h = a.dentropy ? a.dentropy[t] : 0.0f, H = a.dentropy ? a.entropy[t] : 0.0f;
-    int64_t id = a.dlogp ? token_at(a.tokens, a.wide, t) : -1;
-    float g = id >= 0 ? a.dlogp[t] : 0.0f;
-    if (id >= a.V || logs != logs) g = __builtin_nanf("");
-    if (m == -INFINITY) id = -1;
-    float v[U][VEC];
+__global__ __launch_bounds__(BT) void logprob_back_kernel(LogprobBackArgs a) {
+  constexpr int VEC = vec_of<T>(), U = 4, FULL = U * BT * VEC;
+  const int64_t t = a.T - 1 - ((int64_t)blockIdx.z * gridDim.y + blockIdx.y);
+  if (t < 0) return;
+  const int64_t base = (int64_t)blockIdx.x * FULL;
+  const int left = (int)min(a.V - base, (int64_t)FULL);
+  const T* x = static_cast<const T*>(a.logits) + t * a.ld + base;
+  T* dx = static_cast<T*>(a.dlogits) + t * a.ldd + base;
+  float v[U][VEC];
+  if (left == FULL) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) load_n(x + (threadIdx.x + i * BT) * VEC, v[i]);
+  } else {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int64_t j = j0 + i * BT * VEC;
-      if (j + VEC <= a.V) {
-        load_n(x + j, v[i]);
-      } else {
+      const int j = (threadIdx.x + i * BT) * VEC;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[i][e] = j + e < a.V ? (float)x[j + e] : 0.0f;
-      }
+      for (int e = 0; e < VEC; ++e) v[i][e] = j + e < left ? (float)x[j + e] : 0.0f;
     }
+  }
+  const float m = a.stats[2 * t], logs = a.stats[2 * t + 1];
+  const float h = a.dentropy ? a.dentropy[t] : 0.0f, H = a.dentropy ? a.entropy[t] : 0.0f;
+  const int64_t id = a.dlogp ? token_at(a.tokens, a.wide, t) : -1;
+  float g = id >= 0 ? a.dlogp[t] : 0.0f;
+  if (id >= a.V || logs != logs) g = __builtin_nanf("");
+  // the token's place in this chunk, if it is there
+  const int at = m > -INFINITY && id >= base && id - base < left ? (int)(id - base) : -1;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int64_t j = j0 + i * BT * VEC;
+  for (int i = 0; i < U; ++i) {
+    const int j = (threadIdx.x + i * BT) * VEC;
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float lp = held((v[i][e] - m) - logs);       // -inf: p = 0, no term
-        v[i][e] = -exp_of(lp) * (g + h * (lp + H));
-      }
-      if (id >= j && id < j + VEC) {
+    for (int e = 0; e < VEC; ++e) {
+      const float lp = held((v[i][e] - m) - logs);         // -inf: p = 0, no term
+      v[i][e] = -exp_of(lp) * (g + h * (lp + H));
+    }
+    if (at >= j && at < j + VEC) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (j + e == id) v[i][e] += g;
-      }
-      if (j + VEC <= a.V) {
-        store_n(dx + j, v[i]);
-      } else {
+      for (int e = 0; e < VEC; ++e)
+        if (j + e == at) v[i][e] += g;
+    }
+    if (left == FULL) {
+      store_n(dx + j, v[i]);
+    } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (j + e < a.V) dx[j + e] = (T)v[i][e];
-      }
+      for (int e = 0; e < VEC; ++e)
+        if (j + e < left) dx[j + e] = (T)v[i][e];
     }
   }
 }
@@ -361,9 +394,11 @@ Split split(int64_t T, int64_t V) {
 template <typename T>
 int forward_as(hipStream_t s, const LogprobArgs& a) {
   const auto [segs, span] = split(a.T, a.V);
-  const int64_t units = a.T * segs;
-  hipLaunchKernelGGL(logprob_span_kernel<T>, dim3((unsigned)std::min<int64_t>(units, 1 << 20)), dim3(BT), 0, s, a,
-                     segs, span);
+  const dim3 grid(segs, (unsigned)std::min<int64_t>(a.T, 65535));
+  if (a.top > 0)
+    hipLaunchKernelGGL((logprob_span_kernel<T, true>), grid, dim3(BT), 0, s, a, span);
+  else
+    hipLaunchKernelGGL((logprob_span_kernel<T, false>), grid, dim3(BT), 0, s, a, span);
   KMP_LAUNCH_CHECK();
   if (segs > 1) {
     hipLaunchKernelGGL(logprob_join_kernel<T>, dim3((unsigned)a.T), dim3(BT), 0, s, a, segs);
@@ -373,9 +408,10 @@ int forward_as(hipStream_t s, const LogprobArgs& a) {
 }
 template <typename T>
 int backward_as(hipStream_t s, const LogprobBackArgs& a) {
-  const int64_t chunks = ceil_div(a.V, 4 * BT * vec_of<T>());
-  hipLaunchKernelGGL(logprob_back_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T * chunks, 1 << 20)), dim3(BT), 0, s,
-                     a, chunks);
+  const int64_t rows = std::min<int64_t>(a.T, 65535);
+  hipLaunchKernelGGL(logprob_back_kernel<T>,
+                     dim3((unsigned)ceil_div(a.V, 4 * BT * vec_of<T>()), (unsigned)rows, (unsigned)ceil_div(a.T, rows)),
+                     dim3(BT), 0, s, a);
   KMP_LAUNCH_CHECK();
   return 0;
 }
