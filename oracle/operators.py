@@ -44,7 +44,7 @@ def quantize_rows(x):
 
 
 def quantized_product(xq, xscale, wq, wscale, bias=None):
-    y = (np.asarray(xq, np.int64) @ np.asarray(wq, np.int64).T).astype(np.float64)
+    y = np.asarray(xq, np.float64) @ np.asarray(wq, np.float64).T        # whole numbers below 2^53: exact
     y = y * np.asarray(xscale, np.float64)[:, None] * np.asarray(wscale, np.float64)[None, :]
     return y if bias is None else y + np.asarray(bias, np.float64)
 

@@ -30,56 +30,147 @@ __device__ __forceinline__ O scaled(int acc, float xs, float ws, float bias) {
   return (O)((float)acc * xs * ws + bias);
 }
 
-// Tiles of 64 x 64, four wavefronts in a 2 x 2 arrangement, slices of 64 bytes
-// of k through LDS (rows 16 bytes apart from a power of two, against bank
-// conflicts). v_mfma_i32_16x16x64_i8: lane l holds 16 bytes of row l % 16 of
-// either operand from k = 16 (l / 16) on; register r of the result is D(row 4
-// (l / 16) + r, column l % 16).
-template <typename O>
-__global__ __launch_bounds__(256) void qproduct_tile_kernel(QProductArgs a) {
-  __shared__ int4v As[64][5], Bs[64][5];
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int64_t m0 = (int64_t)blockIdx.y * 64, n0 = (int64_t)blockIdx.x * 64;
-  const int row = t >> 2, c = t & 3;
-  const int8_t* pa = a.x + min(m0 + row, a.M - 1) * a.ldx;
-  const int8_t* pb = a.w + min(n0 + row, a.N - 1) * a.ldw;
-  const int wm = (w & 1) * 32, wn = (w >> 1) * 32;
-  int4v acc[2][2] = {};
-  for (int64_t k = 0; k < a.K; k += 64) {
-    const int4v va = chunk16(pa, k + 16 * c, a.K), vb = chunk16(pb, k + 16 * c, a.K);
-    __syncthreads();
-    As[row][c] = va;
-    Bs[row][c] = vb;
-    __syncthreads();
+typedef int int16v __attribute__((ext_vector_type(16)));
+
+// 16 bytes per lane from memory straight into LDS, at `lds` + 16 lane (lds the
+// same for the wavefront). The compiler does not count these loads: they are
+// waited for by wait_loads.
+__device__ __forceinline__ void load_to_lds(const int8_t* p, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Tiles of TM x TN, WR x WC wavefronts of 32 x 32 blocks of v_mfma_i32_32x32x32_i8
+// each (lane l holds 16 bytes of row l % 32 of either operand from k = 16 (l / 32)
+// on; register r of the result is D(row 8 (r / 4) + 4 (l / 32) + r % 4, column l %
+// 32)), slices of 128 bytes of k through two LDS stages: while one is multiplied
+// the next is on its way. A row of a slice is eight 16-byte chunks, chunk c kept
+// at place c ^ (row % 8), so that eight lanes with eight rows and one c read all
+// banks. Rows past the end repeat the last one and are not stored; a last slice
+// that is not whole is brought up with zeros. ALIGNED: rows start at multiples of
+// 16 bytes and go from memory to LDS without registers.
+template <typename O, int TM, int TN, int WR, int WC, bool ALIGNED>
+__global__ __launch_bounds__(64 * WR * WC, 2) void qproduct_tile_kernel(QProductArgs a, int tm, int tn) {
+  constexpr int NW = WR * WC, QA = TM / 8 / NW, QB = TN / 8 / NW;   // loads a wavefront, 8 rows each
+  constexpr int MB = TM / WR / 32, NB = TN / WC / 32;
+  constexpr int STAGE = (TM + TN) * 128;
+  __shared__ __align__(16) int8_t lds[2 * STAGE];
+  // workgroups go round the 8 chiplets: each takes a run of tiles of its own, in
+  // groups of four tile rows, for its cache
+  const int per = (tm * tn + 7) / 8, id = (int)blockIdx.x / 8 + ((int)blockIdx.x % 8) * per;
+  if ((int)blockIdx.x / 8 >= per || id >= tm * tn) return;
+  const int group = id / (4 * tn), rows = min(4, tm - 4 * group), in = id - group * 4 * tn;
+  const int64_t m0 = (int64_t)(4 * group + in % rows) * TM, n0 = (int64_t)(in / rows) * TN;
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int wr = w / WC, wc = w % WC;
+  const int lr = lane >> 3, lc = ((lane & 7) ^ lr) * 16;            // loads: row of 8, byte of the slice
+  const int8_t* pa[QA];
+  const int8_t* pb[QB];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+  for (int q = 0; q < QA; ++q) pa[q] = a.x + min(m0 + (w * QA + q) * 8 + lr, a.M - 1) * a.ldx + lc;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(As[wm + 16 * i + (lane & 15)][lane >> 4],
-                                                          Bs[wn + 16 * j + (lane & 15)][lane >> 4],
-                                                          acc[i][j], 0, 0, 0);
+  for (int q = 0; q < QB; ++q) pb[q] = a.w + min(n0 + (w * QB + q) * 8 + lr, a.N - 1) * a.ldw + lc;
+  const uint32_t base = (uint32_t)(uintptr_t)lds;                   // LDS addresses have 32 bits
+  const auto fetch = [&](int k, int st) {                           // ALIGNED: starts the loads of a whole slice
+#pragma unroll
+    for (int q = 0; q < QA; ++q) load_to_lds(pa[q] + k, base + st * STAGE + (w * QA + q) * 1024);
+#pragma unroll
+    for (int q = 0; q < QB; ++q) load_to_lds(pb[q] + k, base + st * STAGE + TM * 128 + (w * QB + q) * 1024);
+  };
+  int4v ra[QA], rb[QB];
+  const auto pull = [&](int k) {                                    // a slice into registers, zeros past K
+#pragma unroll
+    for (int q = 0; q < QA; ++q) ra[q] = chunk16(pa[q] - lc, k + lc, a.K);
+#pragma unroll
+    for (int q = 0; q < QB; ++q) rb[q] = chunk16(pb[q] - lc, k + lc, a.K);
+  };
+  const auto push = [&](int st) {
+#pragma unroll
+    for (int q = 0; q < QA; ++q) *reinterpret_cast<int4v*>(lds + st * STAGE + (w * QA + q) * 1024 + lane * 16) = ra[q];
+#pragma unroll
+    for (int q = 0; q < QB; ++q)
+      *reinterpret_cast<int4v*>(lds + st * STAGE + TM * 128 + (w * QB + q) * 1024 + lane * 16) = rb[q];
+  };
+  int16v acc[MB][NB] = {};
+  const int row = lane & 31, half = lane >> 5;
+  const int8_t* la = lds + (wr * MB * 32 + row) * 128;
+  const int8_t* lb = lds + TM * 128 + (wc * NB * 32 + row) * 128;
+  const auto multiply = [&](int st) {
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const int c = ((2 * ks + half) ^ (row & 7)) * 16 + st * STAGE;
+      int4v fa[MB], fb[NB];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) fa[i] = *reinterpret_cast<const int4v*>(la + i * 32 * 128 + c);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) fb[j] = *reinterpret_cast<const int4v*>(lb + j * 32 * 128 + c);
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
+    }
+  };
+  const int whole = (int)a.K / 128, tail = (int)a.K % 128;
+  if constexpr (ALIGNED) {
+    if (whole > 0) {
+      fetch(0, 0);
+      wait_loads();
+      __syncthreads();
+      for (int s = 0; s < whole; ++s) {
+        if (s + 1 < whole) fetch((s + 1) * 128, (s + 1) & 1);
+        multiply(s & 1);
+        wait_loads();
+        __syncthreads();
+      }
+    }
+    if (tail > 0) {
+      pull(whole * 128);
+      push(0);
+      __syncthreads();
+      multiply(0);
+    }
+  } else {
+    const int slices = whole + (tail > 0);
+    if (slices > 0) pull(0);
+    for (int s = 0; s < slices; ++s) {                              // (the stages alternate: one barrier each)
+      push(s & 1);
+      __syncthreads();
+      if (s + 1 < slices) pull((s + 1) * 128);
+      multiply(s & 1);
+    }
   }
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int64_t n = n0 + wn + 16 * j + (lane & 15);
+  for (int j = 0; j < NB; ++j) {
+    const int64_t n = n0 + wc * NB * 32 + j * 32 + row;
     if (n >= a.N) continue;
     const float ws = a.wscale[n], bias = a.bias ? a.bias[n] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t m = m0 + wm + 16 * i + 4 * (lane >> 4) + r;
+      for (int r = 0; r < 16; ++r) {
+        const int64_t m = m0 + wr * MB * 32 + i * 32 + 8 * (r / 4) + 4 * half + r % 4;
         if (m < a.M) static_cast<O*>(a.out)[m * a.ldo + n] = scaled<O>(acc[i][j][r], a.xscale[m], ws, bias);
       }
   }
 }
 
-template <typename O>
-int product_as(hipStream_t s, const QProductArgs& a) {
-  hipLaunchKernelGGL(qproduct_tile_kernel<O>, dim3((unsigned)ceil_div(a.N, 64), (unsigned)ceil_div(a.M, 64)),
-                     dim3(256), 0, s, a);
+template <typename O, int TM, int TN, int WR, int WC>
+int tiles_as(hipStream_t s, const QProductArgs& a) {
+  const int tm = (int)ceil_div(a.M, TM), tn = (int)ceil_div(a.N, TN);
+  const bool aligned = ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | a.ldx | a.ldw) & 15) == 0;
+  const dim3 grid((unsigned)round_up((int64_t)tm * tn, 8)), block(64 * WR * WC);
+  if (aligned)
+    hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, true>), grid, block, 0, s, a, tm, tn);
+  else
+    hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, false>), grid, block, 0, s, a, tm, tn);
   KMP_LAUNCH_CHECK();
   return 0;
+}
+
+template <typename O>
+int product_as(hipStream_t s, const QProductArgs& a) {
+  if (ceil_div(a.M, 256) * ceil_div(a.N, 256) >= 192) return tiles_as<O, 256, 256, 2, 4>(s, a);
+  return tiles_as<O, 128, 128, 2, 2>(s, a);
 }
 
 }  // namespace

@@ -267,7 +267,8 @@ def test_layer_norm_in_8_bits(xt):
 PRODUCTS = [(1, 1, 1), (1, 17, 5), (3, 16, 0), (1, 64, 64), (2, 33, 130), (1, 1000, 4096), (5, 129, 1000), (16, 48, 63),
             (17, 256, 65), (33, 100, 2051), (64, 513, 512), (65, 64, 127), (100, 300, 129), (128, 128, 128),
             (129, 257, 384), (255, 640, 130), (256, 256, 256), (257, 511, 259), (300, 2000, 1000), (520, 1030, 77),
-            (1000, 3, 640), (2049, 513, 192)]
+            (1000, 3, 640), (2049, 513, 192),
+            (3500, 3600, 384), (3600, 3500, 130)]      # the largest tiles
 
 
 def _bytes(rng, r, k):
