@@ -30,6 +30,89 @@ __device__ __forceinline__ O scaled(int acc, float xs, float ws, float bias) {
   return (O)((float)acc * xs * ws + bias);
 }
 
+// Few tokens: a workgroup takes 16 RB channels and 16 MT tokens, its NW wavefronts
+// each a run of the 64-byte slices of k, both operands from memory to registers,
+// SPD slices in flight; the wavefronts' sums are added in LDS (whole numbers: in
+// any order). Bound by reading w once. v_mfma_i32_16x16x64_i8: lane l holds 16 bytes of row l % 16 of either
+// operand from k = 16 (l / 16) on; register r of the result is D(row 4 (l / 16) +
+// r, column l % 16): w is the first operand, so a lane has four channels of one
+// token. Rows past the end repeat the last one and are not stored.
+template <typename O, int RB, int MT, int NW>
+__global__ __launch_bounds__(64 * NW) void qproduct_few_kernel(QProductArgs a) {
+  constexpr int SPD = RB + MT <= 2 ? 8 : RB + MT <= 4 ? 4 : 2;
+  __shared__ int sums[RB * MT][4][64];
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+  for (int i = t; i < RB * MT * 256; i += 64 * NW) (&sums[0][0][0])[i] = 0;
+  const int row = lane & 15, c = (lane >> 4) * 16;
+  const int64_t n0 = (int64_t)blockIdx.x * (16 * RB);
+  const int8_t* pw[RB];
+  const int8_t* px[MT];
+#pragma unroll
+  for (int i = 0; i < RB; ++i) pw[i] = a.w + min(n0 + 16 * i + row, a.N - 1) * a.ldw;
+#pragma unroll
+  for (int j = 0; j < MT; ++j) px[j] = a.x + min((int64_t)(16 * j + row), a.M - 1) * a.ldx;
+  // whole slices, dealt to the wavefronts in runs
+  const int whole = (int)a.K / 64, run = (whole + NW - 1) / NW;
+  const int s0 = min(w * run, whole), s1 = min(s0 + run, whole);
+  int4v acc[RB][MT] = {}, fw[SPD][RB], fx[SPD][MT];
+  const int n = s1 - s0;
+  const auto fetch = [&](int i, int4v (&vw)[RB], int4v (&vx)[MT]) {
+    const int k = 64 * (s0 + min(i, n - 1)) + c;  // past the end: the last slice again, unused
+#pragma unroll
+    for (int i = 0; i < RB; ++i) __builtin_memcpy(&vw[i], pw[i] + k, 16);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) __builtin_memcpy(&vx[j], px[j] + k, 16);
+  };
+  const auto products = [&](const int4v (&vw)[RB], const int4v (&vx)[MT]) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < MT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vw[i], vx[j], acc[i][j], 0, 0, 0);
+  };
+  if (n > 0) {
+#pragma unroll
+    for (int p = 0; p < SPD; ++p) fetch(p, fw[p], fx[p]);
+    int i = 0;
+    for (; i + SPD < n; i += SPD) {
+#pragma unroll
+      for (int p = 0; p < SPD; ++p) {
+        products(fw[p], fx[p]);
+        fetch(i + SPD + p, fw[p], fx[p]);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < SPD; ++p)
+      if (i + p < n) products(fw[p], fx[p]);
+  }
+  if (w == NW - 1 && a.K % 64 != 0) {             // the rest of k, zeros past its end
+#pragma unroll
+    for (int i = 0; i < RB; ++i) fw[0][i] = chunk16(pw[i], 64 * whole + c, a.K);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) fx[0][j] = chunk16(px[j], 64 * whole + c, a.K);
+    products(fw[0], fx[0]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) atomicAdd(&sums[i * MT + j][r][lane], acc[i][j][r]);
+  __syncthreads();
+  for (int b = w; b < RB * MT; b += NW) {
+    int v[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = sums[b][r][lane];
+    const int64_t m = 16 * (b % MT) + row, n = n0 + 16 * (b / MT) + (lane >> 4) * 4;
+    if (m >= a.M) continue;
+    const float xs = a.xscale[m];
+    O* out = static_cast<O*>(a.out) + m * a.ldo + n;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (n + r < a.N) out[r] = scaled<O>(v[r], xs, a.wscale[n + r], a.bias ? a.bias[n + r] : 0.0f);
+  }
+}
+
 typedef int int16v __attribute__((ext_vector_type(16)));
 
 // 16 bytes per lane from memory straight into LDS, at `lds` + 16 lane (lds the
@@ -38,7 +121,9 @@ typedef int int16v __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ void load_to_lds(const int8_t* p, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits until no more than LEFT of the wavefront's last loads are under way.
+template <int LEFT>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
 
 // Tiles of TM x TN, WR x WC wavefronts of 32 x 32 blocks of v_mfma_i32_32x32x32_i8
 // each (lane l holds 16 bytes of row l % 32 of either operand from k = 16 (l / 32)
@@ -49,33 +134,34 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)"
 // banks. Rows past the end repeat the last one and are not stored; a last slice
 // that is not whole is brought up with zeros. ALIGNED: rows start at multiples of
 // 16 bytes and go from memory to LDS without registers.
-template <typename O, int TM, int TN, int WR, int WC, bool ALIGNED>
-__global__ __launch_bounds__(64 * WR * WC, 2) void qproduct_tile_kernel(QProductArgs a, int tm, int tn) {
+template <typename O, int TM, int TN, int WR, int WC, int WK, int NS, bool ALIGNED>
+__global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProductArgs a, int tm, int tn) {
   constexpr int NW = WR * WC, QA = TM / 8 / NW, QB = TN / 8 / NW;   // loads a wavefront, 8 rows each
   constexpr int MB = TM / WR / 32, NB = TN / WC / 32;
   constexpr int STAGE = (TM + TN) * 128;
-  __shared__ __align__(16) int8_t lds[2 * STAGE];
+  __shared__ __align__(16) int8_t lds[WK * NS * STAGE];
   // workgroups go round the 8 chiplets: each takes a run of tiles of its own, in
   // groups of four tile rows, for its cache
   const int per = (tm * tn + 7) / 8, id = (int)blockIdx.x / 8 + ((int)blockIdx.x % 8) * per;
   if ((int)blockIdx.x / 8 >= per || id >= tm * tn) return;
   const int group = id / (4 * tn), rows = min(4, tm - 4 * group), in = id - group * 4 * tn;
   const int64_t m0 = (int64_t)(4 * group + in % rows) * TM, n0 = (int64_t)(in / rows) * TN;
-  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
-  const int wr = w / WC, wc = w % WC;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kg = w / NW, wg = w % NW, wr = wg / WC, wc = wg % WC;
   const int lr = lane >> 3, lc = ((lane & 7) ^ lr) * 16;            // loads: row of 8, byte of the slice
   const int8_t* pa[QA];
   const int8_t* pb[QB];
 #pragma unroll
-  for (int q = 0; q < QA; ++q) pa[q] = a.x + min(m0 + (w * QA + q) * 8 + lr, a.M - 1) * a.ldx + lc;
+  for (int q = 0; q < QA; ++q) pa[q] = a.x + min(m0 + (wg * QA + q) * 8 + lr, a.M - 1) * a.ldx + lc;
 #pragma unroll
-  for (int q = 0; q < QB; ++q) pb[q] = a.w + min(n0 + (w * QB + q) * 8 + lr, a.N - 1) * a.ldw + lc;
-  const uint32_t base = (uint32_t)(uintptr_t)lds;                   // LDS addresses have 32 bits
+  for (int q = 0; q < QB; ++q) pb[q] = a.w + min(n0 + (wg * QB + q) * 8 + lr, a.N - 1) * a.ldw + lc;
+  int8_t* ring = lds + kg * (NS * STAGE);
+  const uint32_t base = (uint32_t)(uintptr_t)ring;                  // LDS addresses have 32 bits
   const auto fetch = [&](int k, int st) {                           // ALIGNED: starts the loads of a whole slice
 #pragma unroll
-    for (int q = 0; q < QA; ++q) load_to_lds(pa[q] + k, base + st * STAGE + (w * QA + q) * 1024);
+    for (int q = 0; q < QA; ++q) load_to_lds(pa[q] + k, base + st * STAGE + (wg * QA + q) * 1024);
 #pragma unroll
-    for (int q = 0; q < QB; ++q) load_to_lds(pb[q] + k, base + st * STAGE + TM * 128 + (w * QB + q) * 1024);
+    for (int q = 0; q < QB; ++q) load_to_lds(pb[q] + k, base + st * STAGE + TM * 128 + (wg * QB + q) * 1024);
   };
   int4v ra[QA], rb[QB];
   const auto pull = [&](int k) {                                    // a slice into registers, zeros past K
@@ -86,15 +172,15 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void qproduct_tile_kernel(QProduct
   };
   const auto push = [&](int st) {
 #pragma unroll
-    for (int q = 0; q < QA; ++q) *reinterpret_cast<int4v*>(lds + st * STAGE + (w * QA + q) * 1024 + lane * 16) = ra[q];
+    for (int q = 0; q < QA; ++q) *reinterpret_cast<int4v*>(ring + st * STAGE + (wg * QA + q) * 1024 + lane * 16) = ra[q];
 #pragma unroll
     for (int q = 0; q < QB; ++q)
-      *reinterpret_cast<int4v*>(lds + st * STAGE + TM * 128 + (w * QB + q) * 1024 + lane * 16) = rb[q];
+      *reinterpret_cast<int4v*>(ring + st * STAGE + TM * 128 + (wg * QB + q) * 1024 + lane * 16) = rb[q];
   };
   int16v acc[MB][NB] = {};
   const int row = lane & 31, half = lane >> 5;
-  const int8_t* la = lds + (wr * MB * 32 + row) * 128;
-  const int8_t* lb = lds + TM * 128 + (wc * NB * 32 + row) * 128;
+  const int8_t* la = ring + (wr * MB * 32 + row) * 128;
+  const int8_t* lb = ring + TM * 128 + (wc * NB * 32 + row) * 128;
   const auto multiply = [&](int st) {
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
@@ -112,24 +198,32 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void qproduct_tile_kernel(QProduct
   };
   const int whole = (int)a.K / 128, tail = (int)a.K % 128;
   if constexpr (ALIGNED) {
-    if (whole > 0) {
-      fetch(0, 0);
-      wait_loads();
+    // slice s of a group goes to slot s % NS; it is read once the loads up to it
+    // have landed and every wavefront is there, which frees the slot of s - 1 for
+    // s + NS - 1
+    constexpr int LEFT = (NS - 2) * (QA + QB);
+    const int rounds = (whole + WK - 1) / WK, mine = (whole - kg + WK - 1) / WK;   // slices kg, kg + WK, ..
+    for (int s = 0; s < min(NS - 1, mine); ++s) fetch((s * WK + kg) * 128, s);
+    int slot = 0;
+    for (int s = 0; s < rounds; ++s) {
+      if (s + NS - 1 <= mine) wait_loads<LEFT>();
+      else wait_loads<0>();                                         // the last ones: all that is left
       __syncthreads();
-      for (int s = 0; s < whole; ++s) {
-        if (s + 1 < whole) fetch((s + 1) * 128, (s + 1) & 1);
-        multiply(s & 1);
-        wait_loads();
-        __syncthreads();
-      }
+      if (s + NS - 1 < mine) fetch(((s + NS - 1) * WK + kg) * 128, slot == 0 ? NS - 1 : slot - 1);
+      if (s < mine) multiply(slot);
+      slot = slot + 1 == NS ? 0 : slot + 1;
     }
     if (tail > 0) {
-      pull(whole * 128);
-      push(0);
       __syncthreads();
-      multiply(0);
+      if (kg == WK - 1) {
+        pull(whole * 128);
+        push(0);
+      }
+      __syncthreads();
+      if (kg == WK - 1) multiply(0);
     }
   } else {
+    static_assert(ALIGNED || WK == 1, "one group of wavefronts where rows are not aligned");
     const int slices = whole + (tail > 0);
     if (slices > 0) pull(0);
     for (int s = 0; s < slices; ++s) {                              // (the stages alternate: one barrier each)
@@ -138,6 +232,32 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void qproduct_tile_kernel(QProduct
       if (s + 1 < slices) pull((s + 1) * 128);
       multiply(s & 1);
     }
+  }
+  if constexpr (WK > 1) {                                           // the first group adds the others' sums
+    static_assert((WK - 1) * TM * TN * 4 <= WK * NS * STAGE, "the sums fit the ring");
+    int* sums = reinterpret_cast<int*>(lds);
+    __syncthreads();
+    const auto at = [&](int g, int i, int j, int r) {
+      return sums + (((g - 1) * NW + wg) * MB * NB + i * NB + j) * 1024 + r * 64 + lane;
+    };
+    if (kg > 0) {
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) *at(kg, i, j, r) = acc[i][j][r];
+    }
+    __syncthreads();
+    if (kg > 0) return;
+#pragma unroll
+    for (int g = 1; g < WK; ++g)
+#pragma unroll
+      for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] += *at(g, i, j, r);
   }
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
@@ -154,23 +274,48 @@ __global__ __launch_bounds__(64 * WR * WC, 2) void qproduct_tile_kernel(QProduct
   }
 }
 
-template <typename O, int TM, int TN, int WR, int WC>
+template <typename O, int TM, int TN, int WR, int WC, int WK, int NS>
 int tiles_as(hipStream_t s, const QProductArgs& a) {
   const int tm = (int)ceil_div(a.M, TM), tn = (int)ceil_div(a.N, TN);
   const bool aligned = ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | a.ldx | a.ldw) & 15) == 0;
   const dim3 grid((unsigned)round_up((int64_t)tm * tn, 8)), block(64 * WR * WC);
   if (aligned)
-    hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, true>), grid, block, 0, s, a, tm, tn);
+    hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, WK, NS, true>), grid, dim3(64 * WR * WC * WK), 0, s, a, tm, tn);
   else
-    hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, false>), grid, block, 0, s, a, tm, tn);
+    hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, 1, 2, false>), grid, block, 0, s, a, tm, tn);
   KMP_LAUNCH_CHECK();
   return 0;
 }
 
+// Which form, by what keeps the chip's 256 compute units busy; us per launch at M x
+// N x K, w from HBM (few = qproduct_few_kernel, else rows x columns of a tile, WK):
+//                    few  32x64,4  64x64,2+  64x64,2  64x64,1  128,1  256,1  floor
+//   1 x 4096 x 4096    6.1    7.9     10.5     12.1     17.4     22     50     3.5
+//   16 x 12288 x 4096 16.4   13.5     13.8     19.1     27       34     53    10.5
+//   16 x 32000 x 2048 21.5   18.8     18.8     15.6     18.3     21            13.8
+//   64 x 4096 x 4096  12.8    9.7     12.1     14.2     18       28     56     3.6
+//   128 x 4096 x 4096 21     10.2     12.3     14.2     18.6     29     62     3.8
+//   256 x 4096 x 4096 38     17.5     12.9     14.6     18.9     29     66     4.2
+//   64 x 12288 x 4096 33     23       17.6     20.8     28       38     58    10.8
+//   512 x 4096 x 4096 74     33       23       18.7     20.2     30     66     8.4
+//   2048 x 2048 x 2048 77    46       31       22.3     18.5     22     46     8.4
+//   4096 x 16384 x 4096                                525      437    366   269
+// (64x64,2+ has a ring of three slices, 64x64,2 of two and so two workgroups a
+// compute unit). The floor is the bytes at a copy's 4.82 TB/s or the products at
+// the 2040 TOP/s of the library's 8-bit product of order 8192.
 template <typename O>
 int product_as(hipStream_t s, const QProductArgs& a) {
-  if (ceil_div(a.M, 256) * ceil_div(a.N, 256) >= 192) return tiles_as<O, 256, 256, 2, 4>(s, a);
-  return tiles_as<O, 128, 128, 2, 2>(s, a);
+  const auto tiles = [&](int tm, int tn) { return ceil_div(a.M, tm) * ceil_div(a.N, tn); };
+  if (a.M <= 16 && a.N <= 8192) {
+    hipLaunchKernelGGL((qproduct_few_kernel<O, 1, 1, 4>), dim3((unsigned)ceil_div(a.N, 16)), dim3(256), 0, s, a);
+    KMP_LAUNCH_CHECK();
+    return 0;
+  }
+  if (tiles(32, 64) <= 256) return tiles_as<O, 32, 64, 1, 2, 4, 3>(s, a);
+  if (tiles(64, 64) <= 256) return tiles_as<O, 64, 64, 2, 2, 2, 3>(s, a);
+  if (tiles(64, 64) <= 512) return tiles_as<O, 64, 64, 2, 2, 2, 2>(s, a);
+  if (tiles(256, 256) < 192) return tiles_as<O, 64, 64, 2, 2, 1, 2>(s, a);
+  return tiles_as<O, 256, 256, 2, 4, 1, 2>(s, a);
 }
 
 }  // namespace
