@@ -210,6 +210,9 @@ def kmp_workspace_bytes(spec, n, d, L, fold_id, V, S, Q, sigma_batch) -> int:
 def _stream_ptr(stream) -> int:
     import torch
     if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None and torch.cuda.is_initialized():
+            return raw(torch._C._cuda_getDevice())     # 0.2 us against 2.9
         stream = torch.cuda.current_stream()
     return int(stream.cuda_stream)
 
