@@ -3,6 +3,8 @@
 // x M x K and w N x K row-major. The sums are exact in 32-bit integers up to
 // K = 131071, so their order does not matter; they are converted to 32-bit
 // floats, scaled, and rounded once to the output's type.
+#include <type_traits>
+
 #include "kmp_operators.h"
 
 namespace kmp {
@@ -125,12 +127,95 @@ __device__ __forceinline__ void load_to_lds(const int8_t* p, uint32_t lds) {
 template <int LEFT>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
 
+// Barrier of the workgroup that leaves the wavefront's own reads and loads under
+// way (what has to have ended is waited for before it, or by its use).
+__device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
+
+// First row and column of a workgroup's tile; false where it has none. Workgroups
+// go round the 8 chiplets: each takes a run of tiles of its own, in groups of four
+// tile rows, for its cache.
+__device__ __forceinline__ bool tile_of(int tm, int tn, int TM, int TN, int64_t& m0, int64_t& n0) {
+  const int per = (tm * tn + 7) / 8, id = (int)blockIdx.x / 8 + ((int)blockIdx.x % 8) * per;
+  if ((int)blockIdx.x / 8 >= per || id >= tm * tn) return false;
+  const int group = id / (4 * tn), rows = min(4, tm - 4 * group), in = id - group * 4 * tn;
+  m0 = (int64_t)(4 * group + in % rows) * TM;
+  n0 = (int64_t)(in / rows) * TN;
+  return true;
+}
+
+// Scales and writes a wavefront's MB x NB blocks of 32 x 32 from row m1, column n1
+// on; the blocks are transposed (w was the first operand), so a lane has four
+// neighbouring columns of one row. They go through LDS (`region`, the wavefront's
+// own) into whole rows of 16-byte stores; stored straight from the registers, two
+// bytes a lane, a tile of 256 x 256 took 10 us for its 128 KB, as long as 500 of k.
+template <typename O, int MB, int NB>
+constexpr int region_bytes() { return 32 * (NB * 32 * (int)sizeof(O) + 16); }
+template <typename O, int MB, int NB>
+__device__ __forceinline__ void store_tile(const QProductArgs& a, const int16v (&acc)[MB][NB], int64_t m1, int64_t n1,
+                                           int lane, int8_t* region) {
+  constexpr int S = (int)sizeof(O), STRIDE = NB * 32 * S + 16, PER = 16 / S, CH = NB * 32 / PER, RPI = 64 / CH;
+  const int row = lane & 31, half = lane >> 5;
+  float ws[NB][4][4], bias[NB][4][4];
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int64_t n = n1 + j * 32 + 8 * g + 4 * half;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bias[j][g][e] = 0.0f;
+      if (n + 4 <= a.N) {
+        load_n(a.wscale + n, ws[j][g]);
+        if (a.bias) load_n(a.bias + n, bias[j][g]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ws[j][g][e] = n + e < a.N ? a.wscale[n + e] : 0.0f;
+          if (a.bias && n + e < a.N) bias[j][g][e] = a.bias[n + e];
+        }
+      }
+    }
+  float xs[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) xs[i] = a.xscale[min(m1 + i * 32 + row, a.M - 1)];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        O v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = scaled<O>(acc[i][j][4 * g + e], xs[i], ws[j][g][e], bias[j][g][e]);
+        __builtin_memcpy(__builtin_assume_aligned(region + row * STRIDE + (j * 32 + 8 * g + 4 * half) * S, 4 * S), v, 4 * S);
+      }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int q = 0; q < 32 / RPI; ++q) {
+      const int r = q * RPI + lane / CH, c = lane % CH * PER;
+      const int64_t m = m1 + i * 32 + r, n = n1 + c;
+      O v[PER];
+      __builtin_memcpy(v, __builtin_assume_aligned(region + r * STRIDE + c * S, 16), 16);
+      O* out = static_cast<O*>(a.out) + m * a.ldo + n;
+      if (m < a.M && n + PER <= a.N) {
+        __builtin_memcpy(out, v, 16);
+      } else if (m < a.M) {
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+          if (n + e < a.N) out[e] = v[e];
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // Tiles of TM x TN, WR x WC wavefronts of 32 x 32 blocks of v_mfma_i32_32x32x32_i8
 // each (lane l holds 16 bytes of row l % 32 of either operand from k = 16 (l / 32)
 // on; register r of the result is D(row 8 (r / 4) + 4 (l / 32) + r % 4, column l %
-// 32)), slices of 128 bytes of k through two LDS stages: while one is multiplied
+// 32); w is the first operand), slices of 128 bytes of k through two LDS stages: while one is multiplied
 // the next is on its way. A row of a slice is eight 16-byte chunks, chunk c kept
-// at place c ^ (row % 8), so that eight lanes with eight rows and one c read all
+// at place c ^ (row / 2 % 8), so that 16 lanes with 16 rows and one c read all 64
 // banks. Rows past the end repeat the last one and are not stored; a last slice
 // that is not whole is brought up with zeros. ALIGNED: rows start at multiples of
 // 16 bytes and go from memory to LDS without registers.
@@ -140,35 +225,34 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
   constexpr int MB = TM / WR / 32, NB = TN / WC / 32;
   constexpr int STAGE = (TM + TN) * 128;
   __shared__ __align__(16) int8_t lds[WK * NS * STAGE];
-  // workgroups go round the 8 chiplets: each takes a run of tiles of its own, in
-  // groups of four tile rows, for its cache
-  const int per = (tm * tn + 7) / 8, id = (int)blockIdx.x / 8 + ((int)blockIdx.x % 8) * per;
-  if ((int)blockIdx.x / 8 >= per || id >= tm * tn) return;
-  const int group = id / (4 * tn), rows = min(4, tm - 4 * group), in = id - group * 4 * tn;
-  const int64_t m0 = (int64_t)(4 * group + in % rows) * TM, n0 = (int64_t)(in / rows) * TN;
+  int64_t m0, n0;
+  if (!tile_of(tm, tn, TM, TN, m0, n0)) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kg = w / NW, wg = w % NW, wr = wg / WC, wc = wg % WC;
-  const int lr = lane >> 3, lc = ((lane & 7) ^ lr) * 16;            // loads: row of 8, byte of the slice
+  // loads: row lr of eight, the byte of the slice by the row's place in sixteen
+  static_assert(QA % 2 == 0 && QB % 2 == 0, "pairs of eight rows");
+  const int lr = lane >> 3;
+  const int lc[2] = {((lane & 7) ^ (lr >> 1)) * 16, ((lane & 7) ^ (4 + (lr >> 1))) * 16};
   const int8_t* pa[QA];
   const int8_t* pb[QB];
 #pragma unroll
-  for (int q = 0; q < QA; ++q) pa[q] = a.x + min(m0 + (wg * QA + q) * 8 + lr, a.M - 1) * a.ldx + lc;
+  for (int q = 0; q < QA; ++q) pa[q] = a.x + min(m0 + (wg * QA + q) * 8 + lr, a.M - 1) * a.ldx;
 #pragma unroll
-  for (int q = 0; q < QB; ++q) pb[q] = a.w + min(n0 + (wg * QB + q) * 8 + lr, a.N - 1) * a.ldw + lc;
+  for (int q = 0; q < QB; ++q) pb[q] = a.w + min(n0 + (wg * QB + q) * 8 + lr, a.N - 1) * a.ldw;
   int8_t* ring = lds + kg * (NS * STAGE);
   const uint32_t base = (uint32_t)(uintptr_t)ring;                  // LDS addresses have 32 bits
   const auto fetch = [&](int k, int st) {                           // ALIGNED: starts the loads of a whole slice
 #pragma unroll
-    for (int q = 0; q < QA; ++q) load_to_lds(pa[q] + k, base + st * STAGE + (wg * QA + q) * 1024);
+    for (int q = 0; q < QA; ++q) load_to_lds(pa[q] + k + lc[q & 1], base + st * STAGE + (wg * QA + q) * 1024);
 #pragma unroll
-    for (int q = 0; q < QB; ++q) load_to_lds(pb[q] + k, base + st * STAGE + TM * 128 + (wg * QB + q) * 1024);
+    for (int q = 0; q < QB; ++q) load_to_lds(pb[q] + k + lc[q & 1], base + st * STAGE + TM * 128 + (wg * QB + q) * 1024);
   };
   int4v ra[QA], rb[QB];
   const auto pull = [&](int k) {                                    // a slice into registers, zeros past K
 #pragma unroll
-    for (int q = 0; q < QA; ++q) ra[q] = chunk16(pa[q] - lc, k + lc, a.K);
+    for (int q = 0; q < QA; ++q) ra[q] = chunk16(pa[q], k + lc[q & 1], a.K);
 #pragma unroll
-    for (int q = 0; q < QB; ++q) rb[q] = chunk16(pb[q] - lc, k + lc, a.K);
+    for (int q = 0; q < QB; ++q) rb[q] = chunk16(pb[q], k + lc[q & 1], a.K);
   };
   const auto push = [&](int st) {
 #pragma unroll
@@ -184,7 +268,7 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
   const auto multiply = [&](int st) {
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) {
-      const int c = ((2 * ks + half) ^ (row & 7)) * 16 + st * STAGE;
+      const int c = ((2 * ks + half) ^ (row >> 1 & 7)) * 16 + st * STAGE;
       int4v fa[MB], fb[NB];
 #pragma unroll
       for (int i = 0; i < MB; ++i) fa[i] = *reinterpret_cast<const int4v*>(la + i * 32 * 128 + c);
@@ -193,7 +277,7 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
 #pragma unroll
       for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[i], fb[j], acc[i][j], 0, 0, 0);
+        for (int j = 0; j < NB; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[j], fa[i], acc[i][j], 0, 0, 0);
     }
   };
   const int whole = (int)a.K / 128, tail = (int)a.K % 128;
@@ -233,10 +317,9 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
       multiply(s & 1);
     }
   }
+  __syncthreads();                                                  // the ring is free
   if constexpr (WK > 1) {                                           // the first group adds the others' sums
-    static_assert((WK - 1) * TM * TN * 4 <= WK * NS * STAGE, "the sums fit the ring");
     int* sums = reinterpret_cast<int*>(lds);
-    __syncthreads();
     const auto at = [&](int g, int i, int j, int r) {
       return sums + (((g - 1) * NW + wg) * MB * NB + i * NB + j) * 1024 + r * 64 + lane;
     };
@@ -259,27 +342,109 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[i][j][r] += *at(g, i, j, r);
   }
+  constexpr int REGION = region_bytes<O, MB, NB>(), SUMS = (WK - 1) * TM * TN * 4;   // regions lie behind the sums
+  static_assert(SUMS + NW * REGION <= WK * NS * STAGE, "sums and regions fit the ring");
+  store_tile<O, MB, NB>(a, acc, m0 + wr * MB * 32, n0 + wc * NB * 32, lane, lds + SUMS + wg * REGION);
+}
+
+// The large form: tiles of 256 x 256, eight wavefronts of 128 x 64, aligned rows.
+// Slices of 64 bytes (a row of one is four chunks, chunk c at place c ^ (row / 4 %
+// 4): 16 rows with one c are in 16 different places of all banks) through a ring of
+// four stages, read one half slice ahead: when a wavefront passes the barrier of
+// slice s, slice s + 1 has landed, so the operands of its first half are on their
+// way to registers while the second half of s is multiplied, and no product waits
+// for LDS or for the barrier. Slice s + 3 goes where s - 1 was.
+template <typename O>
+__global__ __launch_bounds__(512) void qproduct_big_kernel(QProductArgs a, int tm, int tn) {
+  constexpr int TM = 256, TN = 256, WC = 4, MB = 4, NB = 2, Q = 2, SL = 64, STAGE = (TM + TN) * SL;
+  __shared__ __align__(16) int8_t lds[4 * STAGE];
+  int64_t m0, n0;
+  if (!tile_of(tm, tn, TM, TN, m0, n0)) return;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = w / WC, wc = w % WC;
+  const int lr = lane >> 2, lc = ((lane & 3) ^ (lr >> 2 & 3)) * 16;   // loads: row of 16, byte of the slice
+  const int8_t* pa[Q];
+  const int8_t* pb[Q];
 #pragma unroll
-  for (int j = 0; j < NB; ++j) {
-    const int64_t n = n0 + wc * NB * 32 + j * 32 + row;
-    if (n >= a.N) continue;
-    const float ws = a.wscale[n], bias = a.bias ? a.bias[n] : 0.0f;
+  for (int q = 0; q < Q; ++q) {
+    pa[q] = a.x + min(m0 + (w * Q + q) * 16 + lr, a.M - 1) * a.ldx;
+    pb[q] = a.w + min(n0 + (w * Q + q) * 16 + lr, a.N - 1) * a.ldw;
+  }
+  const uint32_t base = (uint32_t)(uintptr_t)lds;                     // LDS addresses have 32 bits
+  const auto fetch = [&](int s) {
+    const uint32_t at = base + (s & 3) * STAGE + w * Q * 1024;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      load_to_lds(pa[q] + s * SL + lc, at + q * 1024);
+      load_to_lds(pb[q] + s * SL + lc, at + TM * SL + q * 1024);
+    }
+  };
+  int16v acc[MB][NB] = {};
+  const int row = lane & 31, half = lane >> 5;
+  const int8_t* la = lds + (wr * MB * 32 + row) * SL;
+  const int8_t* lb = lds + TM * SL + (wc * NB * 32 + row) * SL;
+  int4v fa[2][MB], fb[2][NB];
+  const auto read = [&](int s, int h) {                               // half h of slice s
+    const int c = ((2 * h + half) ^ (row >> 2 & 3)) * 16 + (s & 3) * STAGE;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) fa[h][i] = *reinterpret_cast<const int4v*>(la + i * 32 * SL + c);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) fb[h][j] = *reinterpret_cast<const int4v*>(lb + j * 32 * SL + c);
+  };
+  const auto multiply = [&](int h) {
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t m = m0 + wr * MB * 32 + i * 32 + 8 * (r / 4) + 4 * half + r % 4;
-        if (m < a.M) static_cast<O*>(a.out)[m * a.ldo + n] = scaled<O>(acc[i][j][r], a.xscale[m], ws, bias);
-      }
+      for (int j = 0; j < NB; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[h][j], fa[h][i], acc[i][j], 0, 0, 0);
+  };
+  const int whole = (int)a.K / SL, tail = (int)a.K % SL;
+  if (whole > 0) {
+    for (int s = 0; s < min(3, whole); ++s) fetch(s);
+    wait_loads<0>();
+    barrier();
+    read(0, 0);
+    for (int s = 0; s < whole; ++s) {
+      if (s + 2 < whole) wait_loads<2 * Q>();                         // s + 1 has landed, s + 2 may not have
+      else wait_loads<0>();
+      barrier();
+      if (s + 3 < whole) fetch(s + 3);
+      read(s, 1);
+      __builtin_amdgcn_sched_barrier(0);                              // (else the reads sink to their uses)
+      multiply(0);
+      __builtin_amdgcn_sched_barrier(0);
+      read(s + 1, 0);                                                 // (after the last slice: not used)
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(1);
+    }
   }
+  if (tail > 0) {                                                     // zeros past K
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      int8_t* at = lds + (w * Q + q) * 1024 + lane * 16;
+      *reinterpret_cast<int4v*>(at) = chunk16(pa[q], whole * SL + lc, a.K);
+      *reinterpret_cast<int4v*>(at + TM * SL) = chunk16(pb[q], whole * SL + lc, a.K);
+    }
+    __syncthreads();
+    read(0, 0);
+    read(0, 1);
+    multiply(0);
+    multiply(1);
+  }
+  __syncthreads();                                                    // the ring is free
+  store_tile<O, MB, NB>(a, acc, m0 + wr * MB * 32, n0 + wc * NB * 32, lane, lds + w * region_bytes<O, MB, NB>());
+}
+
+bool aligned_rows(const QProductArgs& a) {
+  return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | a.ldx | a.ldw) & 15) == 0;
 }
 
 template <typename O, int TM, int TN, int WR, int WC, int WK, int NS>
 int tiles_as(hipStream_t s, const QProductArgs& a) {
   const int tm = (int)ceil_div(a.M, TM), tn = (int)ceil_div(a.N, TN);
-  const bool aligned = ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | a.ldx | a.ldw) & 15) == 0;
   const dim3 grid((unsigned)round_up((int64_t)tm * tn, 8)), block(64 * WR * WC);
-  if (aligned)
+  if (aligned_rows(a))
     hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, WK, NS, true>), grid, dim3(64 * WR * WC * WK), 0, s, a, tm, tn);
   else
     hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, 1, 2, false>), grid, block, 0, s, a, tm, tn);
@@ -315,7 +480,11 @@ int product_as(hipStream_t s, const QProductArgs& a) {
   if (tiles(64, 64) <= 256) return tiles_as<O, 64, 64, 2, 2, 2, 3>(s, a);
   if (tiles(64, 64) <= 512) return tiles_as<O, 64, 64, 2, 2, 2, 2>(s, a);
   if (tiles(256, 256) < 192) return tiles_as<O, 64, 64, 2, 2, 1, 2>(s, a);
-  return tiles_as<O, 256, 256, 2, 4, 1, 2>(s, a);
+  if (!aligned_rows(a)) return tiles_as<O, 128, 128, 2, 2, 1, 2>(s, a);
+  const int tm = (int)ceil_div(a.M, 256), tn = (int)ceil_div(a.N, 256);
+  hipLaunchKernelGGL(qproduct_big_kernel<O>, dim3((unsigned)round_up((int64_t)tm * tn, 8)), dim3(512), 0, s, a, tm, tn);
+  KMP_LAUNCH_CHECK();
+  return 0;
 }
 
 }  // namespace
