@@ -65,7 +65,8 @@ struct ByteScale {
   }
 };
 
-// One workgroup per row, any length (rows too long for the registers): a pass for the mean, one for the
+// One workgroup per row, any length (rows too long for the registers, or shorter
+// than a vector): a pass for the mean, one for the
 // variance, one for the largest |y| of the 8-bit form, one to write.
 template <typename T, typename W, int MODE>
 __global__ __launch_bounds__(BT) void norm_row_kernel(NormArgs a) {
@@ -138,6 +139,28 @@ __device__ __forceinline__ A row_total(A v, A (*red)[threads_of(TPR) / 64], int&
   }
   return v;
 }
+// Two sums at once.
+template <typename A, int TPR>
+__device__ __forceinline__ void row_totals(A& u, A& v, A (*red)[2 * (threads_of(TPR) / 64)], int& slot) {
+#pragma unroll
+  for (int off = (TPR < 64 ? TPR : 64) / 2; off >= 1; off >>= 1) {
+    u += __shfl_xor(u, off, kWave);
+    v += __shfl_xor(v, off, kWave);
+  }
+  if constexpr (TPR > 64) {
+    A* r = red[slot];
+    slot ^= 1;
+    if ((threadIdx.x & 63) == 0) {
+      r[2 * (threadIdx.x >> 6)] = u;
+      r[2 * (threadIdx.x >> 6) + 1] = v;
+    }
+    __syncthreads();
+    u = r[0];
+    v = r[1];
+#pragma unroll
+    for (int i = 1; i < TPR / 64; ++i) u += r[2 * i], v += r[2 * i + 1];
+  }
+}
 template <int TPR>
 __device__ __forceinline__ float row_most(float v, float (*red)[threads_of(TPR) / 64], int& slot) {
 #pragma unroll
@@ -154,24 +177,31 @@ __device__ __forceinline__ float row_most(float v, float (*red)[threads_of(TPR) 
   return v;
 }
 
-// Elements j .. j + N - 1 of a row of d, `fill` past its end.
-template <typename T, int N, typename A>
-__device__ __forceinline__ void load_part(const T* p, int j, int d, A fill, A (&v)[N]) {
-  if (j + N <= d) {
-    load_n(p + j, v);
-  } else {
+// A thread's vector of N elements of a row of d >= N that would start at j: it is
+// moved back to end with the row, so that every load is one access and no branch
+// stands between the loads (a branch for the row's end made each wait for the one
+// before). Its first `skip` elements are another vector's, all of them where j
+// lies past the end: cleared, and not stored.
+template <int N>
+struct Place {
+  int at, skip;
+  __device__ Place(int j, int d) : at(min(j, d - N)), skip(j - at) {}
+};
+template <int N, typename A>
+__device__ __forceinline__ void clear(const Place<N>& q, A (&v)[N]) {
+  if (q.skip > 0) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = j + e < d ? (A)p[j + e] : fill;
+    for (int e = 0; e < N; ++e) v[e] = e < q.skip ? (A)0 : v[e];
   }
 }
 template <typename T, int N, typename A>
-__device__ __forceinline__ void store_part(T* p, int j, int d, const A (&v)[N]) {
-  if (j + N <= d) {
-    store_n(p + j, v);
+__device__ __forceinline__ void store_at(T* p, const Place<N>& q, const A (&v)[N]) {
+  if (q.skip == 0) {
+    store_n(p + q.at, v);
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (j + e < d) p[j + e] = (T)v[e];
+      if (e >= q.skip) p[q.at + e] = (T)v[e];
   }
 }
 
@@ -187,11 +217,13 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_reg_kernel(NormArgs a) {
   if constexpr (MODE != kBytesOfX) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int j = (t + i * TPR) * VEC;
+      const Place<VEC> q((t + i * TPR) * VEC, d);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) g[i][e] = 1, b[i][e] = 0;
-      if (a.gamma) load_part(static_cast<const W*>(a.gamma), j, d, (A)0, g[i]);
-      if (a.beta) load_part(static_cast<const W*>(a.beta), j, d, (A)0, b[i]);
+      if (a.gamma) load_n(static_cast<const W*>(a.gamma) + q.at, g[i]);
+      if (a.beta) load_n(static_cast<const W*>(a.beta) + q.at, b[i]);
+      clear(q, g[i]);
+      clear(q, b[i]);
     }
   }
   // a workgroup's rows: every thread takes part in every round (the barriers)
@@ -201,7 +233,9 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_reg_kernel(NormArgs a) {
     const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     A v[NV][VEC];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load_part(x, (t + i * TPR) * VEC, d, (A)0, v[i]);
+    for (int i = 0; i < NV; ++i) load_n(x + Place<VEC>((t + i * TPR) * VEC, d).at, v[i]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) clear(Place<VEC>((t + i * TPR) * VEC, d), v[i]);
     if constexpr (MODE != kBytesOfX) {
       A s = 0;
 #pragma unroll
@@ -212,13 +246,9 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_reg_kernel(NormArgs a) {
       A q = 0;
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
-        const int j = (t + i * TPR) * VEC;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) v[i][e] -= mu;
-        if (j + VEC > d) {                        // past the end: no deviation
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) v[i][e] = j + e < d ? v[i][e] : (A)0;
-        }
+        clear(Place<VEC>((t + i * TPR) * VEC, d), v[i]);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) q += v[i][e] * v[i][e];
       }
@@ -236,7 +266,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_reg_kernel(NormArgs a) {
       T* y = static_cast<T*>(a.y) + r * a.ldy;
       if (live) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) store_part(y, (t + i * TPR) * VEC, d, v[i]);
+        for (int i = 0; i < NV; ++i) store_at(y, Place<VEC>((t + i * TPR) * VEC, d), v[i]);
       }
     } else {
       float m = 0.0f;
@@ -252,7 +282,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_reg_kernel(NormArgs a) {
           int8_t q[VEC];
 #pragma unroll
           for (int e = 0; e < VEC; ++e) q[e] = bs((float)v[i][e]);
-          store_part(y, (t + i * TPR) * VEC, d, q);
+          store_at(y, Place<VEC>((t + i * TPR) * VEC, d), q);
         }
         if (t == 0) a.scale[r] = bs.scale;
       }
@@ -295,7 +325,7 @@ template <typename T, typename W, int TPR, int NV>
 __global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBackArgs a) {
   typedef typename acc_of<T>::type A;
   constexpr int VEC = vec_of<T>(), RPB = threads_of(TPR) / TPR;
-  __shared__ A red[2][threads_of(TPR) / 64];
+  __shared__ A red[2][2 * (threads_of(TPR) / 64)];
   __shared__ A sums[RPB > 1 ? TPR * NV * VEC : 1];
   int slot = 0;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
@@ -306,23 +336,22 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBack
     for (int e = 0; e < VEC; ++e) g[i][e] = 1, dg[i][e] = 0, db[i][e] = 0;
   if (a.gamma) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) load_part(static_cast<const W*>(a.gamma), (t + i * TPR) * VEC, d, (A)0, g[i]);
+    for (int i = 0; i < NV; ++i)
+      load_n(static_cast<const W*>(a.gamma) + Place<VEC>((t + i * TPR) * VEC, d).at, g[i]);
   }
   const int64_t step = (int64_t)gridDim.x * RPB;
-  const auto fetch = [&](int64_t r, T (&rx)[NV][VEC], T (&rd)[NV][VEC]) {
+  T nx[NV][VEC], nd[NV][VEC];                     // the next row, as it comes
+  A nmu, nrs;
+  const auto next = [&](int64_t r) {
+    r = min(r, a.rows - 1);
     const T* px = static_cast<const T*>(a.x) + r * a.ldx;
     const T* pd = static_cast<const T*>(a.dy) + r * a.lddy;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      load_part(px, (t + i * TPR) * VEC, d, (T)0.0f, rx[i]);
-      load_part(pd, (t + i * TPR) * VEC, d, (T)0.0f, rd[i]);
+      const int at = Place<VEC>((t + i * TPR) * VEC, d).at;
+      __builtin_memcpy(nx[i], px + at, sizeof(nx[i]));
+      __builtin_memcpy(nd[i], pd + at, sizeof(nd[i]));
     }
-  };
-  T nx[NV][VEC], nd[NV][VEC];
-  A nmu, nrs;
-  const auto next = [&](int64_t r) {
-    r = min(r, a.rows - 1);
-    fetch(r, nx, nd);
     nmu = static_cast<const A*>(a.mean)[r];
     nrs = static_cast<const A*>(a.rstd)[r];
   };
@@ -331,30 +360,34 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBack
   for (; r0 < a.rows; r0 += step) {
     const int64_t r = r0 + sub;
     const bool live = r < a.rows;
-    const A mu = nmu, rs = nrs;
+    const A mu = nmu, rs = live ? nrs : (A)0;
     A s1 = 0, s2 = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[i][e] = ((A)nx[i][e] - mu) * rs, w[i][e] = (A)nd[i][e];
+      for (int e = 0; e < VEC; ++e) {
+        x[i][e] = ((A)nx[i][e] - mu) * rs;
+        w[i][e] = live ? (A)nd[i][e] : (A)0;      // (a last round's missing rows add nothing)
+      }
+      clear(Place<VEC>((t + i * TPR) * VEC, d), w[i]);
     }
-    if (r0 + step < a.rows) next(r + step);
+    next(r + step);                               // past the end: the last row again, unused
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        if (live) {                               // past the end: w = 0
-          dg[i][e] += w[i][e] * x[i][e];
-          db[i][e] += w[i][e];
-        }
+        dg[i][e] += w[i][e] * x[i][e];
+        db[i][e] += w[i][e];
         w[i][e] *= g[i][e];
         s1 += w[i][e];
         s2 += w[i][e] * x[i][e];
       }
     }
     if (a.dx) {
-      s1 = row_total<A, TPR>(s1, red, slot) / (A)d;
-      s2 = row_total<A, TPR>(s2, red, slot) / (A)d;
+      row_totals<A, TPR>(s1, s2, red, slot);
+      s1 /= (A)d;
+      s2 /= (A)d;
 #pragma unroll
       for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -362,7 +395,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBack
       if (live) {
         T* dx = static_cast<T*>(a.dx) + r * a.lddx;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) store_part(dx, (t + i * TPR) * VEC, d, w[i]);
+        for (int i = 0; i < NV; ++i) store_at(dx, Place<VEC>((t + i * TPR) * VEC, d), w[i]);
       }
     }
   }
@@ -392,7 +425,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBack
     }
     if (sub == 0) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) store_part(out, (t + i * TPR) * VEC, d, v[i]);
+      for (int i = 0; i < NV; ++i) store_at(out, Place<VEC>((t + i * TPR) * VEC, d), v[i]);
     }
   };
   write(dg, p);
@@ -445,7 +478,8 @@ __global__ __launch_bounds__(1024) void norm_back_join_kernel(const A* partial, 
 
 template <typename T, typename W, int MODE>
 int forward_mode(hipStream_t s, const NormArgs& a) {
-  const int64_t nv = ceil_div(a.d, vec_of<T>());
+  // (rows shorter than a vector go with those too long for the registers)
+  const int64_t nv = a.d < vec_of<T>() ? INT32_MAX : ceil_div(a.d, vec_of<T>());
   const auto grid = [&](int rpb) { return dim3((unsigned)std::min<int64_t>(ceil_div(a.rows, rpb), 2048)); };
 #define KMP_NORM_CASE(TPR, NV)                                                                   \
   if (nv <= TPR * NV) {                                                                          \
@@ -481,7 +515,8 @@ int forward_as(hipStream_t s, const NormArgs& a) {
 template <typename T, typename W>
 int backward_as(hipStream_t s, const NormBackArgs& a) {
   typedef typename acc_of<T>::type A;
-  const int64_t parts = norm_partials(a.xtype, a.rows, a.d), nv = ceil_div(a.d, vec_of<T>());
+  const int64_t parts = norm_partials(a.xtype, a.rows, a.d);
+  const int64_t nv = a.d < vec_of<T>() ? INT32_MAX : ceil_div(a.d, vec_of<T>());
   const bool weights = a.dgamma || a.dbeta;
 #define KMP_NORM_CASE(TPR, NV)                                                                             \
   if (nv <= TPR * NV) {                                                                                    \
