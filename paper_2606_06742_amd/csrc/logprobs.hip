@@ -131,6 +131,32 @@ __device__ __forceinline__ key_t kth_of_groups(TopShared& sh, int k, key_t mine)
   return sh.bound;
 }
 
+// Writes the k largest of the n <= CAP different keys in sh.list in order, through
+// put(rank, key): every key's place is the number of larger ones. A long list is
+// cut first, by the k-th of its groups' maxima.
+template <typename Put>
+__device__ __forceinline__ void place_top(TopShared& sh, int k, int n, Put put) {
+  const int t = threadIdx.x;
+  const key_t* list = sh.list;
+  if (n > 96) {
+    const key_t bound = kth_of_groups(sh, k, max(t < n ? sh.list[t] : (key_t)0, t + BT < n ? sh.list[t + BT] : (key_t)0));
+    if (t == 0) sh.count = 0;
+    __syncthreads();
+    for (int i = t; i < n; i += BT)
+      if (sh.list[i] >= bound) sh.few[atomicAdd(&sh.count, 1)] = sh.list[i];
+    __syncthreads();
+    n = sh.count;
+    list = sh.few;
+  }
+  for (int i = t; i < n; i += BT) {
+    const key_t key = list[i];
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += list[j] > key;
+    if (rank < k) put(rank, key);
+  }
+}
+
 // The k largest of the keys that the threads hold: thread t's are visited by
 // visit(t, i) for i < per, each a call add(key); its largest lies in [lower,
 // upper] (0: it has none; different threads' lowers differ). The largest keys of
@@ -166,26 +192,7 @@ __device__ __forceinline__ void select_top(TopShared& sh, int k, key_t lower, ke
     if (t == 0) sh.count = 0;
     __syncthreads();
   }
-  // a long list (equal values below a bound of the value alone) once more by its
-  // own bound, then every key's place is the number of larger ones
-  const key_t* list = sh.list;
-  if (n > 96) {
-    bound = kth_of_groups(sh, k, max(t < n ? sh.list[t] : (key_t)0, t + BT < n ? sh.list[t + BT] : (key_t)0));
-    if (t == 0) sh.count = 0;
-    __syncthreads();
-    for (int i = t; i < n; i += BT)
-      if (sh.list[i] >= bound) sh.few[atomicAdd(&sh.count, 1)] = sh.list[i];
-    __syncthreads();
-    n = sh.count;
-    list = sh.few;
-  }
-  for (int i = t; i < n; i += BT) {
-    const key_t key = list[i];
-    int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += list[j] > key;
-    if (rank < k) put(rank, key);
-  }
+  place_top(sh, k, n, put);
 }
 
 __device__ __forceinline__ int64_t token_at(const void* tokens, bool wide, int64_t t) {
@@ -311,6 +318,16 @@ __global__ __launch_bounds__(BT) void logprob_join_kernel(LogprobArgs a, int seg
     if (a.top > 0) {
       const key_t* keys = keys_of(a, segs) + t * segs * a.top;
       const int n = segs * a.top;
+      const auto put = [&](int rank, key_t key) {
+        if (key != 0) put_top(a, t, row, rank, key);
+      };
+      if (n <= CAP) {                             // (empty places: 0, the last ones)
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += BT) sh.list[i] = keys[i] != 0 ? keys[i] : (key_t)i;
+        __syncthreads();
+        place_top(sh, a.top, n, put);
+        continue;
+      }
       key_t mine = 0;
       for (int i = threadIdx.x; i < n; i += BT) mine = max(mine, keys[i]);
       select_top(
@@ -319,9 +336,7 @@ __global__ __launch_bounds__(BT) void logprob_join_kernel(LogprobArgs a, int seg
             const int at = i * BT + owner;
             if (at < n && keys[at] != 0) add(keys[at]);
           },
-          [&](int rank, key_t key) {
-            if (key != 0) put_top(a, t, row, rank, key);
-          });
+          put);
     }
   }
 }

@@ -12,19 +12,28 @@ namespace {
 
 typedef int int4v __attribute__((ext_vector_type(4)));
 
-// The 16 bytes of row `p` from byte k on, zeros from byte K on. No byte past K
-// is touched.
+// The 16 bytes of row `p` from byte k on, zeros from byte K on. No byte outside
+// the row is touched: where the row ends within them, its last 16 bytes are read
+// and moved down (one load; sixteen conditional ones took 3 us of a short product).
 __device__ __forceinline__ int4v chunk16(const int8_t* p, int64_t k, int64_t K) {
-  int4v v = {0, 0, 0, 0};
-  if (k + 16 <= K) {
-    __builtin_memcpy(&v, p + k, 16);
-  } else if (k < K) {
-    int8_t b[16];
+  union { int4v v; uint64_t w[2]; int8_t b[16]; } u;
+  u.v = int4v{0, 0, 0, 0};
+  if (k >= K) return u.v;
+  const int over = (int)max((int64_t)0, k + 16 - K);
+  if (over <= k) {
+    __builtin_memcpy(&u, p + k - over, 16);
+    if (over >= 8) {
+      u.w[0] = u.w[1] >> (8 * over - 64);
+      u.w[1] = 0;
+    } else if (over > 0) {
+      u.w[0] = u.w[0] >> (8 * over) | u.w[1] << (64 - 8 * over);
+      u.w[1] >>= 8 * over;
+    }
+  } else {                                        // a row of less than 16 bytes
 #pragma unroll
-    for (int i = 0; i < 16; ++i) b[i] = k + i < K ? p[k + i] : (int8_t)0;
-    __builtin_memcpy(&v, b, 16);
+    for (int i = 0; i < 16; ++i) u.b[i] = k + i < K ? p[k + i] : (int8_t)0;
   }
-  return v;
+  return u.v;
 }
 
 template <typename O>
