@@ -207,13 +207,19 @@ def kmp_workspace_bytes(spec, n, d, L, fold_id, V, S, Q, sigma_batch) -> int:
                                          int(sigma_batch)))
 
 
+_current = None      # (device, handle of its current stream), once HIP is up
+
+
 def _stream_ptr(stream) -> int:
-    import torch
+    global _current
     if stream is None:
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is not None and torch.cuda.is_initialized():
-            return raw(torch._C._cuda_getDevice())     # 0.2 us against 2.9
+        if _current is not None:
+            return _current[1](_current[0]())          # 0.2 us; a stream object takes 2.9
+        import torch
         stream = torch.cuda.current_stream()
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            _current = torch._C._cuda_getDevice, raw
     return int(stream.cuda_stream)
 
 
@@ -272,16 +278,17 @@ def kmp_dgemm_grouped(A, B, C, stream=None) -> None:
 _TYPES: dict = {}
 
 
-def _type(t, name: str) -> int:
-    """KMP_* code of a tensor's (or torch) type."""
-    if not _TYPES:
+def _type(dtype, name: str) -> int:
+    """KMP_* code of a torch type."""
+    code = _TYPES.get(dtype)
+    if code is None:
         import torch
         _TYPES.update({torch.float64: KMP_F64, torch.float32: KMP_F32, torch.bfloat16: KMP_BF16,
                        torch.float16: KMP_F16, torch.int8: KMP_I8})
-    dtype = getattr(t, "dtype", t)
-    if dtype not in _TYPES:
-        raise KmpError(KMP_EINVAL, f"{name}: type {dtype} is not supported")
-    return _TYPES[dtype]
+        code = _TYPES.get(dtype)
+        if code is None:
+            raise KmpError(KMP_EINVAL, f"{name}: type {dtype} is not supported")
+    return code
 
 
 def _refuse(what: str):
@@ -290,16 +297,20 @@ def _refuse(what: str):
 
 def _matrix(t, name: str, rows=None, cols=None, dtype=None):
     """(pointer, rows, columns, row stride) of a 2-D device tensor."""
-    if t.dim() != 2 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         _refuse(f"{name} must be a 2-D device tensor")
-    (r, c), (sr, sc) = t.shape, t.stride()
+    r, c = shape
+    sr, sc = t.stride()
     if (rows is not None and r != rows) or (cols is not None and c != cols):
         _refuse(f"{name} has shape {r} x {c}, not {rows} x {cols}")
     if dtype is not None and t.dtype != dtype:
         _refuse(f"{name} has type {t.dtype}, not {dtype}")
-    if (sc != 1 and c > 1) or (r > 1 and sr < c):
+    if r <= 1:
+        sr = c or 1
+    if (sc != 1 and c > 1) or sr < c:
         _refuse(f"{name} must have consecutive elements in a row and rows that do not overlap")
-    return t.data_ptr(), r, c, sr if r > 1 else max(c, 1)
+    return t.data_ptr(), r, c, sr or 1
 
 
 def _vector(t, name: str, n: int, dtype=None):
@@ -337,17 +348,16 @@ def kmp_layer_norm(x, gamma, beta, eps, y, mean=None, rstd=None, scale=None, str
     (None: ones, zeros); mean and rstd (rows) take what the backward reads."""
     xp, rows, d, ldx = _matrix(x, "x")
     yp, _, _, ldy = _matrix(y, "y", rows, d)
-    xt = _type(x, "x")
+    xt = _type(x.dtype, "x")
     w = gamma if gamma is not None else beta
-    wt = _type(w, "gamma") if w is not None else xt
-    wd = w.dtype if w is not None else None
+    wd = w.dtype if w is not None else x.dtype
     sd = rd = None
     if mean is not None or rstd is not None or scale is not None:
         import torch
         sd, rd = torch.float64 if xt == KMP_F64 else torch.float32, torch.float32
     _check(lib().kmp_layer_norm(
-        _stream_ptr(stream), xt, xp, rows, d, ldx, wt, _vector(gamma, "gamma", d, wd),
-        _vector(beta, "beta", d, wd), float(eps), _type(y, "y"), yp, ldy,
+        _stream_ptr(stream), xt, xp, rows, d, ldx, _type(wd, "gamma"), _vector(gamma, "gamma", d, wd),
+        _vector(beta, "beta", d, wd), float(eps), _type(y.dtype, "y"), yp, ldy,
         _vector(mean, "mean", rows, sd), _vector(rstd, "rstd", rows, sd),
         _vector(scale, "scale", rows, rd)), allow_maxiter=False)
 
@@ -366,14 +376,12 @@ def kmp_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspa
     dxp, lddx = None, d
     if dx is not None:
         dxp, _, _, lddx = _matrix(dx, "dx", rows, d, x.dtype)
-    xt = _type(x, "x")
-    w = next((t for t in (gamma, dgamma, dbeta) if t is not None), None)
-    wt = _type(w, "gamma") if w is not None else xt
-    wd = w.dtype if w is not None else None
+    xt = _type(x.dtype, "x")
+    wd = next((t.dtype for t in (gamma, dgamma, dbeta) if t is not None), x.dtype)
     sd = torch.float64 if xt == KMP_F64 else torch.float32
     wsp, wsb = _workspace(workspace)
     _check(lib().kmp_layer_norm_backward(
-        _stream_ptr(stream), xt, dyp, lddy, xp, ldx, rows, d, wt, _vector(gamma, "gamma", d, wd),
+        _stream_ptr(stream), xt, dyp, lddy, xp, ldx, rows, d, _type(wd, "gamma"), _vector(gamma, "gamma", d, wd),
         _vector(mean, "mean", rows, sd), _vector(rstd, "rstd", rows, sd), dxp, lddx,
         _vector(dgamma, "dgamma", d, wd), _vector(dbeta, "dbeta", d, wd), wsp, wsb),
         allow_maxiter=False)
@@ -384,7 +392,7 @@ def kmp_quantize_rows(x, q, scale, stream=None) -> None:
     import torch
     xp, rows, d, ldx = _matrix(x, "x")
     qp, _, _, ldq = _matrix(q, "q", rows, d, torch.int8)
-    _check(lib().kmp_quantize_rows(_stream_ptr(stream), _type(x, "x"), xp, rows, d, ldx, qp, ldq,
+    _check(lib().kmp_quantize_rows(_stream_ptr(stream), _type(x.dtype, "x"), xp, rows, d, ldx, qp, ldq,
                                    _vector(scale, "scale", rows, torch.float32)), allow_maxiter=False)
 
 
@@ -399,7 +407,7 @@ def kmp_quantized_product(xq, xscale, wq, wscale, out, bias=None, stream=None) -
     f = torch.float32
     _check(lib().kmp_quantized_product(
         _stream_ptr(stream), xp, ldx, _vector(xscale, "xscale", M, f), M, wp, ldw,
-        _vector(wscale, "wscale", N, f), N, K, _vector(bias, "bias", N, f), _type(out, "out"), op,
+        _vector(wscale, "wscale", N, f), N, K, _vector(bias, "bias", N, f), _type(out.dtype, "out"), op,
         ldo), allow_maxiter=False)
 
 
@@ -423,7 +431,7 @@ def kmp_token_logprobs(logits, tokens, logp, entropy=None, stats=None, top_id=No
     f = torch.float32
     wsp, wsb = _workspace(workspace)
     _check(lib().kmp_token_logprobs(
-        _stream_ptr(stream), _type(logits, "logits"), lp, T, V, ldl, bits, tp,
+        _stream_ptr(stream), _type(logits.dtype, "logits"), lp, T, V, ldl, bits, tp,
         _vector(logp, "logp", T, f), _vector(entropy, "entropy", T, f), _vector(stats, "stats", 2 * T, f), top,
         _vector(top_id, "top_id", T * top, torch.int32), _vector(top_logp, "top_logp", T * top, f),
         wsp, wsb), allow_maxiter=False)
@@ -440,7 +448,7 @@ def kmp_token_logprobs_backward(logits, tokens, stats, dlogp, dlogits, entropy=N
     bits, tp = _tokens(tokens, T)
     f = torch.float32
     _check(lib().kmp_token_logprobs_backward(
-        _stream_ptr(stream), _type(logits, "logits"), lp, T, V, ldl, bits, tp,
+        _stream_ptr(stream), _type(logits.dtype, "logits"), lp, T, V, ldl, bits, tp,
         _vector(stats, "stats", 2 * T, f), _vector(entropy, "entropy", T, f), _vector(dlogp, "dlogp", T, f),
         _vector(dentropy, "dentropy", T, f), dp, ldd), allow_maxiter=False)
 
