@@ -3,8 +3,6 @@
 // x M x K and w N x K row-major. The sums are exact in 32-bit integers up to
 // K = 131071, so their order does not matter; they are converted to 32-bit
 // floats, scaled, and rounded once to the output's type.
-#include <type_traits>
-
 #include "kmp_operators.h"
 
 namespace kmp {
@@ -41,87 +39,64 @@ __device__ __forceinline__ O scaled(int acc, float xs, float ws, float bias) {
   return (O)((float)acc * xs * ws + bias);
 }
 
-// Few tokens: a workgroup takes 16 RB channels and 16 MT tokens, its NW wavefronts
+// Few tokens: a workgroup takes 16 channels and up to 16 tokens, its four wavefronts
 // each a run of the 64-byte slices of k, both operands from memory to registers,
-// SPD slices in flight; the wavefronts' sums are added in LDS (whole numbers: in
-// any order). Bound by reading w once. v_mfma_i32_16x16x64_i8: lane l holds 16 bytes of row l % 16 of either
+// DEEP slices in flight; the wavefronts' sums are added in LDS (whole numbers: in
+// any order). v_mfma_i32_16x16x64_i8: lane l holds 16 bytes of row l % 16 of either
 // operand from k = 16 (l / 16) on; register r of the result is D(row 4 (l / 16) +
 // r, column l % 16): w is the first operand, so a lane has four channels of one
-// token. Rows past the end repeat the last one and are not stored.
-template <typename O, int RB, int MT, int NW>
-__global__ __launch_bounds__(64 * NW) void qproduct_few_kernel(QProductArgs a) {
-  constexpr int SPD = RB + MT <= 2 ? 8 : RB + MT <= 4 ? 4 : 2;
-  __shared__ int sums[RB * MT][4][64];
+// token. Rows past the end repeat the last one and are not stored. Bound by reading
+// w once: 1 x 4096 x 4096 in 6.0 us, 2.8 TB/s (launch, one round of loads, sum).
+template <typename O>
+__global__ __launch_bounds__(256) void qproduct_few_kernel(QProductArgs a) {
+  constexpr int DEEP = 8;
+  __shared__ int sums[4][64];
   const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
-  for (int i = t; i < RB * MT * 256; i += 64 * NW) (&sums[0][0][0])[i] = 0;
+  (&sums[0][0])[t] = 0;
   const int row = lane & 15, c = (lane >> 4) * 16;
-  const int64_t n0 = (int64_t)blockIdx.x * (16 * RB);
-  const int8_t* pw[RB];
-  const int8_t* px[MT];
-#pragma unroll
-  for (int i = 0; i < RB; ++i) pw[i] = a.w + min(n0 + 16 * i + row, a.N - 1) * a.ldw;
-#pragma unroll
-  for (int j = 0; j < MT; ++j) px[j] = a.x + min((int64_t)(16 * j + row), a.M - 1) * a.ldx;
-  // whole slices, dealt to the wavefronts in runs
-  const int whole = (int)a.K / 64, run = (whole + NW - 1) / NW;
-  const int s0 = min(w * run, whole), s1 = min(s0 + run, whole);
-  int4v acc[RB][MT] = {}, fw[SPD][RB], fx[SPD][MT];
-  const int n = s1 - s0;
-  const auto fetch = [&](int i, int4v (&vw)[RB], int4v (&vx)[MT]) {
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int8_t* pw = a.w + min(n0 + row, a.N - 1) * a.ldw;
+  const int8_t* px = a.x + min((int64_t)row, a.M - 1) * a.ldx;
+  // whole slices, dealt to the wavefronts in runs of n from s0 on
+  const int whole = (int)a.K / 64, run = (whole + 3) / 4;
+  const int s0 = min(w * run, whole), n = min(s0 + run, whole) - s0;
+  int4v acc = {}, fw[DEEP], fx[DEEP];
+  const auto fetch = [&](int i, int4v& vw, int4v& vx) {
     const int k = 64 * (s0 + min(i, n - 1)) + c;  // past the end: the last slice again, unused
-#pragma unroll
-    for (int i = 0; i < RB; ++i) __builtin_memcpy(&vw[i], pw[i] + k, 16);
-#pragma unroll
-    for (int j = 0; j < MT; ++j) __builtin_memcpy(&vx[j], px[j] + k, 16);
+    __builtin_memcpy(&vw, pw + k, 16);
+    __builtin_memcpy(&vx, px + k, 16);
   };
-  const auto products = [&](const int4v (&vw)[RB], const int4v (&vx)[MT]) {
-#pragma unroll
-    for (int i = 0; i < RB; ++i)
-#pragma unroll
-      for (int j = 0; j < MT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vw[i], vx[j], acc[i][j], 0, 0, 0);
+  const auto products = [&](const int4v& vw, const int4v& vx) {
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(vw, vx, acc, 0, 0, 0);
   };
   if (n > 0) {
 #pragma unroll
-    for (int p = 0; p < SPD; ++p) fetch(p, fw[p], fx[p]);
+    for (int p = 0; p < DEEP; ++p) fetch(p, fw[p], fx[p]);
     int i = 0;
-    for (; i + SPD < n; i += SPD) {
+    for (; i + DEEP < n; i += DEEP) {
 #pragma unroll
-      for (int p = 0; p < SPD; ++p) {
+      for (int p = 0; p < DEEP; ++p) {
         products(fw[p], fx[p]);
-        fetch(i + SPD + p, fw[p], fx[p]);
+        fetch(i + DEEP + p, fw[p], fx[p]);
       }
     }
 #pragma unroll
-    for (int p = 0; p < SPD; ++p)
+    for (int p = 0; p < DEEP; ++p)
       if (i + p < n) products(fw[p], fx[p]);
   }
-  if (w == NW - 1 && a.K % 64 != 0) {             // the rest of k, zeros past its end
-#pragma unroll
-    for (int i = 0; i < RB; ++i) fw[0][i] = chunk16(pw[i], 64 * whole + c, a.K);
-#pragma unroll
-    for (int j = 0; j < MT; ++j) fx[0][j] = chunk16(px[j], 64 * whole + c, a.K);
-    products(fw[0], fx[0]);
-  }
+  if (w == 3 && a.K % 64 != 0)                    // the rest of k, zeros past its end
+    products(chunk16(pw, 64 * whole + c, a.K), chunk16(px, 64 * whole + c, a.K));
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < RB; ++i)
-#pragma unroll
-    for (int j = 0; j < MT; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) atomicAdd(&sums[i * MT + j][r][lane], acc[i][j][r]);
+  for (int r = 0; r < 4; ++r) atomicAdd(&sums[r][lane], acc[r]);
   __syncthreads();
-  for (int b = w; b < RB * MT; b += NW) {
-    int v[4];
+  if (w > 0 || row >= a.M) return;
+  const int64_t n1 = n0 + (lane >> 4) * 4;
+  const float xs = a.xscale[row];
+  O* out = static_cast<O*>(a.out) + row * a.ldo + n1;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = sums[b][r][lane];
-    const int64_t m = 16 * (b % MT) + row, n = n0 + 16 * (b / MT) + (lane >> 4) * 4;
-    if (m >= a.M) continue;
-    const float xs = a.xscale[m];
-    O* out = static_cast<O*>(a.out) + m * a.ldo + n;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (n + r < a.N) out[r] = scaled<O>(v[r], xs, a.wscale[n + r], a.bias ? a.bias[n + r] : 0.0f);
-  }
+  for (int r = 0; r < 4; ++r)
+    if (n1 + r < a.N) out[r] = scaled<O>(sums[r][lane], xs, a.wscale[n1 + r], a.bias ? a.bias[n1 + r] : 0.0f);
 }
 
 typedef int int16v __attribute__((ext_vector_type(16)));
@@ -130,12 +105,13 @@ typedef int int16v __attribute__((ext_vector_type(16)));
 // same for the wavefront). The compiler does not count these loads: they are
 // waited for by wait_loads.
 __device__ __forceinline__ void load_to_lds(const int8_t* p, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(p) : "memory", "m0");
 }
 // Waits until no more than LEFT of the wavefront's last loads are under way.
 template <int LEFT>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(LEFT) : "memory"); }
 
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 // Barrier of the workgroup that leaves the wavefront's own reads and loads under
 // way (what has to have ended is waited for before it, or by its use).
 __device__ __forceinline__ void barrier() { asm volatile("s_barrier" ::: "memory"); }
@@ -222,12 +198,16 @@ __device__ __forceinline__ void store_tile(const QProductArgs& a, const int16v (
 // Tiles of TM x TN, WR x WC wavefronts of 32 x 32 blocks of v_mfma_i32_32x32x32_i8
 // each (lane l holds 16 bytes of row l % 32 of either operand from k = 16 (l / 32)
 // on; register r of the result is D(row 8 (r / 4) + 4 (l / 32) + r % 4, column l %
-// 32); w is the first operand), slices of 128 bytes of k through two LDS stages: while one is multiplied
-// the next is on its way. A row of a slice is eight 16-byte chunks, chunk c kept
-// at place c ^ (row / 2 % 8), so that 16 lanes with 16 rows and one c read all 64
-// banks. Rows past the end repeat the last one and are not stored; a last slice
-// that is not whole is brought up with zeros. ALIGNED: rows start at multiples of
-// 16 bytes and go from memory to LDS without registers.
+// 32); w is the first operand), slices of 128 bytes of k through a ring of NS LDS
+// stages: while one is multiplied the next NS - 1 are on their way. A row of a slice
+// is eight 16-byte chunks, chunk c kept at place c ^ (row / 2 % 8), so that 16 lanes
+// with 16 rows and one c read all 64 banks. Rows past the end repeat the last one
+// and are not stored; a last slice that is not whole is brought up with zeros. WK >
+// 1: so many groups of wavefronts, each with a ring of its own and every WK-th
+// slice, for products with few tiles, whose time is the chain of slices (0.2 to 0.3
+// us each); their sums are added in LDS. ALIGNED: rows start at multiples of 16
+// bytes and go from memory to LDS without registers; else through registers, which
+// hold the next slice while one is multiplied.
 template <typename O, int TM, int TN, int WR, int WC, int WK, int NS, bool ALIGNED>
 __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProductArgs a, int tm, int tn) {
   constexpr int NW = WR * WC, QA = TM / 8 / NW, QB = TN / 8 / NW;   // loads a wavefront, 8 rows each
@@ -356,90 +336,99 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
   store_tile<O, MB, NB>(a, acc, m0 + wr * MB * 32, n0 + wc * NB * 32, lane, lds + SUMS + wg * REGION);
 }
 
-// The large form: tiles of 256 x 256, eight wavefronts of 128 x 64, aligned rows.
-// Slices of 64 bytes (a row of one is four chunks, chunk c at place c ^ (row / 4 %
-// 4): 16 rows with one c are in 16 different places of all banks) through a ring of
-// four stages, read one half slice ahead: when a wavefront passes the barrier of
-// slice s, slice s + 1 has landed, so the operands of its first half are on their
-// way to registers while the second half of s is multiplied, and no product waits
-// for LDS or for the barrier. Slice s + 3 goes where s - 1 was.
-template <typename O>
-__global__ __launch_bounds__(512) void qproduct_big_kernel(QProductArgs a, int tm, int tn) {
-  constexpr int TM = 256, TN = 256, WC = 4, MB = 4, NB = 2, Q = 2, SL = 64, STAGE = (TM + TN) * SL;
-  __shared__ __align__(16) int8_t lds[4 * STAGE];
+// The larger forms, aligned rows: slices as in qproduct_tile_kernel in a ring of NS
+// stages, and the operands of every 32 bytes of k are read from LDS while the 32
+// before them are multiplied. The barrier of slice s stands before its last 32:
+// their operands are in registers, so that the stage is free for slice s + NS, and
+// slice s + 1 has landed, so that its first operands can be read behind the last
+// products of s: no product waits for LDS or for the barrier. (Slices of 64 bytes
+// through four stages had twice the requests to the second-level cache.)
+template <typename O, int TM, int TN, int WR, int WC, int NS>
+__global__ __launch_bounds__(64 * WR * WC) void qproduct_ahead_kernel(QProductArgs a, int tm, int tn) {
+  constexpr int NW = WR * WC, MB = TM / WR / 32, NB = TN / WC / 32, QA = TM / 8 / NW, QB = TN / 8 / NW;
+  constexpr int SL = 128, STAGE = (TM + TN) * SL;
+  static_assert(QA % 2 == 0 && QB % 2 == 0, "pairs of eight rows");
+  static_assert(NW * region_bytes<O, MB, NB>() <= NS * STAGE, "the regions fit the ring");
+  __shared__ __align__(16) int8_t lds[NS * STAGE];
   int64_t m0, n0;
   if (!tile_of(tm, tn, TM, TN, m0, n0)) return;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = w / WC, wc = w % WC;
-  const int lr = lane >> 2, lc = ((lane & 3) ^ (lr >> 2 & 3)) * 16;   // loads: row of 16, byte of the slice
-  const int8_t* pa[Q];
-  const int8_t* pb[Q];
+  const int lr = lane >> 3;                                           // loads: row of eight, byte of the slice
+  const int lc[2] = {((lane & 7) ^ (lr >> 1)) * 16, ((lane & 7) ^ (4 + (lr >> 1))) * 16};
+  const int8_t* pa[QA];
+  const int8_t* pb[QB];
 #pragma unroll
-  for (int q = 0; q < Q; ++q) {
-    pa[q] = a.x + min(m0 + (w * Q + q) * 16 + lr, a.M - 1) * a.ldx;
-    pb[q] = a.w + min(n0 + (w * Q + q) * 16 + lr, a.N - 1) * a.ldw;
-  }
+  for (int q = 0; q < QA; ++q) pa[q] = a.x + min(m0 + (w * QA + q) * 8 + lr, a.M - 1) * a.ldx + lc[q & 1];
+#pragma unroll
+  for (int q = 0; q < QB; ++q) pb[q] = a.w + min(n0 + (w * QB + q) * 8 + lr, a.N - 1) * a.ldw + lc[q & 1];
   const uint32_t base = (uint32_t)(uintptr_t)lds;                     // LDS addresses have 32 bits
   const auto fetch = [&](int s) {
-    const uint32_t at = base + (s & 3) * STAGE + w * Q * 1024;
+    const uint32_t at = base + s % NS * STAGE;
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      load_to_lds(pa[q] + s * SL + lc, at + q * 1024);
-      load_to_lds(pb[q] + s * SL + lc, at + TM * SL + q * 1024);
-    }
+    for (int q = 0; q < QA; ++q) load_to_lds(pa[q] + s * SL, at + (w * QA + q) * 1024);
+#pragma unroll
+    for (int q = 0; q < QB; ++q) load_to_lds(pb[q] + s * SL, at + TM * SL + (w * QB + q) * 1024);
   };
   int16v acc[MB][NB] = {};
   const int row = lane & 31, half = lane >> 5;
   const int8_t* la = lds + (wr * MB * 32 + row) * SL;
   const int8_t* lb = lds + TM * SL + (wc * NB * 32 + row) * SL;
   int4v fa[2][MB], fb[2][NB];
-  const auto read = [&](int s, int h) {                               // half h of slice s
-    const int c = ((2 * h + half) ^ (row >> 2 & 3)) * 16 + (s & 3) * STAGE;
+  const auto read = [&](int s, int h) {                               // bytes 32 h .. of slice s
+    const int c = ((2 * h + half) ^ (row >> 1 & 7)) * 16 + s % NS * STAGE;
 #pragma unroll
-    for (int i = 0; i < MB; ++i) fa[h][i] = *reinterpret_cast<const int4v*>(la + i * 32 * SL + c);
+    for (int i = 0; i < MB; ++i) fa[h & 1][i] = *reinterpret_cast<const int4v*>(la + i * 32 * SL + c);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) fb[h][j] = *reinterpret_cast<const int4v*>(lb + j * 32 * SL + c);
+    for (int j = 0; j < NB; ++j) fb[h & 1][j] = *reinterpret_cast<const int4v*>(lb + j * 32 * SL + c);
+    __builtin_amdgcn_sched_barrier(0);                                // (else the reads sink to their uses)
   };
   const auto multiply = [&](int h) {
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int j = 0; j < NB; ++j)
-        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[h][j], fa[h][i], acc[i][j], 0, 0, 0);
+        acc[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[h & 1][j], fa[h & 1][i], acc[i][j], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
   };
   const int whole = (int)a.K / SL, tail = (int)a.K % SL;
   if (whole > 0) {
-    for (int s = 0; s < min(3, whole); ++s) fetch(s);
-    wait_loads<0>();
+    for (int s = 0; s < min(NS, whole); ++s) fetch(s);
+    if (whole >= NS) wait_loads<(NS - 1) * (QA + QB)>();
+    else wait_loads<0>();
     barrier();
     read(0, 0);
     for (int s = 0; s < whole; ++s) {
-      if (s + 2 < whole) wait_loads<2 * Q>();                         // s + 1 has landed, s + 2 may not have
+#pragma unroll
+      for (int h = 0; h < 3; ++h) {
+        read(s, h + 1);
+        multiply(h);
+      }
+      if (s + NS <= whole) wait_loads<(NS - 2) * (QA + QB)>();        // s + 1 has landed, the later ones may not have
       else wait_loads<0>();
+      wait_lds();                                                     // the last operands of s are here
       barrier();
-      if (s + 3 < whole) fetch(s + 3);
-      read(s, 1);
-      __builtin_amdgcn_sched_barrier(0);                              // (else the reads sink to their uses)
-      multiply(0);
-      __builtin_amdgcn_sched_barrier(0);
-      read(s + 1, 0);                                                 // (after the last slice: not used)
-      __builtin_amdgcn_sched_barrier(0);
-      multiply(1);
+      if (s + NS < whole) fetch(s + NS);
+      if (s + 1 < whole) read(s + 1, 0);
+      multiply(3);
     }
   }
   if (tail > 0) {                                                     // zeros past K
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      int8_t* at = lds + (w * Q + q) * 1024 + lane * 16;
-      *reinterpret_cast<int4v*>(at) = chunk16(pa[q], whole * SL + lc, a.K);
-      *reinterpret_cast<int4v*>(at + TM * SL) = chunk16(pb[q], whole * SL + lc, a.K);
-    }
+    for (int q = 0; q < QA; ++q)
+      *reinterpret_cast<int4v*>(lds + (w * QA + q) * 1024 + lane * 16) =
+          chunk16(pa[q] - lc[q & 1], whole * SL + lc[q & 1], a.K);
+#pragma unroll
+    for (int q = 0; q < QB; ++q)
+      *reinterpret_cast<int4v*>(lds + TM * SL + (w * QB + q) * 1024 + lane * 16) =
+          chunk16(pb[q] - lc[q & 1], whole * SL + lc[q & 1], a.K);
     __syncthreads();
-    read(0, 0);
-    read(0, 1);
-    multiply(0);
-    multiply(1);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      read(0, h);
+      multiply(h);
+    }
   }
   __syncthreads();                                                    // the ring is free
   store_tile<O, MB, NB>(a, acc, m0 + wr * MB * 32, n0 + wc * NB * 32, lane, lds + w * region_bytes<O, MB, NB>());
@@ -449,51 +438,60 @@ bool aligned_rows(const QProductArgs& a) {
   return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | a.ldx | a.ldw) & 15) == 0;
 }
 
-template <typename O, int TM, int TN, int WR, int WC, int WK, int NS>
-int tiles_as(hipStream_t s, const QProductArgs& a) {
+template <int TM, int TN, typename F>
+int launch_tiles(hipStream_t s, const QProductArgs& a, F kernel, int threads) {
   const int tm = (int)ceil_div(a.M, TM), tn = (int)ceil_div(a.N, TN);
-  const dim3 grid((unsigned)round_up((int64_t)tm * tn, 8)), block(64 * WR * WC);
-  if (aligned_rows(a))
-    hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, WK, NS, true>), grid, dim3(64 * WR * WC * WK), 0, s, a, tm, tn);
-  else
-    hipLaunchKernelGGL((qproduct_tile_kernel<O, TM, TN, WR, WC, 1, 2, false>), grid, block, 0, s, a, tm, tn);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)round_up((int64_t)tm * tn, 8)), dim3(threads), 0, s, a, tm, tn);
   KMP_LAUNCH_CHECK();
   return 0;
 }
+template <typename O, int TM, int TN, int WR, int WC, int WK, int NS, bool ALIGNED>
+int tiles_as(hipStream_t s, const QProductArgs& a) {
+  return launch_tiles<TM, TN>(s, a, qproduct_tile_kernel<O, TM, TN, WR, WC, WK, NS, ALIGNED>, 64 * WR * WC * WK);
+}
+template <typename O, int TM, int TN, int WR, int WC>
+int ahead_as(hipStream_t s, const QProductArgs& a) {
+  return launch_tiles<TM, TN>(s, a, qproduct_ahead_kernel<O, TM, TN, WR, WC, 2>, 64 * WR * WC);
+}
 
-// Which form, by what keeps the chip's 256 compute units busy; us per launch at M x
-// N x K, w from HBM (few = qproduct_few_kernel, else rows x columns of a tile, WK):
-//                    few  32x64,4  64x64,2+  64x64,2  64x64,1  128,1  256,1  floor
-//   1 x 4096 x 4096    6.1    7.9     10.5     12.1     17.4     22     50     3.5
-//   16 x 12288 x 4096 16.4   13.5     13.8     19.1     27       34     53    10.5
-//   16 x 32000 x 2048 21.5   18.8     18.8     15.6     18.3     21            13.8
-//   64 x 4096 x 4096  12.8    9.7     12.1     14.2     18       28     56     3.6
-//   128 x 4096 x 4096 21     10.2     12.3     14.2     18.6     29     62     3.8
-//   256 x 4096 x 4096 38     17.5     12.9     14.6     18.9     29     66     4.2
-//   64 x 12288 x 4096 33     23       17.6     20.8     28       38     58    10.8
-//   512 x 4096 x 4096 74     33       23       18.7     20.2     30     66     8.4
-//   2048 x 2048 x 2048 77    46       31       22.3     18.5     22     46     8.4
-//   4096 x 16384 x 4096                                525      437    366   269
-// (64x64,2+ has a ring of three slices, 64x64,2 of two and so two workgroups a
-// compute unit). The floor is the bytes at a copy's 4.82 TB/s or the products at
-// the 2040 TOP/s of the library's 8-bit product of order 8192.
+// Which form, by what keeps the chip's 256 compute units busy. us per launch at M x
+// N x K, w from HBM: few tokens; tiles of 32 x 64 (four groups over k, ring of 3), 64
+// x 64 (two groups, ring of 3, or of 2 and so two workgroups a compute unit); operands
+// ahead in tiles of 128 and 256; 64 and 128 unaligned (64u, 128u); the floor, the
+// larger of the bytes at a copy's 4.82 TB/s and the products at the 2040 TOP/s of the
+// library's 8-bit product of order 8192:
+//                      few  32x64  64,3  64,2   128   256   64u  128u  floor
+//   1 x 4096 x 4096    6.0   7.5   9.7  12.0  20.9  48.7  34.2  61.4   3.5
+//   16 x 8192 x 4096  11.6  10.4  11.4  16.6  30.0  51.2  41.2  65.6   7.0
+//   16 x 32000 x 2048 21.2  18.2  18.5  15.6  20.3  30.4  24.4  36.3  13.8
+//   64 x 1000 x 8192        11.8  15.8  21.6  39.6  91.8  64.8   118   1.8
+//   64 x 4096 x 4096         8.1  10.1  12.9  22.2  49.2  34.4  61.6   3.6
+//   128 x 4096 x 4096        8.7  10.7  12.8  23.4  50.2  34.3  62.5   3.8
+//   256 x 4096 x 4096       14.6  11.7  13.2  23.5  52.2  34.4  62.4   4.2
+//   64 x 12288 x 4096       20.8  16.5  19.8  32.3  52.6  43.0  67.4  10.8
+//   64 x 32000 x 2048       27.5  21.3  18.0  21.2  31.4  25.8  37.5  14.5
+//   512 x 4096 x 4096       27.0  19.6  16.6  24.0  52.0  36.6  62.4   8.4
+//   2048 x 2048 x 2048      35.9  24.6  18.4  16.6  31.7  26.2  35.8   8.4
+//   1024 x 8192 x 4096       132    89    74  45.6  60.5  94.3  74.3  33.7
+//   3000 x 5000 x 1000       159    83    63  36.4  32.6  55.2  51.5  14.7
+//   4096 x 4096 x 4096       224   169   135  87.0  71.0   184   145  67.4
+//   4096 x 16384 x 4096      850   632   534   364   293   672   534   269
 template <typename O>
 int product_as(hipStream_t s, const QProductArgs& a) {
   const auto tiles = [&](int tm, int tn) { return ceil_div(a.M, tm) * ceil_div(a.N, tn); };
-  if (a.M <= 16 && a.N <= 8192) {
-    hipLaunchKernelGGL((qproduct_few_kernel<O, 1, 1, 4>), dim3((unsigned)ceil_div(a.N, 16)), dim3(256), 0, s, a);
+  if (a.M <= 16 && a.N <= 6144) {
+    hipLaunchKernelGGL(qproduct_few_kernel<O>, dim3((unsigned)ceil_div(a.N, 16)), dim3(256), 0, s, a);
     KMP_LAUNCH_CHECK();
     return 0;
   }
-  if (tiles(32, 64) <= 256) return tiles_as<O, 32, 64, 1, 2, 4, 3>(s, a);
-  if (tiles(64, 64) <= 256) return tiles_as<O, 64, 64, 2, 2, 2, 3>(s, a);
-  if (tiles(64, 64) <= 512) return tiles_as<O, 64, 64, 2, 2, 2, 2>(s, a);
-  if (tiles(256, 256) < 192) return tiles_as<O, 64, 64, 2, 2, 1, 2>(s, a);
-  if (!aligned_rows(a)) return tiles_as<O, 128, 128, 2, 2, 1, 2>(s, a);
-  const int tm = (int)ceil_div(a.M, 256), tn = (int)ceil_div(a.N, 256);
-  hipLaunchKernelGGL(qproduct_big_kernel<O>, dim3((unsigned)round_up((int64_t)tm * tn, 8)), dim3(512), 0, s, a, tm, tn);
-  KMP_LAUNCH_CHECK();
-  return 0;
+  if (!aligned_rows(a))
+    return tiles(64, 64) <= 1024 ? tiles_as<O, 64, 64, 2, 2, 1, 2, false>(s, a)
+                                 : tiles_as<O, 128, 128, 2, 2, 1, 2, false>(s, a);
+  if (tiles(32, 64) <= 256) return tiles_as<O, 32, 64, 1, 2, 4, 3, true>(s, a);
+  if (tiles(64, 64) <= 256) return tiles_as<O, 64, 64, 2, 2, 2, 3, true>(s, a);
+  if (tiles(64, 64) <= 512) return tiles_as<O, 64, 64, 2, 2, 2, 2, true>(s, a);
+  if (tiles(256, 256) < 192) return ahead_as<O, 128, 128, 2, 4>(s, a);
+  return ahead_as<O, 256, 256, 2, 4>(s, a);
 }
 
 }  // namespace

@@ -268,7 +268,8 @@ PRODUCTS = [(1, 1, 1), (1, 17, 5), (3, 16, 0), (1, 64, 64), (2, 33, 130), (1, 10
             (17, 256, 65), (33, 100, 2051), (64, 513, 512), (65, 64, 127), (100, 300, 129), (128, 128, 128),
             (129, 257, 384), (255, 640, 130), (256, 256, 256), (257, 511, 259), (300, 2000, 1000), (520, 1030, 77),
             (1000, 3, 640), (2049, 513, 192),
-            (3500, 3600, 384), (3600, 3500, 130)]      # the largest tiles
+            (1100, 2100, 200),
+            (3500, 3600, 384), (3600, 3500, 130)]      # the larger tiles
 
 
 def _bytes(rng, r, k):
