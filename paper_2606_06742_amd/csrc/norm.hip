@@ -10,9 +10,12 @@
 namespace kmp {
 namespace {
 
-constexpr int BT = 256;                // threads of a workgroup
+constexpr int BT = 256, BIG = 1024;    // threads of a workgroup; of one for a long row
 // what is written: the norm in x's type or in 8 bits, or x itself in 8 bits
 enum { kNorm, kNormBytes, kBytesOfX };
+
+// The larger, or NaN where either is NaN.
+__device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }
 
 template <typename A>
 __device__ __forceinline__ A block_total(A v, A* red) {
@@ -23,30 +26,34 @@ __device__ __forceinline__ A block_total(A v, A* red) {
   __syncthreads();
   A t = 0;
 #pragma unroll
-  for (int i = 0; i < BT / 64; ++i) t += red[i];
+  for (int i = 0; i < BIG / 64; ++i) t += red[i];
   return t;
 }
 // Largest value, or NaN where any is NaN.
 __device__ __forceinline__ float block_most(float v, float* red) {
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    const float o = __shfl_xor(v, off, kWave);
-    v = o > v || o != o ? o : v;
-  }
+  for (int off = 32; off >= 1; off >>= 1) v = larger(v, __shfl_xor(v, off, kWave));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
   float t = red[0];
 #pragma unroll
-  for (int i = 1; i < BT / 64; ++i) t = red[i] > t || red[i] != red[i] ? red[i] : t;
+  for (int i = 1; i < BIG / 64; ++i) t = larger(t, red[i]);
   return t;
+}
+// f(j, N elements) over a row of d by a workgroup of BIG threads: whole vectors of
+// 16 bytes, then single elements.
+template <int N> struct Count { static constexpr int n = N; };
+template <int VEC, typename F>
+__device__ __forceinline__ void over_row(int64_t d, F f) {
+  const int64_t whole = d / VEC;
+#pragma unroll 2
+  for (int64_t v = threadIdx.x; v < whole; v += BIG) f(v * VEC, Count<VEC>());
+  if (whole * VEC + threadIdx.x < d) f(whole * VEC + threadIdx.x, Count<1>());
 }
 
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 __device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
-
-// The larger, or NaN where either is NaN.
-__device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }
 
 // The factor 127 / a that takes a row into 8 bits, and its scale a / 127.
 // Below 2^-100 the factor would overflow: such rows are brought up by 2^100
@@ -66,14 +73,15 @@ struct ByteScale {
 };
 
 // One workgroup per row, any length (rows too long for the registers, or shorter
-// than a vector): a pass for the mean, one for the
-// variance, one for the largest |y| of the 8-bit form, one to write.
+// than a vector): a pass for the mean, one for the variance, one for the largest
+// |y| of the 8-bit form, one to write; all but the first find the row in the cache.
 template <typename T, typename W, int MODE>
-__global__ __launch_bounds__(BT) void norm_row_kernel(NormArgs a) {
+__global__ __launch_bounds__(BIG) void norm_row_kernel(NormArgs a) {
   typedef typename acc_of<T>::type A;
   constexpr bool BYTES = MODE != kNorm, PLAIN = MODE == kBytesOfX;
-  __shared__ A red[BT / 64];
-  __shared__ float fred[BT / 64];
+  constexpr int VEC = vec_of<T>();
+  __shared__ A red[BIG / 64];
+  __shared__ float fred[BIG / 64];
   const W* gamma = static_cast<const W*>(a.gamma);
   const W* beta = static_cast<const W*>(a.beta);
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -81,39 +89,65 @@ __global__ __launch_bounds__(BT) void norm_row_kernel(NormArgs a) {
     A mu = 0, rs = 1;
     if constexpr (!PLAIN) {
       A s = 0;
-      for (int64_t j = threadIdx.x; j < a.d; j += BT) s += (A)x[j];
+      over_row<VEC>(a.d, [&](int64_t j, auto c) {
+        A v[c.n];
+        load_n(x + j, v);
+#pragma unroll
+        for (int e = 0; e < c.n; ++e) s += v[e];
+      });
       mu = block_total(s, red) / (A)a.d;
       A q = 0;
-      for (int64_t j = threadIdx.x; j < a.d; j += BT) {
-        const A t = (A)x[j] - mu;
-        q += t * t;
-      }
+      over_row<VEC>(a.d, [&](int64_t j, auto c) {
+        A v[c.n];
+        load_n(x + j, v);
+#pragma unroll
+        for (int e = 0; e < c.n; ++e) q += (v[e] - mu) * (v[e] - mu);
+      });
       rs = inv_sqrt(block_total(q, red) / (A)a.d + (A)a.eps);
       if (threadIdx.x == 0) {
         if (a.mean) static_cast<A*>(a.mean)[r] = mu;
         if (a.rstd) static_cast<A*>(a.rstd)[r] = rs;
       }
     }
-    const auto value = [&](int64_t j) {
-      if constexpr (PLAIN) return (A)x[j];
-      A v = ((A)x[j] - mu) * rs;
-      if (gamma) v *= (A)gamma[j];
-      if (beta) v += (A)beta[j];
-      return v;
+    const auto values = [&](int64_t j, auto& v) {
+      constexpr int N = sizeof(v) / sizeof(A);
+      load_n(x + j, v);
+      if constexpr (!PLAIN) {
+        A g[N], b[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) g[e] = 1, b[e] = 0;
+        if (gamma) load_n(gamma + j, g);
+        if (beta) load_n(beta + j, b);
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (v[e] - mu) * rs * g[e] + b[e];
+      }
     };
     if constexpr (BYTES) {
       float m = 0.0f;
-      for (int64_t j = threadIdx.x; j < a.d; j += BT) {
-        const float v = fabsf((float)value(j));
-        m = v > m || v != v ? v : m;
-      }
+      over_row<VEC>(a.d, [&](int64_t j, auto c) {
+        A v[c.n];
+        values(j, v);
+#pragma unroll
+        for (int e = 0; e < c.n; ++e) m = larger(m, fabsf((float)v[e]));
+      });
       const ByteScale b(block_most(m, fred));
       int8_t* y = static_cast<int8_t*>(a.y) + r * a.ldy;
-      for (int64_t j = threadIdx.x; j < a.d; j += BT) y[j] = b((float)value(j));
+      over_row<VEC>(a.d, [&](int64_t j, auto c) {
+        A v[c.n];
+        int8_t q[c.n];
+        values(j, v);
+#pragma unroll
+        for (int e = 0; e < c.n; ++e) q[e] = b((float)v[e]);
+        store_n(y + j, q);
+      });
       if (threadIdx.x == 0) a.scale[r] = b.scale;
     } else {
       T* y = static_cast<T*>(a.y) + r * a.ldy;
-      for (int64_t j = threadIdx.x; j < a.d; j += BT) y[j] = (T)value(j);
+      over_row<VEC>(a.d, [&](int64_t j, auto c) {
+        A v[c.n];
+        values(j, v);
+        store_n(y + j, v);
+      });
     }
   }
 }
@@ -303,29 +337,45 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_reg_kernel(NormArgs a) {
   }
 }
 
-// dx of one row per workgroup, any length.
+// dx of one row per workgroup, any length: a pass for the two means, one to write.
 template <typename T, typename W>
-__global__ __launch_bounds__(BT) void norm_back_row_kernel(NormBackArgs a) {
+__global__ __launch_bounds__(BIG) void norm_back_row_kernel(NormBackArgs a) {
   typedef typename acc_of<T>::type A;
-  __shared__ A red[BT / 64];
+  constexpr int VEC = vec_of<T>();
+  __shared__ A red[BIG / 64];
   const W* gamma = static_cast<const W*>(a.gamma);
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
     const A mu = static_cast<const A*>(a.mean)[r], rs = static_cast<const A*>(a.rstd)[r];
+    const auto values = [&](int64_t j, auto& xh, auto& w) {
+      constexpr int N = sizeof(w) / sizeof(A);
+      A g[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) g[e] = 1;
+      load_n(x + j, xh);
+      load_n(dy + j, w);
+      if (gamma) load_n(gamma + j, g);
+#pragma unroll
+      for (int e = 0; e < N; ++e) xh[e] = (xh[e] - mu) * rs, w[e] *= g[e];
+    };
     A s1 = 0, s2 = 0;
-    for (int64_t j = threadIdx.x; j < a.d; j += BT) {
-      const A w = (A)dy[j] * (gamma ? (A)gamma[j] : (A)1);
-      s1 += w;
-      s2 += w * (((A)x[j] - mu) * rs);
-    }
+    over_row<VEC>(a.d, [&](int64_t j, auto c) {
+      A xh[c.n], w[c.n];
+      values(j, xh, w);
+#pragma unroll
+      for (int e = 0; e < c.n; ++e) s1 += w[e], s2 += w[e] * xh[e];
+    });
     s1 = block_total(s1, red) / (A)a.d;
     s2 = block_total(s2, red) / (A)a.d;
     T* dx = static_cast<T*>(a.dx) + r * a.lddx;
-    for (int64_t j = threadIdx.x; j < a.d; j += BT) {
-      const A w = (A)dy[j] * (gamma ? (A)gamma[j] : (A)1);
-      dx[j] = (T)(rs * (w - s1 - ((A)x[j] - mu) * rs * s2));
-    }
+    over_row<VEC>(a.d, [&](int64_t j, auto c) {
+      A xh[c.n], w[c.n];
+      values(j, xh, w);
+#pragma unroll
+      for (int e = 0; e < c.n; ++e) w[e] = rs * (w[e] - s1 - xh[e] * s2);
+      store_n(dx + j, w);
+    });
   }
 }
 
@@ -454,6 +504,7 @@ __global__ __launch_bounds__(BT) void norm_back_columns_kernel(NormBackArgs a, i
   if (j >= a.d) return;
   const int64_t r0 = (int64_t)blockIdx.y * strip, r1 = min(r0 + strip, a.rows);
   A dg = 0, db = 0;
+#pragma unroll 4
   for (int64_t r = r0; r < r1; ++r) {
     const A g = (A)static_cast<const T*>(a.dy)[r * a.lddy + j];
     const A xh = ((A)static_cast<const T*>(a.x)[r * a.ldx + j] - static_cast<const A*>(a.mean)[r]) *
@@ -508,9 +559,12 @@ int forward_mode(hipStream_t s, const NormArgs& a) {
   KMP_NORM_CASE(256, 2)
   KMP_NORM_CASE(256, 4)
   KMP_NORM_CASE(1024, 2)
+  if constexpr (sizeof(T) >= 4) {                 // (more than 128 registers in 16 bits)
+    KMP_NORM_CASE(1024, 4)
+  }
 #undef KMP_NORM_CASE
   hipLaunchKernelGGL((norm_row_kernel<T, W, MODE>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
-                     dim3(BT), 0, s, a);
+                     dim3(BIG), 0, s, a);
   KMP_LAUNCH_CHECK();
   return 0;
 }
@@ -547,10 +601,10 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
     if (sizeof(T) >= 4 && nv <= 2048) {
       hipLaunchKernelGGL((norm_back_reg_kernel<T, W, 1024, sizeof(T) >= 4 ? 2 : 1>), dim3((unsigned)parts),
                          dim3(1024), 0, s, a);
-    } else {
+    } else {                                      // x and dy are read again for the weights
       if (a.dx)
         hipLaunchKernelGGL((norm_back_row_kernel<T, W>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
-                           dim3(BT), 0, s, a);
+                           dim3(BIG), 0, s, a);
       if (weights)
         hipLaunchKernelGGL((norm_back_columns_kernel<T>), dim3((unsigned)ceil_div(a.d, BT), (unsigned)parts),
                            dim3(BT), 0, s, a, ceil_div(a.rows, parts));

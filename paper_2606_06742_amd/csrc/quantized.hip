@@ -434,8 +434,10 @@ __global__ __launch_bounds__(64 * WR * WC) void qproduct_ahead_kernel(QProductAr
   store_tile<O, MB, NB>(a, acc, m0 + wr * MB * 32, n0 + wc * NB * 32, lane, lds + w * region_bytes<O, MB, NB>());
 }
 
+// Every row at a multiple of 16 bytes (a single row's pitch means nothing).
 bool aligned_rows(const QProductArgs& a) {
-  return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | a.ldx | a.ldw) & 15) == 0;
+  const int64_t pitch = (a.M > 1 ? a.ldx : 0) | (a.N > 1 ? a.ldw : 0);
+  return ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)pitch) & 15) == 0;
 }
 
 template <int TM, int TN, typename F>
