@@ -239,6 +239,12 @@ __device__ __forceinline__ key_t* keys_of(const LogprobArgs& a, int segs) {
   return reinterpret_cast<key_t*>(static_cast<char*>(a.workspace) + round_up(a.T * segs * (int64_t)sizeof(Part), 16));
 }
 
+// The lowest finite value, which masks are often made of.
+template <typename T> __device__ constexpr float lowest();
+template <> __device__ constexpr float lowest<float>() { return -0x1.fffffep127f; }
+template <> __device__ constexpr float lowest<bf16_t>() { return -0x1.fep127f; }
+template <> __device__ constexpr float lowest<f16_t>() { return -65504.0f; }
+
 // One workgroup per segment of a row (gridDim.x of them, span elements each): one
 // pass of 16-byte loads, U in flight, every thread with its own maximum and sums;
 // with TOP a second look at the few threads that can hold the alternatives. With
@@ -283,6 +289,18 @@ __global__ __launch_bounds__(BT, 8) void logprob_span_kernel(LogprobArgs a, int6
     else if (threadIdx.x == 0)
       parts_of(a)[unit] = p;
     if constexpr (TOP) {
+      const auto put = [&](int rank, key_t key) {
+        if (segs > 1) keys_of(a, segs)[unit * a.top + rank] = key;
+        else if (key != 0) put_top(a, t, row, rank, key);
+      };
+      // a segment of masked tokens only (-inf, or the type's lowest value: s then
+      // counts them): the first ones
+      const uint32_t few = min((uint32_t)a.top, len);
+      if (p.m == -INFINITY || (p.m == lowest<T>() && p.s == (float)len && len < 1u << 24)) {
+        if (threadIdx.x < a.top)
+          put(threadIdx.x, threadIdx.x < few ? key_of(p.m, (uint32_t)e0 + threadIdx.x) : (key_t)0);
+        continue;
+      }
       // this thread's best key lies between these two: its vector is known, not
       // the place in it
       const bool any = threadIdx.x * VEC < len;
@@ -298,10 +316,7 @@ __global__ __launch_bounds__(BT, 8) void logprob_span_kernel(LogprobArgs a, int6
             for (int e = 0; e < VEC; ++e)
               if (at + e < len) add(key_of(v[e], (uint32_t)e0 + at + e));
           },
-          [&](int rank, key_t key) {
-            if (segs > 1) keys_of(a, segs)[unit * a.top + rank] = key;
-            else if (key != 0) put_top(a, t, row, rank, key);
-          });
+          put);
     }
   }
 }
@@ -395,13 +410,15 @@ __global__ __launch_bounds__(BT) void logprob_back_kernel(LogprobBackArgs a) {
   }
 }
 
-// Segments of a row: one where there are rows enough for the chip (four
-// workgroups a compute unit), else as many as make them so, of at least 4096
-// elements.
+// Segments of a row: as many as make four workgroups a compute unit, of at least
+// 4096 elements (8192: 2 x 32000 with 20 alternatives 12.1 -> 11.7 us, 1 x 128000
+// 12.9 -> 13.5). Two or three are not worth the join for rows of up to 65536: us in
+// two or three segments against one, 2 x 12000 11.6 / 8.2, 333 x 40009 14.5 / 12.1,
+// 512 x 50001 26.9 / 25.8, but 300 x 128000 19.4 / 23.5, 500 x 128000 38.5 / 51.7.
 struct Split { int segs; int64_t span; };
 Split split(int64_t T, int64_t V) {
   const int64_t segs = std::min<int64_t>({1024 / std::max<int64_t>(T, 1), ceil_div(V, 4096), kMaxSegs});
-  if (segs <= 1) return {1, V};
+  if (segs <= 1 || (segs <= 3 && V <= 65536)) return {1, V};
   const int64_t span = round_up(ceil_div(V, segs), 1024);
   return {(int)ceil_div(V, span), span};
 }
