@@ -412,20 +412,22 @@ __global__ __launch_bounds__(BT) void logprob_back_kernel(LogprobBackArgs a) {
 
 // Segments of a row: as many as make four workgroups a compute unit, of at least
 // 4096 elements (8192: 2 x 32000 with 20 alternatives 12.1 -> 11.7 us, 1 x 128000
-// 12.9 -> 13.5). Two or three are not worth the join for rows of up to 65536: us in
-// two or three segments against one, 2 x 12000 11.6 / 8.2, 333 x 40009 14.5 / 12.1,
-// 512 x 50001 26.9 / 25.8, but 300 x 128000 19.4 / 23.5, 500 x 128000 38.5 / 51.7.
+// 12.9 -> 13.5). One for rows of up to 64 KB, whose pass costs less than the join
+// (16 x 20000 in 16 bits 11.1 / 7.9 us, with 20 alternatives 13.1 / 10.6), and in
+// place of two or three for rows of up to 65536: 333 x 40009 in 32 bits 14.5 / 12.1,
+// 512 x 50001 26.9 / 25.8, but 300 x 128000 in 16 bits 19.4 / 23.5, 500 x 128000
+// 38.5 / 51.7.
 struct Split { int segs; int64_t span; };
-Split split(int64_t T, int64_t V) {
+Split split(int64_t T, int64_t V, int size) {
   const int64_t segs = std::min<int64_t>({1024 / std::max<int64_t>(T, 1), ceil_div(V, 4096), kMaxSegs});
-  if (segs <= 1 || (segs <= 3 && V <= 65536)) return {1, V};
+  if (segs <= 1 || V * size <= 65536 || (segs <= 3 && V <= 65536)) return {1, V};
   const int64_t span = round_up(ceil_div(V, segs), 1024);
   return {(int)ceil_div(V, span), span};
 }
 
 template <typename T>
 int forward_as(hipStream_t s, const LogprobArgs& a) {
-  const auto [segs, span] = split(a.T, a.V);
+  const auto [segs, span] = split(a.T, a.V, (int)sizeof(T));
   const dim3 grid(segs, (unsigned)std::min<int64_t>(a.T, 65535));
   if (a.top > 0)
     hipLaunchKernelGGL((logprob_span_kernel<T, true>), grid, dim3(BT), 0, s, a, span);
@@ -451,7 +453,7 @@ int backward_as(hipStream_t s, const LogprobBackArgs& a) {
 }  // namespace
 
 size_t logprob_workspace(int64_t T, int64_t V, int top) {
-  const int segs = split(T, V).segs;
+  const int segs = split(T, V, 4).segs;           // 32 bits are split the most
   if (segs == 1) return 256;
   return (size_t)(round_up(T * segs * (int64_t)sizeof(Part), 16) + T * segs * top * (int64_t)sizeof(key_t));
 }

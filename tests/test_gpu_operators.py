@@ -467,7 +467,7 @@ def _edge_rows(V, lowest):
 
 
 @pytest.mark.parametrize("xt", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("V", [70, 1000, 8191, 50000])
+@pytest.mark.parametrize("V", [70, 1000, 8191, 20011, 50000])
 @pytest.mark.parametrize("copies", [1, 40])
 def test_token_logprobs_rows_that_go_wrong_easily(xt, V, copies):
     """Few rows and many rows (which may take different forms)."""
