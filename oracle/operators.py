@@ -36,7 +36,7 @@ def quantize_rows(x):
         a = np.abs(x).max(axis=1)                  # NaN where a row has one
         lift = np.where(a < np.float32(2.0 ** -100), np.float32(2.0 ** 100), np.float32(1.0)).astype(np.float32)
         good = a < np.inf
-        factor = np.where(good & (a > 0), np.float32(127.0) / (a * lift), np.float32(0.0)).astype(np.float32)
+        factor = np.where(good & (a > 0), np.float32(1.0) / (a * lift) * np.float32(127.0), np.float32(0.0)).astype(np.float32)
         q = np.rint((x * lift[:, None]) * factor[:, None])
         q = np.where((factor > 0)[:, None], np.clip(q, -127, 127), 0)
         scale = np.where(good, a / np.float32(127.0), np.float32(np.nan)).astype(np.float32)

@@ -3,7 +3,7 @@
 //   dx = r (w - mean(w) - xh mean(w xh)),  w = dy g,  xh = (x - mu) r
 //   dg_j = sum over rows of dy xh,  db_j = sum over rows of dy
 // The variance is the mean square of x - mu in a pass of its own (no
-// cancellation of two large sums). The 8-bit form writes rint(y 127 / a) with
+// cancellation of two large sums). The 8-bit form writes rint(y (1 / a) 127) with
 // a = max_j |y_j| and the row's scale a / 127.
 #include "kmp_operators.h"
 
@@ -55,7 +55,7 @@ __device__ __forceinline__ void over_row(int64_t d, F f) {
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 __device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
 
-// The factor 127 / a that takes a row into 8 bits, and its scale a / 127.
+// The factor (1 / a) 127 that takes a row into 8 bits, and its scale a / 127.
 // Below 2^-100 the factor would overflow: such rows are brought up by 2^100
 // first. A row with an infinity or NaN gets factor 0 and scale NaN.
 struct ByteScale {
@@ -63,7 +63,7 @@ struct ByteScale {
   __device__ explicit ByteScale(float a) {
     const bool tiny = a < 0x1p-100f, good = a < INFINITY;
     lift = tiny ? 0x1p100f : 1.0f;
-    factor = good && a > 0.0f ? 127.0f / (a * lift) : 0.0f;
+    factor = good && a > 0.0f ? 1.0f / (a * lift) * 127.0f : 0.0f;
     scale = good ? a / 127.0f : __builtin_nanf("");
   }
   __device__ int8_t operator()(float v) const {
