@@ -563,3 +563,36 @@ def test_operators_replayed_from_a_graph():
         for k in eager:
             if k not in ("ws", "wn"):
                 assert torch.equal(eager[k], kept[k]), (i, k)
+
+
+@pytest.mark.parametrize("xt", ["f32", "bf16", "f16"])
+def test_token_logprobs_of_masks_alone(xt):
+    """Rows and whole segments made of -inf and the type's lowest value: the
+    alternatives by index among equals, probabilities shared by the lowest ones."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    announce(f"token logprobs of masks alone {xt}")
+    lowest = {"f32": -3.4028234663852886e38, "bf16": -3.3895313892515355e38, "f16": -65504.0}[xt]
+    for V in (37, 9000, 70000):
+        a = np.full((5, V), -np.inf)
+        a[0, ::3] = lowest                        # both, mixed
+        a[1, V // 2:] = lowest                    # segments of one or the other
+        a[2, : V - 1] = lowest
+        a[3, V - 1] = lowest                      # the only possible token
+        a[4, : V // 2] = lowest
+        a[4, V - 2] = 1.0
+        x, xv = _put(a, _dtype(xt))
+        tok = np.array([3, V - 1, V - 1, V - 1, 0])
+        for top in (3, 20):
+            f = lambda *s: torch.empty(*s, device=device())
+            logp, ent, stats, tl, ti = f(5), f(5), f(5, 2), f(5, top), torch.empty(5, top, dtype=torch.int32, device=device())
+            ws = torch.empty(km.kmp_token_logprobs_workspace_bytes(5, V, top), dtype=torch.uint8, device=device())
+            km.kmp_token_logprobs(x, torch.as_tensor(tok, device=device()), logp, entropy=ent, stats=stats, top_id=ti,
+                                  top_logp=tl, workspace=ws)
+            o = OO.token_logprobs(xv, tok, top)
+            assert np.array_equal(ti.cpu().numpy(), o["top_id"])
+            # every term is exp(0) = 1 or 0: s is exact, log s within 2u of itself
+            for got, want in ((logp, o["logp"]), (ent, o["entropy"]), (stats, o["stats"]), (tl, o["top_logp"])):
+                got = _np(got)
+                with np.errstate(invalid="ignore"):
+                    assert np.all((got == want) | (np.abs(got - want) <= 4 * U["f32"] * np.abs(want))), (V, top)
