@@ -379,17 +379,53 @@ __global__ __launch_bounds__(BIG) void norm_back_row_kernel(NormBackArgs a) {
   }
 }
 
+// dgamma and dbeta of columns j0 .. j0 + 15 over all rows by a workgroup of NT
+// threads: 16 columns beside each other, every NT / 16-th row, then the row groups
+// in order. `sums` holds 2 NT values.
+template <typename T, typename W, int NT, typename A>
+__device__ __forceinline__ void sum_columns(const NormBackArgs& a, int64_t j0, A* sums) {
+  constexpr int G = NT / 16;
+  const int c = threadIdx.x & 15, q = threadIdx.x >> 4;
+  const int64_t j = min(j0 + c, a.d - 1);
+  A dg = 0, db = 0;
+#pragma unroll 8
+  for (int64_t r = q; r < a.rows; r += G) {
+    const A w = (A)static_cast<const T*>(a.dy)[r * a.lddy + j];
+    const A xh = ((A)static_cast<const T*>(a.x)[r * a.ldx + j] - static_cast<const A*>(a.mean)[r]) *
+                 static_cast<const A*>(a.rstd)[r];
+    dg += w * xh;
+    db += w;
+  }
+  sums[threadIdx.x] = dg;
+  sums[NT + threadIdx.x] = db;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;                  // 16 columns of the one, 16 of the other
+  A v = 0;
+  for (int i = 0; i < G; ++i) v += sums[(q ? NT : 0) + 16 * i + c];
+  W* out = static_cast<W*>(q ? a.dbeta : a.dgamma);
+  if (out && j0 + c < a.d) out[j0 + c] = (W)v;
+}
+
 // dx and the column sums in one pass over x and dy, rows in registers as in
 // norm_reg_kernel: workgroup b takes rows b, b + gridDim.x, .. (RPB at a time),
 // keeps its threads' columns of the two sums in registers, adds its RPB row
 // groups in LDS and writes partial[b]. The next rows' loads are in flight
 // during the current ones' sums.
-template <typename T, typename W, int TPR, int NV>
-__global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBackArgs a) {
+// ONE: a single launch for few rows, whose time is launches: the first rowblocks
+// workgroups form dx alone, the others the sums over all rows of 16 columns each,
+// which need no more than the given mean and rstd.
+template <typename T, typename W, int TPR, int NV, bool ONE>
+__global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBackArgs a, int rowblocks) {
   typedef typename acc_of<T>::type A;
   constexpr int VEC = vec_of<T>(), RPB = threads_of(TPR) / TPR;
   __shared__ A red[2][2 * (threads_of(TPR) / 64)];
-  __shared__ A sums[RPB > 1 ? TPR * NV * VEC : 1];
+  __shared__ A sums[ONE ? 2 * threads_of(TPR) : RPB > 1 ? TPR * NV * VEC : 1];
+  if constexpr (ONE) {
+    if ((int)blockIdx.x >= rowblocks) {
+      sum_columns<T, W, threads_of(TPR)>(a, (int64_t)((int)blockIdx.x - rowblocks) * 16, sums);
+      return;
+    }
+  }
   int slot = 0;
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
   A g[NV][VEC], dg[NV][VEC], db[NV][VEC], x[NV][VEC], w[NV][VEC];
@@ -402,7 +438,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBack
     for (int i = 0; i < NV; ++i)
       load_n(static_cast<const W*>(a.gamma) + Place<VEC>((t + i * TPR) * VEC, d).at, g[i]);
   }
-  const int64_t step = (int64_t)gridDim.x * RPB;
+  const int64_t step = (int64_t)rowblocks * RPB;
   T nx[NV][VEC], nd[NV][VEC];                     // the next row, as it comes
   A nmu, nrs;
   const auto next = [&](int64_t r) {
@@ -440,8 +476,10 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBack
     for (int i = 0; i < NV; ++i) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        dg[i][e] += w[i][e] * x[i][e];
-        db[i][e] += w[i][e];
+        if constexpr (!ONE) {
+          dg[i][e] += w[i][e] * x[i][e];
+          db[i][e] += w[i][e];
+        }
         w[i][e] *= g[i][e];
         s1 += w[i][e];
         s2 += w[i][e] * x[i][e];
@@ -462,7 +500,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_back_reg_kernel(NormBack
       }
     }
   }
-  if (!a.dgamma && !a.dbeta) return;
+  if (ONE || (!a.dgamma && !a.dbeta)) return;
   A* p = static_cast<A*>(a.partial) + (int64_t)blockIdx.x * 2 * a.d;
   const auto write = [&](A (&v)[NV][VEC], A* out) {
     if constexpr (RPB > 1) {
@@ -585,10 +623,25 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
   const int64_t parts = norm_partials(a.xtype, a.rows, a.d);
   const int64_t nv = a.d < vec_of<T>() ? INT32_MAX : ceil_div(a.d, vec_of<T>());
   const bool weights = a.dgamma || a.dbeta;
-#define KMP_NORM_CASE(TPR, NV)                                                                             \
-  if (nv <= TPR * NV) {                                                                                    \
-    hipLaunchKernelGGL((norm_back_reg_kernel<T, W, TPR, NV>), dim3((unsigned)parts),                       \
-                       dim3(threads_of(TPR)), 0, s, a);                                                    \
+  // One launch where that is what the call costs; us of the kernels in one and in
+  // two launches: 4 x 1024 in 16 bits 2.6 / 6.9, 300 x 512 4.4 / 8.1, 500 x 4096 8.8 /
+  // 15.0, 200 x 8192 in 32 bits 10.8 / 15.6, 1003 x 1999 14.0 / 12.9, but 1000 x 4096
+  // in 16 bits 21.8 / 17.2, 2000 x 512 12.4 / 10.7 (and 3 us of launch on the host).
+  const int64_t size = a.rows * a.d * (int64_t)sizeof(T);
+  const bool one = weights && a.rows > 0 && nv <= (sizeof(T) >= 4 ? 2048 : 1024) &&
+                   (a.rows <= 512 ? size <= 8 << 20 : a.rows <= 2048 && size <= 4 << 20);
+  const auto blocks = [&](int rpb) {              // of rows; with one launch 16 columns each beside them
+    return one ? (a.dx ? (int)std::min<int64_t>(ceil_div(a.rows, rpb), 1024) : 0) : (int)parts;
+  };
+  const auto launch = [&](auto kernel, int rowblocks, int threads) {
+    const int64_t grid = rowblocks + (one ? ceil_div(a.d, 16) : 0);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(threads), 0, s, a, rowblocks);
+  };
+#define KMP_NORM_CASE(TPR, NV)                                                                       \
+  if (nv <= TPR * NV) {                                                                              \
+    const int rpb = threads_of(TPR) / TPR;                                                           \
+    if (one) launch(norm_back_reg_kernel<T, W, TPR, NV, true>, blocks(rpb), threads_of(TPR));        \
+    else launch(norm_back_reg_kernel<T, W, TPR, NV, false>, blocks(rpb), threads_of(TPR));           \
   } else
   if (a.rows > 0) {
     KMP_NORM_CASE(32, 1)
@@ -598,10 +651,8 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
     KMP_NORM_CASE(256, 2)
     KMP_NORM_CASE(1024, 1)
     // (two vectors of eight elements need more registers than 1024 threads have)
-    if (sizeof(T) >= 4 && nv <= 2048) {
-      hipLaunchKernelGGL((norm_back_reg_kernel<T, W, 1024, sizeof(T) >= 4 ? 2 : 1>), dim3((unsigned)parts),
-                         dim3(1024), 0, s, a);
-    } else {                                      // x and dy are read again for the weights
+    KMP_NORM_CASE(1024, (sizeof(T) >= 4 ? 2 : 1))
+    {                                             // x and dy are read again for the weights
       if (a.dx)
         hipLaunchKernelGGL((norm_back_row_kernel<T, W>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
                            dim3(BIG), 0, s, a);
@@ -612,7 +663,7 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
     KMP_LAUNCH_CHECK();
   }
 #undef KMP_NORM_CASE
-  if (!weights) return 0;
+  if (!weights || one) return 0;
   hipLaunchKernelGGL((norm_back_join_kernel<A, W>), dim3((unsigned)ceil_div(a.d, 64), 2), dim3(1024), 0, s,
                      static_cast<const A*>(a.partial), a.rows > 0 ? parts : 0, a.d, static_cast<W*>(a.dgamma),
                      static_cast<W*>(a.dbeta));

@@ -118,12 +118,12 @@ def test_layer_norm_forward_and_backward(xt, wt):
         assert torch.equal(dx2, dx) and torch.equal(dg2, dg)
 
 
-@pytest.mark.parametrize("rows", [1, 31, 700, 5003])
+@pytest.mark.parametrize("rows", [1, 31, 700, 2049, 5003])
 def test_layer_norm_weight_gradients_over_many_rows(rows):
     """The reduction over rows: counts around its strips, the same bits again."""
     import torch
     from paper_2606_06742_amd import kmpath as km
-    for d in (96, 1000, 2500):
+    for d in (7, 96, 1000, 2500, 7001):
         announce(f"layer norm backward f32 {rows} x {d}")
         rng = np.random.default_rng(rows + d)
         x, xv, g, gv, b, bv = _norm_inputs(rng, rows, d, "f32", "f32", 0, 0)
