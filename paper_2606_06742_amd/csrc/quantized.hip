@@ -207,7 +207,7 @@ __device__ __forceinline__ void store_tile(const QProductArgs& a, const int16v (
 // slice, for products with few tiles, whose time is the chain of slices (0.2 to 0.3
 // us each); their sums are added in LDS. ALIGNED: rows start at multiples of 16
 // bytes and go from memory to LDS without registers; else through registers, which
-// hold the next slice while one is multiplied.
+// hold the next two slices while one is multiplied.
 template <typename O, int TM, int TN, int WR, int WC, int WK, int NS, bool ALIGNED>
 __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProductArgs a, int tm, int tn) {
   constexpr int NW = WR * WC, QA = TM / 8 / NW, QB = TN / 8 / NW;   // loads a wavefront, 8 rows each
@@ -236,19 +236,12 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
 #pragma unroll
     for (int q = 0; q < QB; ++q) load_to_lds(pb[q] + k + lc[q & 1], base + st * STAGE + TM * 128 + (wg * QB + q) * 1024);
   };
-  int4v ra[QA], rb[QB];
-  const auto pull = [&](int k) {                                    // a slice into registers, zeros past K
+  const auto push = [&](const int4v (&va)[QA], const int4v (&vb)[QB], int st) {
 #pragma unroll
-    for (int q = 0; q < QA; ++q) ra[q] = chunk16(pa[q], k + lc[q & 1], a.K);
-#pragma unroll
-    for (int q = 0; q < QB; ++q) rb[q] = chunk16(pb[q], k + lc[q & 1], a.K);
-  };
-  const auto push = [&](int st) {
-#pragma unroll
-    for (int q = 0; q < QA; ++q) *reinterpret_cast<int4v*>(ring + st * STAGE + (wg * QA + q) * 1024 + lane * 16) = ra[q];
+    for (int q = 0; q < QA; ++q) *reinterpret_cast<int4v*>(ring + st * STAGE + (wg * QA + q) * 1024 + lane * 16) = va[q];
 #pragma unroll
     for (int q = 0; q < QB; ++q)
-      *reinterpret_cast<int4v*>(ring + st * STAGE + TM * 128 + (wg * QB + q) * 1024 + lane * 16) = rb[q];
+      *reinterpret_cast<int4v*>(ring + st * STAGE + TM * 128 + (wg * QB + q) * 1024 + lane * 16) = vb[q];
   };
   int16v acc[MB][NB] = {};
   const int row = lane & 31, half = lane >> 5;
@@ -270,12 +263,12 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
     }
   };
   const int whole = (int)a.K / 128, tail = (int)a.K % 128;
+  const int rounds = (whole + WK - 1) / WK, mine = (whole - kg + WK - 1) / WK;       // slices kg, kg + WK, ..
   if constexpr (ALIGNED) {
     // slice s of a group goes to slot s % NS; it is read once the loads up to it
     // have landed and every wavefront is there, which frees the slot of s - 1 for
     // s + NS - 1
     constexpr int LEFT = (NS - 2) * (QA + QB);
-    const int rounds = (whole + WK - 1) / WK, mine = (whole - kg + WK - 1) / WK;   // slices kg, kg + WK, ..
     for (int s = 0; s < min(NS - 1, mine); ++s) fetch((s * WK + kg) * 128, s);
     int slot = 0;
     for (int s = 0; s < rounds; ++s) {
@@ -286,25 +279,48 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void qproduct_tile_kernel(QProdu
       if (s < mine) multiply(slot);
       slot = slot + 1 == NS ? 0 : slot + 1;
     }
-    if (tail > 0) {
-      __syncthreads();
-      if (kg == WK - 1) {
-        pull(whole * 128);
-        push(0);
+  } else if (rounds > 0) {
+    static_assert(ALIGNED || NS == 2, "two slices on their way, two stages");
+    int4v ra[2][QA], rb[2][QB];
+    const auto pull = [&](int s, int p) {                           // past the end: the last slice again, unused
+      const int k = min(s * WK + kg, whole - 1) * 128;
+#pragma unroll
+      for (int q = 0; q < QA; ++q) __builtin_memcpy(&ra[p][q], pa[q] + k + lc[q & 1], 16);
+#pragma unroll
+      for (int q = 0; q < QB; ++q) __builtin_memcpy(&rb[p][q], pb[q] + k + lc[q & 1], 16);
+    };
+    pull(0, 0);
+    pull(1, 1);
+    int s = 0;
+    for (; s + 2 < rounds; s += 2) {                                // (the stages alternate: one barrier each)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        push(ra[p], rb[p], p);
+        __syncthreads();
+        pull(s + p + 2, p);
+        multiply(p);
       }
-      __syncthreads();
-      if (kg == WK - 1) multiply(0);
     }
-  } else {
-    static_assert(ALIGNED || WK == 1, "one group of wavefronts where rows are not aligned");
-    const int slices = whole + (tail > 0);
-    if (slices > 0) pull(0);
-    for (int s = 0; s < slices; ++s) {                              // (the stages alternate: one barrier each)
-      push(s & 1);
-      __syncthreads();
-      if (s + 1 < slices) pull((s + 1) * 128);
-      multiply(s & 1);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+      if (s + p < rounds) {
+        push(ra[p], rb[p], p);
+        __syncthreads();
+        if (s + p < mine) multiply(p);
+      }
+  }
+  if (tail > 0) {                                                   // the rest of k, zeros past its end
+    __syncthreads();
+    if (kg == WK - 1) {
+      int4v va[QA], vb[QB];
+#pragma unroll
+      for (int q = 0; q < QA; ++q) va[q] = chunk16(pa[q], whole * 128 + lc[q & 1], a.K);
+#pragma unroll
+      for (int q = 0; q < QB; ++q) vb[q] = chunk16(pb[q], whole * 128 + lc[q & 1], a.K);
+      push(va, vb, 0);
     }
+    __syncthreads();
+    if (kg == WK - 1) multiply(0);
   }
   __syncthreads();                                                  // the ring is free
   if constexpr (WK > 1) {                                           // the first group adds the others' sums
@@ -459,25 +475,49 @@ int ahead_as(hipStream_t s, const QProductArgs& a) {
 // Which form, by what keeps the chip's 256 compute units busy. us per launch at M x
 // N x K, w from HBM: few tokens; tiles of 32 x 64 (four groups over k, ring of 3), 64
 // x 64 (two groups, ring of 3, or of 2 and so two workgroups a compute unit); operands
-// ahead in tiles of 128 and 256; 64 and 128 unaligned (64u, 128u); the floor, the
-// larger of the bytes at a copy's 4.82 TB/s and the products at the 2040 TOP/s of the
-// library's 8-bit product of order 8192:
-//                      few  32x64  64,3  64,2   128   256   64u  128u  floor
-//   1 x 4096 x 4096    6.0   7.5   9.7  12.0  20.9  48.7  34.2  61.4   3.5
-//   16 x 8192 x 4096  11.6  10.4  11.4  16.6  30.0  51.2  41.2  65.6   7.0
-//   16 x 32000 x 2048 21.2  18.2  18.5  15.6  20.3  30.4  24.4  36.3  13.8
-//   64 x 1000 x 8192        11.8  15.8  21.6  39.6  91.8  64.8   118   1.8
-//   64 x 4096 x 4096         8.1  10.1  12.9  22.2  49.2  34.4  61.6   3.6
-//   128 x 4096 x 4096        8.7  10.7  12.8  23.4  50.2  34.3  62.5   3.8
-//   256 x 4096 x 4096       14.6  11.7  13.2  23.5  52.2  34.4  62.4   4.2
-//   64 x 12288 x 4096       20.8  16.5  19.8  32.3  52.6  43.0  67.4  10.8
-//   64 x 32000 x 2048       27.5  21.3  18.0  21.2  31.4  25.8  37.5  14.5
-//   512 x 4096 x 4096       27.0  19.6  16.6  24.0  52.0  36.6  62.4   8.4
-//   2048 x 2048 x 2048      35.9  24.6  18.4  16.6  31.7  26.2  35.8   8.4
-//   1024 x 8192 x 4096       132    89    74  45.6  60.5  94.3  74.3  33.7
-//   3000 x 5000 x 1000       159    83    63  36.4  32.6  55.2  51.5  14.7
-//   4096 x 4096 x 4096       224   169   135  87.0  71.0   184   145  67.4
-//   4096 x 16384 x 4096      850   632   534   364   293   672   534   269
+// ahead in tiles of 128 and 256; the floor, the larger of the bytes at a copy's 4.82
+// TB/s and the products at the 2040 TOP/s of the library's 8-bit product of order 8192:
+//                      few  32x64  64,3  64,2   128   256  floor
+//   1 x 4096 x 4096    6.0   7.5   9.7  12.0  20.9  48.7   3.5
+//   16 x 8192 x 4096  11.6  10.4  11.4  16.6  30.0  51.2   7.0
+//   16 x 32000 x 2048 21.2  18.2  18.5  15.6  20.3  30.4  13.8
+//   64 x 1000 x 8192        11.8  15.8  21.6  39.6  91.8   1.8
+//   64 x 4096 x 4096         8.1  10.1  12.9  22.2  49.2   3.6
+//   128 x 4096 x 4096        8.7  10.7  12.8  23.4  50.2   3.8
+//   256 x 4096 x 4096       14.6  11.7  13.2  23.5  52.2   4.2
+//   64 x 12288 x 4096       20.8  16.5  19.8  32.3  52.6  10.8
+//   64 x 32000 x 2048       27.5  21.3  18.0  21.2  31.4  14.5
+//   512 x 4096 x 4096       27.0  19.6  16.6  24.0  52.0   8.4
+//   2048 x 2048 x 2048      35.9  24.6  18.4  16.6  31.7   8.4
+//   1024 x 8192 x 4096       132    89    74  45.6  60.5  33.7
+//   3000 x 5000 x 1000       159    83    63  36.4  32.6  14.7
+//   4096 x 4096 x 4096       224   169   135  87.0  71.0  67.4
+//   4096 x 16384 x 4096      850   632   534   364   293   269
+// Between 512 and 768 tiles of 64 those of 128 leave compute units idle: one group a
+// tile of 64 and a ring of 2, up to five workgroups a compute unit (64,1; here and
+// below in a recorded graph, 1 to 2 us more a launch):
+//                       64,2  64,1   128  floor
+//   600 x 4500 x 700    13.0   9.9  11.0   1.9
+//   1500 x 1500 x 1500  17.3  12.7  14.5   3.3
+//   1244 x 1824 x 10909 74.2  61.7  84.4  24.3
+//   1000 x 3000 x 4096  34.1  28.7  32.5  12.0
+//   768 x 4096 x 8192   51.1  50.6  59.5  25.3
+//   1024 x 3584 x 4096  35.2  34.2  32.6  14.7
+//   2048 x 2048 x 2048  18.3  18.8  16.0   8.4
+// Rows that are not aligned: few tokens; tiles of 32 x 64 (four groups), 64 and 128
+// (one; 128 with eight wavefronts, with four 97 for 87 at 1244 x 1824 x 10909):
+//                        few  32x64    64   128  floor
+//   16 x 4096 x 4097    17.3   17.6  21.6  38.1   3.5
+//   7 x 6245 x 9579     42.7   38.9  47.5  87.5  12.4
+//   16 x 32000 x 2047   60.5   21.7  20.1  20.6  13.8
+//   64 x 1000 x 8191           24.6  28.4  54.7   1.8
+//   128 x 4096 x 4097          17.1  21.8  40.6   3.8
+//   512 x 4096 x 4097          61.5  36.1  37.1   8.4
+//   957 x 5082 x 1874          79.9  31.1  28.3   8.9
+//   1244 x 1824 x 10909         155   110  86.2  24.3
+//   4426 x 1994 x 543           107  27.4  25.2   4.7
+//   3000 x 5000 x 1001          189  63.2  42.4  14.7
+//   4096 x 4096 x 4097          425   213   134  67.4
 template <typename O>
 int product_as(hipStream_t s, const QProductArgs& a) {
   const auto tiles = [&](int tm, int tn) { return ceil_div(a.M, tm) * ceil_div(a.N, tn); };
@@ -486,12 +526,15 @@ int product_as(hipStream_t s, const QProductArgs& a) {
     KMP_LAUNCH_CHECK();
     return 0;
   }
-  if (!aligned_rows(a))
-    return tiles(64, 64) <= 1024 ? tiles_as<O, 64, 64, 2, 2, 1, 2, false>(s, a)
-                                 : tiles_as<O, 128, 128, 2, 2, 1, 2, false>(s, a);
+  if (!aligned_rows(a)) {
+    if (tiles(32, 64) <= 256) return tiles_as<O, 32, 64, 1, 2, 4, 2, false>(s, a);
+    if (tiles(64, 64) <= 512) return tiles_as<O, 64, 64, 2, 2, 1, 2, false>(s, a);
+    return tiles_as<O, 128, 128, 2, 4, 1, 2, false>(s, a);
+  }
   if (tiles(32, 64) <= 256) return tiles_as<O, 32, 64, 1, 2, 4, 3, true>(s, a);
   if (tiles(64, 64) <= 256) return tiles_as<O, 64, 64, 2, 2, 2, 3, true>(s, a);
   if (tiles(64, 64) <= 512) return tiles_as<O, 64, 64, 2, 2, 2, 2, true>(s, a);
+  if (tiles(64, 64) <= 768) return tiles_as<O, 64, 64, 2, 2, 1, 2, true>(s, a);
   if (tiles(256, 256) < 192) return ahead_as<O, 128, 128, 2, 4>(s, a);
   return ahead_as<O, 256, 256, 2, 4>(s, a);
 }

@@ -305,6 +305,28 @@ def test_quantized_product(ot, pad, off):
         assert np.all(np.abs(_np(out) - want) <= bound + uo * (np.abs(want) + bound) + TINY[ot]), (M, N, K)
 
 
+# between the forms' sizes: many tiles of each, slices of 128 bytes from none to more
+# than are on their way, with and without a rest
+@pytest.mark.parametrize("pad", [0, 1, 16], ids=["packed", "odd", "aligned"])
+@pytest.mark.parametrize("M,N", [(33, 70), (40, 8200), (1500, 1500), (1700, 1750)])
+def test_quantized_product_slices(M, N, pad):
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    for K in (5, 127, 128, 130, 256, 300, 384, 515, 640, 777, 1024, 1153, 1290):
+        announce(f"quantized product {M} x {N} x {K} gap {pad}")
+        g = torch.Generator().manual_seed(M + N + K)
+        x, w = (torch.randint(-128, 128, (r, K), dtype=torch.int8, generator=g) for r in (M, N))
+        ld = K + (-K % 16 if pad == 16 else pad)
+        xq, wq = (torch.full((r, ld), 77, dtype=torch.int8, device=device())[:, :K] for r in (M, N))
+        xq.copy_(x)
+        wq.copy_(w)
+        out = torch.empty(M, N, device=device())
+        km.kmp_quantized_product(xq, torch.ones(M, device=device()), wq, torch.ones(N, device=device()), out)
+        # below 2^24 in magnitude nearly always; one rounding to 32 bits otherwise
+        want = (x.double() @ w.double().T).float()
+        assert torch.equal(out.cpu(), want), (M, N, K)
+
+
 def test_quantized_product_largest_sums_and_rows():
     """The largest sum that is allowed; NaN scales stay in their row or column."""
     import torch
