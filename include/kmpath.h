@@ -377,9 +377,9 @@ int kmp_layer_norm_backward(void* stream, int32_t xtype, const void* dy, int64_t
 
 /* Rows of x (DEVICE, rows x d; KMP_F32, KMP_BF16 or KMP_F16) in 8 bits:
  * q = rint(x f), f = (1 / a) 127, scale = a / 127, a the row's largest |x|, every
- * operation rounded to 32 bits (DEVICE, q rows x d, scale [rows]). A zero row has q = 0 and scale 0; a row with a
- * NaN or an infinity q = 0 and scale NaN, so that products with it are NaN and
- * other rows are not touched.                                               */
+ * operation rounded to 32 bits (DEVICE, q rows x d, scale [rows]). A zero row
+ * has q = 0 and scale 0; a row with a NaN or an infinity q = 0 and scale NaN, so
+ * that products with it are NaN and other rows are not touched.             */
 int kmp_quantize_rows(void* stream, int32_t xtype, const void* x, int64_t rows, int64_t d, int64_t ldx,
                       int8_t* q, int64_t ldq, float* scale);
 
