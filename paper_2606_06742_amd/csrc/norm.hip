@@ -337,14 +337,49 @@ __global__ __launch_bounds__(threads_of(TPR)) void norm_reg_kernel(NormArgs a) {
   }
 }
 
+// dgamma and dbeta of columns j0 .. j0 + 15 over all rows by a workgroup of NT
+// threads: 16 columns beside each other, every NT / 16-th row, then the row groups
+// in order. `sums` holds 2 NT values.
+template <typename T, typename W, int NT, typename A>
+__device__ __forceinline__ void sum_columns(const NormBackArgs& a, int64_t j0, A* sums) {
+  constexpr int G = NT / 16;
+  const int c = threadIdx.x & 15, q = threadIdx.x >> 4;
+  const int64_t j = min(j0 + c, a.d - 1);
+  A dg = 0, db = 0;
+#pragma unroll 8
+  for (int64_t r = q; r < a.rows; r += G) {
+    const A w = (A)static_cast<const T*>(a.dy)[r * a.lddy + j];
+    const A xh = ((A)static_cast<const T*>(a.x)[r * a.ldx + j] - static_cast<const A*>(a.mean)[r]) *
+                 static_cast<const A*>(a.rstd)[r];
+    dg += w * xh;
+    db += w;
+  }
+  sums[threadIdx.x] = dg;
+  sums[NT + threadIdx.x] = db;
+  __syncthreads();
+  if (threadIdx.x >= 32) return;                  // 16 columns of the one, 16 of the other
+  A v = 0;
+  for (int i = 0; i < G; ++i) v += sums[(q ? NT : 0) + 16 * i + c];
+  W* out = static_cast<W*>(q ? a.dbeta : a.dgamma);
+  if (out && j0 + c < a.d) out[j0 + c] = (W)v;
+}
+
 // dx of one row per workgroup, any length: a pass for the two means, one to write.
-template <typename T, typename W>
-__global__ __launch_bounds__(BIG) void norm_back_row_kernel(NormBackArgs a) {
+// ONE: as in norm_back_reg_kernel.
+template <typename T, typename W, bool ONE>
+__global__ __launch_bounds__(BIG) void norm_back_row_kernel(NormBackArgs a, int rowblocks) {
   typedef typename acc_of<T>::type A;
   constexpr int VEC = vec_of<T>();
   __shared__ A red[BIG / 64];
+  if constexpr (ONE) {
+    __shared__ A sums[2 * BIG];
+    if ((int)blockIdx.x >= rowblocks) {
+      sum_columns<T, W, BIG>(a, (int64_t)((int)blockIdx.x - rowblocks) * 16, sums);
+      return;
+    }
+  }
   const W* gamma = static_cast<const W*>(a.gamma);
-  for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
+  for (int64_t r = blockIdx.x; r < a.rows; r += rowblocks) {
     const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
     const A mu = static_cast<const A*>(a.mean)[r], rs = static_cast<const A*>(a.rstd)[r];
@@ -377,33 +412,6 @@ __global__ __launch_bounds__(BIG) void norm_back_row_kernel(NormBackArgs a) {
       store_n(dx + j, w);
     });
   }
-}
-
-// dgamma and dbeta of columns j0 .. j0 + 15 over all rows by a workgroup of NT
-// threads: 16 columns beside each other, every NT / 16-th row, then the row groups
-// in order. `sums` holds 2 NT values.
-template <typename T, typename W, int NT, typename A>
-__device__ __forceinline__ void sum_columns(const NormBackArgs& a, int64_t j0, A* sums) {
-  constexpr int G = NT / 16;
-  const int c = threadIdx.x & 15, q = threadIdx.x >> 4;
-  const int64_t j = min(j0 + c, a.d - 1);
-  A dg = 0, db = 0;
-#pragma unroll 8
-  for (int64_t r = q; r < a.rows; r += G) {
-    const A w = (A)static_cast<const T*>(a.dy)[r * a.lddy + j];
-    const A xh = ((A)static_cast<const T*>(a.x)[r * a.ldx + j] - static_cast<const A*>(a.mean)[r]) *
-                 static_cast<const A*>(a.rstd)[r];
-    dg += w * xh;
-    db += w;
-  }
-  sums[threadIdx.x] = dg;
-  sums[NT + threadIdx.x] = db;
-  __syncthreads();
-  if (threadIdx.x >= 32) return;                  // 16 columns of the one, 16 of the other
-  A v = 0;
-  for (int i = 0; i < G; ++i) v += sums[(q ? NT : 0) + 16 * i + c];
-  W* out = static_cast<W*>(q ? a.dbeta : a.dgamma);
-  if (out && j0 + c < a.d) out[j0 + c] = (W)v;
 }
 
 // dx and the column sums in one pass over x and dy, rows in registers as in
@@ -626,9 +634,11 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
   // One launch where that is what the call costs; us of the kernels in one and in
   // two launches: 4 x 1024 in 16 bits 2.6 / 6.9, 300 x 512 4.4 / 8.1, 500 x 4096 8.8 /
   // 15.0, 200 x 8192 in 32 bits 10.8 / 15.6, 1003 x 1999 14.0 / 12.9, but 1000 x 4096
-  // in 16 bits 21.8 / 17.2, 2000 x 512 12.4 / 10.7 (and 3 us of launch on the host).
+  // in 16 bits 21.8 / 17.2, 2000 x 512 12.4 / 10.7 (and 3 us of launch on the host). Rows
+  // too long for the registers, in one and in three: 4 x 13134 in 16 bits 6.0 / 10.0,
+  // 116 x 14770 10.1 / 17.9, 250 x 16384 19.6 / 23.7, 100 x 16384 in 32 bits 10.1 / 18.2.
   const int64_t size = a.rows * a.d * (int64_t)sizeof(T);
-  const bool one = weights && a.rows > 0 && nv <= (sizeof(T) >= 4 ? 2048 : 1024) &&
+  const bool one = weights && a.rows > 0 &&
                    (a.rows <= 512 ? size <= 8 << 20 : a.rows <= 2048 && size <= 4 << 20);
   const auto blocks = [&](int rpb) {              // of rows; with one launch 16 columns each beside them
     return one ? (a.dx ? (int)std::min<int64_t>(ceil_div(a.rows, rpb), 1024) : 0) : (int)parts;
@@ -649,14 +659,18 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
     KMP_NORM_CASE(64, 2)
     KMP_NORM_CASE(256, 1)
     KMP_NORM_CASE(256, 2)
-    KMP_NORM_CASE(1024, 1)
+    // 512 threads with two vectors each take rows that 1024 threads with one were
+    // slower on (8038 x 4228 in 16 bits 56 / 64 us, 8192 x 8192 87 / 94, 3000 x 4096 in
+    // 32 bits 30 / 33)
+    KMP_NORM_CASE(512, 2)
     // (two vectors of eight elements need more registers than 1024 threads have)
-    KMP_NORM_CASE(1024, (sizeof(T) >= 4 ? 2 : 1))
+    KMP_NORM_CASE((sizeof(T) >= 4 ? 1024 : 512), 2)
     {                                             // x and dy are read again for the weights
-      if (a.dx)
-        hipLaunchKernelGGL((norm_back_row_kernel<T, W>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)),
-                           dim3(BIG), 0, s, a);
-      if (weights)
+      if (one)
+        launch(norm_back_row_kernel<T, W, true>, blocks(1), BIG);
+      else if (a.dx)
+        launch(norm_back_row_kernel<T, W, false>, (int)std::min<int64_t>(a.rows, 1 << 20), BIG);
+      if (weights && !one)
         hipLaunchKernelGGL((norm_back_columns_kernel<T>), dim3((unsigned)ceil_div(a.d, BT), (unsigned)parts),
                            dim3(BT), 0, s, a, ceil_div(a.rows, parts));
     }

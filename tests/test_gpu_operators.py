@@ -144,6 +144,38 @@ def test_layer_norm_weight_gradients_over_many_rows(rows):
             assert np.all(np.abs(_np(got) - want) <= (rows + 16) * U["f32"] * size.sum(axis=0))
 
 
+# rows too long for registers and rows shorter than a vector, with the sums in a
+# launch beside dx and in passes of their own
+@pytest.mark.parametrize("xt,rows,d", [("f32", 40, 9001), ("f32", 300, 16500), ("bf16", 60, 16391), ("bf16", 600, 8200),
+                                       ("f16", 300, 17000), ("f32", 2500, 3), ("f32", 1000, 3), ("bf16", 3000, 7)])
+def test_layer_norm_gradients_of_long_and_tiny_rows(xt, rows, d):
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    announce(f"layer norm backward {xt} {rows} x {d}")
+    u, uo = U["f32"], U[xt]
+    rng = np.random.default_rng(rows + d)
+    x, xv, g, gv, b, _ = _norm_inputs(rng, rows, d, xt, "f32", 3, 1)
+    dy, dyv = _put(rng.standard_normal((rows, d)) + 0.1, _dtype(xt), 1, 0)
+    _, me, re = OO.layer_norm(xv, gv, 0 * gv, EPS)
+    mean, rstd = (torch.as_tensor(v, device=device()).float() for v in (me, re))
+    mk, rk = _np(mean), _np(rstd)
+    ws = torch.empty(km.kmp_layer_norm_workspace_bytes(rows, d, _dtype(xt)), dtype=torch.uint8, device=device())
+    ws.fill_(255)                                # NaN: every partial sum is written before it is read
+    dx, _ = _put(np.zeros((rows, d)), _dtype(xt), 2, 1)
+    dg, db = torch.empty_like(g), torch.empty_like(b)
+    km.kmp_layer_norm_backward(dy, x, g, mean, rstd, dx, dg, db, ws)
+    dxe, dge, dbe = OO.layer_norm_backward(dyv, xv, gv, mk, rk)
+    xh, w, c = np.abs((xv - mk[:, None]) * rk[:, None]), np.abs(dyv * gv), d / 64 + 16
+    bound = u * rk[:, None] * ((c + 16) * (w.mean(axis=1)[:, None] + 2 * xh * (w * xh).mean(axis=1)[:, None]) + 8 * w)
+    assert np.all(np.abs(_np(dx) - dxe) <= bound + (uo if uo != u else 0) * (np.abs(dxe) + bound) + 2 * u * np.abs(dxe) + TINY[xt])
+    for got, want, size in ((dg, dge, np.abs(dyv) * xh), (db, dbe, np.abs(dyv))):
+        assert np.all(np.abs(_np(got) - want) <= (rows + 16) * u * size.sum(axis=0) + TINY["f32"])
+    dx2, dg2 = torch.empty(rows, d, dtype=x.dtype, device=device()), torch.empty_like(g)
+    km.kmp_layer_norm_backward(dy, x, g, mean, rstd, dx2, None, None, None)
+    km.kmp_layer_norm_backward(dy, x, g, mean, rstd, None, dg2, None, ws)
+    assert torch.equal(dx2, dx) and torch.equal(dg2, dg)
+
+
 def test_layer_norm_gradient_against_differences():
     """64-bit rows: the backward against central differences of the forward.
     Step 1e-4: error 1e-8 times third derivatives (tens), rounding 1e-12."""
