@@ -633,13 +633,13 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
   const bool weights = a.dgamma || a.dbeta;
   // One launch where that is what the call costs; us of the kernels in one and in
   // two launches: 4 x 1024 in 16 bits 2.6 / 6.9, 300 x 512 4.4 / 8.1, 500 x 4096 8.8 /
-  // 15.0, 200 x 8192 in 32 bits 10.8 / 15.6, 1003 x 1999 14.0 / 12.9, but 1000 x 4096
+  // 15.0, 200 x 8192 in 32 bits 9.1 / 15.6, 1003 x 1999 14.0 / 12.9, but 1000 x 4096
   // in 16 bits 21.8 / 17.2, 2000 x 512 12.4 / 10.7 (and 3 us of launch on the host). Rows
   // too long for the registers, in one and in three: 4 x 13134 in 16 bits 6.0 / 10.0,
   // 116 x 14770 10.1 / 17.9, 250 x 16384 19.6 / 23.7, 100 x 16384 in 32 bits 10.1 / 18.2.
   const int64_t size = a.rows * a.d * (int64_t)sizeof(T);
-  const bool one = weights && a.rows > 0 &&
-                   (a.rows <= 512 ? size <= 8 << 20 : a.rows <= 2048 && size <= 4 << 20);
+  const bool small = a.rows <= 512 ? size <= 8 << 20 : a.rows <= 2048 && size <= 4 << 20;
+  const bool one = weights && a.rows > 0 && small;
   const auto blocks = [&](int rpb) {              // of rows; with one launch 16 columns each beside them
     return one ? (a.dx ? (int)std::min<int64_t>(ceil_div(a.rows, rpb), 1024) : 0) : (int)parts;
   };
@@ -663,14 +663,20 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
     // slower on (8038 x 4228 in 16 bits 56 / 64 us, 8192 x 8192 87 / 94, 3000 x 4096 in
     // 32 bits 30 / 33)
     KMP_NORM_CASE(512, 2)
-    // (two vectors of eight elements need more registers than 1024 threads have)
-    KMP_NORM_CASE((sizeof(T) >= 4 ? 1024 : 512), 2)
-    {                                             // x and dy are read again for the weights
-      if (one)
-        launch(norm_back_row_kernel<T, W, true>, blocks(1), BIG);
-      else if (a.dx)
+    // Longer rows in one launch without registers (with four vectors in them 116 x
+    // 14770 in 16 bits 12.8 / 10.1 us, 250 x 16384 24.4 / 19.6). Else four vectors
+    // against the passes for any length: 2000 x 16384 in 16 bits 79 / 97, 4000 x 9000
+    // 97 / 109, 8000 x 16384 227 / 306, though 36 registers are spilled; eight vectors
+    // of 32-bit elements spill 169, 2000 x 16384 226 / 158. (The choice is the same
+    // without the weights, so that dx has the same bits.)
+    if (one) {
+      launch(norm_back_row_kernel<T, W, true>, blocks(1), BIG);
+    } else if (nv <= 2048 && !small) {
+      launch(norm_back_reg_kernel<T, W, 512, 4, false>, blocks(1), 512);
+    } else {                                      // x and dy are read again for the weights
+      if (a.dx)
         launch(norm_back_row_kernel<T, W, false>, (int)std::min<int64_t>(a.rows, 1 << 20), BIG);
-      if (weights && !one)
+      if (weights)
         hipLaunchKernelGGL((norm_back_columns_kernel<T>), dim3((unsigned)ceil_div(a.d, BT), (unsigned)parts),
                            dim3(BT), 0, s, a, ceil_div(a.rows, parts));
     }
