@@ -467,9 +467,9 @@ template <typename O, int TM, int TN, int WR, int WC, int WK, int NS, bool ALIGN
 int tiles_as(hipStream_t s, const QProductArgs& a) {
   return launch_tiles<TM, TN>(s, a, qproduct_tile_kernel<O, TM, TN, WR, WC, WK, NS, ALIGNED>, 64 * WR * WC * WK);
 }
-template <typename O, int TM, int TN, int WR, int WC>
+template <typename O, int TM, int TN, int WR, int WC, int NS>
 int ahead_as(hipStream_t s, const QProductArgs& a) {
-  return launch_tiles<TM, TN>(s, a, qproduct_ahead_kernel<O, TM, TN, WR, WC, 2>, 64 * WR * WC);
+  return launch_tiles<TM, TN>(s, a, qproduct_ahead_kernel<O, TM, TN, WR, WC, NS>, 64 * WR * WC);
 }
 
 // Which form, by what keeps the chip's 256 compute units busy. us per launch at M x
@@ -504,6 +504,19 @@ int ahead_as(hipStream_t s, const QProductArgs& a) {
 //   768 x 4096 x 8192   51.1  50.6  59.5  25.3
 //   1024 x 3584 x 4096  35.2  34.2  32.6  14.7
 //   2048 x 2048 x 2048  18.3  18.8  16.0   8.4
+// Up to 256 tiles of 128 have a compute unit each and room for a ring of 4 there,
+// which hides more of the loads than a ring of 2 (128,4; in a recorded graph, both
+// sides in turn):
+//                       64,1   128  128,4
+//   600 x 4500 x 700    10.7         11.4
+//   1500 x 1500 x 1500  13.9         14.4
+//   1244 x 1824 x 10909 63.6         48.4
+//   4138 x 534 x 7988   44.9         39.0
+//   1000 x 3000 x 4096  24.9         23.7
+//   768 x 4096 x 8192   44.1         39.3
+//   1024 x 3584 x 4096        26.7   23.9
+//   2000 x 2000 x 8192        47.6   43.5
+//   2048 x 2048 x 2048        17.1   16.1
 // Rows that are not aligned: few tokens; tiles of 32 x 64 (four groups), 64 and 128
 // (one; 128 with eight wavefronts, with four 97 for 87 at 1244 x 1824 x 10909):
 //                        few  32x64    64   128  floor
@@ -534,9 +547,10 @@ int product_as(hipStream_t s, const QProductArgs& a) {
   if (tiles(32, 64) <= 256) return tiles_as<O, 32, 64, 1, 2, 4, 3, true>(s, a);
   if (tiles(64, 64) <= 256) return tiles_as<O, 64, 64, 2, 2, 2, 3, true>(s, a);
   if (tiles(64, 64) <= 512) return tiles_as<O, 64, 64, 2, 2, 2, 2, true>(s, a);
-  if (tiles(64, 64) <= 768) return tiles_as<O, 64, 64, 2, 2, 1, 2, true>(s, a);
-  if (tiles(256, 256) < 192) return ahead_as<O, 128, 128, 2, 4>(s, a);
-  return ahead_as<O, 256, 256, 2, 4>(s, a);
+  if (tiles(64, 64) <= 768 && (a.K < 2048 || tiles(128, 128) > 256)) return tiles_as<O, 64, 64, 2, 2, 1, 2, true>(s, a);
+  if (tiles(128, 128) <= 256) return ahead_as<O, 128, 128, 2, 4, 4>(s, a);
+  if (tiles(256, 256) < 192) return ahead_as<O, 128, 128, 2, 4, 2>(s, a);
+  return ahead_as<O, 256, 256, 2, 4, 2>(s, a);
 }
 
 }  // namespace

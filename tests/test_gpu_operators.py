@@ -359,6 +359,26 @@ def test_quantized_product_slices(M, N, pad):
         assert torch.equal(out.cpu(), want), (M, N, K)
 
 
+# a tile of 128 for each compute unit at most: a ring of four slices, from none to
+# more than it holds
+@pytest.mark.parametrize("M,N,Ks", [(1900, 2000, (5, 128, 129, 250, 384, 400, 512, 530, 640, 777, 1025)),
+                                    (1300, 1450, (2048, 2177)), (100, 28000, (2048, 2200))])
+def test_quantized_product_slices_in_a_ring_of_four(M, N, Ks):
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    for K in Ks:
+        announce(f"quantized product {M} x {N} x {K}")
+        g = torch.Generator().manual_seed(M + N + K)
+        x, w = (torch.randint(-128, 128, (r, K), dtype=torch.int8, generator=g) for r in (M, N))
+        xq, wq = (torch.full((r, K + -K % 16), 77, dtype=torch.int8, device=device())[:, :K] for r in (M, N))
+        xq.copy_(x)
+        wq.copy_(w)
+        out = torch.empty(M, N, device=device())
+        km.kmp_quantized_product(xq, torch.ones(M, device=device()), wq, torch.ones(N, device=device()), out)
+        # the sums are whole numbers; one rounding to 32 bits
+        assert torch.equal(out.cpu(), (x.double() @ w.double().T).float()), (M, N, K)
+
+
 def test_quantized_product_largest_sums_and_rows():
     """The largest sum that is allowed; NaN scales stay in their row or column."""
     import torch
