@@ -454,7 +454,9 @@ int backward_as(hipStream_t s, const LogprobBackArgs& a) {
 
 size_t logprob_workspace(int64_t T, int64_t V, int top) {
   const int segs = split(T, V, 4).segs;           // 32 bits are split the most
-  if (segs == 1) return 256;
+  // 256 bytes where there is nothing to keep (no tokens, one segment a row), so that 0
+  // means an error
+  if (segs == 1 || T == 0) return 256;
   return (size_t)(round_up(T * segs * (int64_t)sizeof(Part), 16) + T * segs * top * (int64_t)sizeof(key_t));
 }
 
