@@ -398,7 +398,9 @@ int kmp_quantized_product(void* stream, const int8_t* x, int64_t ldx, const floa
 /* Most alternatives per token. */
 #define KMP_MAX_TOP 64
 
-/* Bytes of DEVICE workspace of kmp_token_logprobs; 0: bad arguments.        */
+/* Bytes of DEVICE workspace of kmp_token_logprobs (at least 256, under 1 MiB);
+ * 0: bad arguments. The size does not fall as T, V or top grows: the workspace of
+ * a program's largest call serves its smaller ones.                         */
 size_t kmp_token_logprobs_workspace_bytes(int64_t T, int64_t V, int32_t top);
 
 /* Log probabilities of given tokens under the rows of logits (DEVICE, T x V;

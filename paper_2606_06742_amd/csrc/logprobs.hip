@@ -452,12 +452,14 @@ int backward_as(hipStream_t s, const LogprobBackArgs& a) {
 
 }  // namespace
 
+// A bound on what split() takes at T, V (of 32-bit logits, which are split the most)
+// that never falls as T, V or top grows, so that the workspace of a program's largest
+// call serves its smaller ones: T * segs is at most 1024 and T times the segments of a
+// single row. 256 bytes where there is nothing to keep, so that 0 means an error.
 size_t logprob_workspace(int64_t T, int64_t V, int top) {
-  const int segs = split(T, V, 4).segs;           // 32 bits are split the most
-  // 256 bytes where there is nothing to keep (no tokens, one segment a row), so that 0
-  // means an error
-  if (segs == 1 || T == 0) return 256;
-  return (size_t)(round_up(T * segs * (int64_t)sizeof(Part), 16) + T * segs * top * (int64_t)sizeof(key_t));
+  if (V * 4 <= 65536) return 256;
+  const int64_t units = std::min<int64_t>(T * std::min<int64_t>(ceil_div(V, 4096), kMaxSegs), 1024);
+  return std::max<size_t>(256, round_up(units * (int64_t)sizeof(Part), 16) + units * top * (int64_t)sizeof(key_t));
 }
 
 int token_logprobs(hipStream_t s, const LogprobArgs& a) {

@@ -20,3 +20,19 @@ def test_workspace_of_no_tokens(km):
     for V in (1, 16384, 16385, 128000, 2 ** 31 - 1):
         for top in (0, 1):
             assert km.kmp_token_logprobs_workspace_bytes(0, V, top) > 0, (V, top)
+
+
+def test_workspace_of_the_largest_call_serves_smaller_ones(km):
+    """The size never falls as T, V or top grows."""
+    size = km.kmp_token_logprobs_workspace_bytes
+    Ts = [0, 1, 2, 3, 5, 16, 31, 32, 100, 204, 205, 341, 342, 511, 512, 513, 1023, 1024, 1025, 2048, 2 ** 20, 2 ** 31 - 1]
+    Vs = [64, 4096, 4097, 16384, 16385, 20000, 32768, 32769, 40009, 65536, 65537, 128000, 262144, 262145, 2 ** 31 - 1]
+    tops = [0, 1, 5, 20, 64]
+    for i, T in enumerate(Ts):
+        for j, V in enumerate(Vs):
+            for k, top in enumerate(tops):
+                n = size(T, V, top)
+                assert 0 < n <= 1 << 20
+                assert i == 0 or size(Ts[i - 1], V, top) <= n, (T, V, top)
+                assert j == 0 or size(T, Vs[j - 1], top) <= n, (T, V, top)
+                assert k == 0 or size(T, V, tops[k - 1]) <= n, (T, V, top)
