@@ -328,10 +328,10 @@ def _tokens(t, n: int):
     """(bits, pointer) of the tokens; None stays None."""
     if t is None:
         return 32, None
-    bits = t.element_size() * 8
-    if t.is_floating_point() or bits not in (32, 64):
+    import torch
+    if t.dtype != torch.int64 and t.dtype != torch.int32:
         _refuse(f"tokens have type {t.dtype}, not int32 or int64")
-    return bits, _vector(t, "tokens", n)
+    return t.dtype.itemsize * 8, _vector(t, "tokens", n)
 
 
 def _workspace(t):

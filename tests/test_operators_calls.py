@@ -36,3 +36,46 @@ def test_workspace_of_the_largest_call_serves_smaller_ones(km):
                 assert i == 0 or size(Ts[i - 1], V, top) <= n, (T, V, top)
                 assert j == 0 or size(T, Vs[j - 1], top) <= n, (T, V, top)
                 assert k == 0 or size(T, V, tops[k - 1]) <= n, (T, V, top)
+
+
+class Fake:
+    """A device tensor's metadata."""
+
+    def __init__(self, *shape, dtype, index=0):
+        import torch
+        self.shape, self.dtype, self.is_cuda, self.index = torch.Size(shape), dtype, True, index
+        self.device = torch.device("cuda", index)
+
+    def get_device(self):
+        return self.index
+
+    def stride(self):
+        out, n = [], 1
+        for s in reversed(self.shape):
+            out.append(n)
+            n *= s
+        return tuple(reversed(out))
+
+    def numel(self):
+        return self.shape.numel()
+
+    def is_contiguous(self):
+        return True
+
+    def is_floating_point(self):
+        return self.dtype.is_floating_point
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def data_ptr(self):
+        return 0x1000
+
+
+def test_tokens_are_signed_whole_numbers(km):
+    import torch
+    assert km._tokens(Fake(4, dtype=torch.int32), 4) == (32, 0x1000)
+    assert km._tokens(Fake(4, dtype=torch.int64), 4) == (64, 0x1000)
+    for dt in (torch.complex64, torch.uint64, torch.uint32, torch.complex32, torch.int16, torch.bool, torch.float64):
+        with pytest.raises(km.KmpError, match="tokens have type"):
+            km._tokens(Fake(4, dtype=dt), 4)
