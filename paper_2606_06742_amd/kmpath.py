@@ -271,10 +271,11 @@ def kmp_dgemm_grouped(A, B, C, stream=None) -> None:
 
 
 # ------------------------------------------ operators at a language model's end
-# Tensors are on the current device; matrices are 2-D with consecutive elements
-# in a row and any row stride, vectors are contiguous. Nothing waits for the
-# device: `stream` (the current stream if None) carries the work, and tensors
-# made on another stream are the caller's to order.
+# Tensors are on the current device, and so is `stream` (others are refused);
+# matrices are 2-D with consecutive elements in a row and any row stride, vectors
+# are contiguous. Nothing waits for the device: `stream` (the current stream if
+# None) carries the work, and tensors made on another stream are the caller's to
+# order.
 _TYPES: dict = {}
 
 
@@ -295,11 +296,28 @@ def _refuse(what: str):
     raise KmpError(KMP_EINVAL, what)
 
 
-def _matrix(t, name: str, rows=None, cols=None, dtype=None):
-    """(pointer, rows, columns, row stride) of a 2-D device tensor."""
+def _place(t, name: str, stream):
+    """(index of the tensor's device, handle of the stream); both are of the
+    current device: a kernel that ran elsewhere would not own the memory."""
+    if stream is None and _current is not None:
+        now = _current[0]()
+        handle = _current[1](now)
+    else:
+        import torch
+        handle, now = _stream_ptr(stream), torch.cuda.current_device()
+        if stream is not None and getattr(stream, "device_index", now) != now:
+            _refuse(f"the stream is of device {stream.device_index}, the current device is {now}")
+    if t.get_device() != now:
+        _refuse(f"{name} is on device {t.get_device()}, the current device is {now}")
+    return now, handle
+
+
+def _matrix(t, name: str, rows=None, cols=None, dtype=None, on=None):
+    """(pointer, rows, columns, row stride) of a 2-D tensor of device `on` (None:
+    of any)."""
     shape = t.shape
-    if len(shape) != 2 or not t.is_cuda:
-        _refuse(f"{name} must be a 2-D device tensor")
+    if len(shape) != 2 or (not t.is_cuda if on is None else t.get_device() != on):
+        _refuse(f"{name} must be a 2-D device tensor" + ("" if on is None else f" of device {on}"))
     r, c = shape
     sr, sc = t.stride()
     if (rows is not None and r != rows) or (cols is not None and c != cols):
@@ -313,32 +331,33 @@ def _matrix(t, name: str, rows=None, cols=None, dtype=None):
     return t.data_ptr(), r, c, sr or 1
 
 
-def _vector(t, name: str, n: int, dtype=None):
-    """Pointer of a contiguous device tensor of n elements; None stays None."""
+def _vector(t, name: str, n: int, dtype=None, on=None):
+    """Pointer of a contiguous tensor of n elements of device `on` (None: of any);
+    None stays None."""
     if t is None:
         return None
-    if t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        _refuse(f"{name} must be a contiguous device tensor of {n} elements")
+    if (not t.is_cuda if on is None else t.get_device() != on) or t.numel() != n or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous device tensor of {n} elements" + ("" if on is None else f" of device {on}"))
     if dtype is not None and t.dtype != dtype:
         _refuse(f"{name} has type {t.dtype}, not {dtype}")
     return t.data_ptr()
 
 
-def _tokens(t, n: int):
+def _tokens(t, n: int, on=None):
     """(bits, pointer) of the tokens; None stays None."""
     if t is None:
         return 32, None
     import torch
     if t.dtype != torch.int64 and t.dtype != torch.int32:
         _refuse(f"tokens have type {t.dtype}, not int32 or int64")
-    return t.dtype.itemsize * 8, _vector(t, "tokens", n)
+    return t.dtype.itemsize * 8, _vector(t, "tokens", n, None, on)
 
 
-def _workspace(t):
+def _workspace(t, on):
     if t is None:
         return None, 0
-    if not t.is_cuda or not t.is_contiguous():
-        _refuse("workspace must be a contiguous device tensor")
+    if t.get_device() != on or not t.is_contiguous():
+        _refuse(f"workspace must be a contiguous device tensor of device {on}")
     return t.data_ptr(), t.numel() * t.element_size()
 
 
@@ -347,7 +366,8 @@ def kmp_layer_norm(x, gamma, beta, eps, y, mean=None, rstd=None, scale=None, str
     the rows' scales in `scale`. gamma and beta (d) are of x's type or float32
     (None: ones, zeros); mean and rstd (rows) take what the backward reads."""
     xp, rows, d, ldx = _matrix(x, "x")
-    yp, _, _, ldy = _matrix(y, "y", rows, d)
+    on, sp = _place(x, "x", stream)
+    yp, _, _, ldy = _matrix(y, "y", rows, d, None, on)
     xt = _type(x.dtype, "x")
     w = gamma if gamma is not None else beta
     wd = w.dtype if w is not None else x.dtype
@@ -356,10 +376,10 @@ def kmp_layer_norm(x, gamma, beta, eps, y, mean=None, rstd=None, scale=None, str
         import torch
         sd, rd = torch.float64 if xt == KMP_F64 else torch.float32, torch.float32
     _check(lib().kmp_layer_norm(
-        _stream_ptr(stream), xt, xp, rows, d, ldx, _type(wd, "gamma"), _vector(gamma, "gamma", d, wd),
-        _vector(beta, "beta", d, wd), float(eps), _type(y.dtype, "y"), yp, ldy,
-        _vector(mean, "mean", rows, sd), _vector(rstd, "rstd", rows, sd),
-        _vector(scale, "scale", rows, rd)), allow_maxiter=False)
+        sp, xt, xp, rows, d, ldx, _type(wd, "gamma"), _vector(gamma, "gamma", d, wd, on),
+        _vector(beta, "beta", d, wd, on), float(eps), _type(y.dtype, "y"), yp, ldy,
+        _vector(mean, "mean", rows, sd, on), _vector(rstd, "rstd", rows, sd, on),
+        _vector(scale, "scale", rows, rd, on)), allow_maxiter=False)
 
 
 def kmp_layer_norm_workspace_bytes(rows: int, d: int, dtype) -> int:
@@ -372,18 +392,19 @@ def kmp_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspa
     kmp_layer_norm_workspace_bytes(rows, d, x.dtype) bytes."""
     import torch
     xp, rows, d, ldx = _matrix(x, "x")
-    dyp, _, _, lddy = _matrix(dy, "dy", rows, d, x.dtype)
+    on, sp = _place(x, "x", stream)
+    dyp, _, _, lddy = _matrix(dy, "dy", rows, d, x.dtype, on)
     dxp, lddx = None, d
     if dx is not None:
-        dxp, _, _, lddx = _matrix(dx, "dx", rows, d, x.dtype)
+        dxp, _, _, lddx = _matrix(dx, "dx", rows, d, x.dtype, on)
     xt = _type(x.dtype, "x")
     wd = next((t.dtype for t in (gamma, dgamma, dbeta) if t is not None), x.dtype)
     sd = torch.float64 if xt == KMP_F64 else torch.float32
-    wsp, wsb = _workspace(workspace)
+    wsp, wsb = _workspace(workspace, on)
     _check(lib().kmp_layer_norm_backward(
-        _stream_ptr(stream), xt, dyp, lddy, xp, ldx, rows, d, _type(wd, "gamma"), _vector(gamma, "gamma", d, wd),
-        _vector(mean, "mean", rows, sd), _vector(rstd, "rstd", rows, sd), dxp, lddx,
-        _vector(dgamma, "dgamma", d, wd), _vector(dbeta, "dbeta", d, wd), wsp, wsb),
+        sp, xt, dyp, lddy, xp, ldx, rows, d, _type(wd, "gamma"), _vector(gamma, "gamma", d, wd, on),
+        _vector(mean, "mean", rows, sd, on), _vector(rstd, "rstd", rows, sd, on), dxp, lddx,
+        _vector(dgamma, "dgamma", d, wd, on), _vector(dbeta, "dbeta", d, wd, on), wsp, wsb),
         allow_maxiter=False)
 
 
@@ -391,9 +412,10 @@ def kmp_quantize_rows(x, q, scale, stream=None) -> None:
     """Rows of x (rows, d) in 8 bits: q (rows, d) int8, scale (rows) float32."""
     import torch
     xp, rows, d, ldx = _matrix(x, "x")
-    qp, _, _, ldq = _matrix(q, "q", rows, d, torch.int8)
-    _check(lib().kmp_quantize_rows(_stream_ptr(stream), _type(x.dtype, "x"), xp, rows, d, ldx, qp, ldq,
-                                   _vector(scale, "scale", rows, torch.float32)), allow_maxiter=False)
+    on, sp = _place(x, "x", stream)
+    qp, _, _, ldq = _matrix(q, "q", rows, d, torch.int8, on)
+    _check(lib().kmp_quantize_rows(sp, _type(x.dtype, "x"), xp, rows, d, ldx, qp, ldq,
+                                   _vector(scale, "scale", rows, torch.float32, on)), allow_maxiter=False)
 
 
 def kmp_quantized_product(xq, xscale, wq, wscale, out, bias=None, stream=None) -> None:
@@ -402,12 +424,13 @@ def kmp_quantized_product(xq, xscale, wq, wscale, out, bias=None, stream=None) -
     floating types up to 32 bits."""
     import torch
     xp, M, K, ldx = _matrix(xq, "xq", dtype=torch.int8)
-    wp, N, _, ldw = _matrix(wq, "wq", None, K, torch.int8)
-    op, _, _, ldo = _matrix(out, "out", M, N)
+    on, sp = _place(xq, "xq", stream)
+    wp, N, _, ldw = _matrix(wq, "wq", None, K, torch.int8, on)
+    op, _, _, ldo = _matrix(out, "out", M, N, None, on)
     f = torch.float32
     _check(lib().kmp_quantized_product(
-        _stream_ptr(stream), xp, ldx, _vector(xscale, "xscale", M, f), M, wp, ldw,
-        _vector(wscale, "wscale", N, f), N, K, _vector(bias, "bias", N, f), _type(out.dtype, "out"), op,
+        sp, xp, ldx, _vector(xscale, "xscale", M, f, on), M, wp, ldw,
+        _vector(wscale, "wscale", N, f, on), N, K, _vector(bias, "bias", N, f, on), _type(out.dtype, "out"), op,
         ldo), allow_maxiter=False)
 
 
@@ -425,15 +448,16 @@ def kmp_token_logprobs(logits, tokens, logp, entropy=None, stats=None, top_id=No
     bytes."""
     import torch
     lp, T, V, ldl = _matrix(logits, "logits")
-    bits, tp = _tokens(tokens, T)
+    on, sp = _place(logits, "logits", stream)
+    bits, tp = _tokens(tokens, T, on)
     tops = [t.shape[-1] for t in (top_id, top_logp) if t is not None]
     top = tops[0] if tops else 0
     f = torch.float32
-    wsp, wsb = _workspace(workspace)
+    wsp, wsb = _workspace(workspace, on)
     _check(lib().kmp_token_logprobs(
-        _stream_ptr(stream), _type(logits.dtype, "logits"), lp, T, V, ldl, bits, tp,
-        _vector(logp, "logp", T, f), _vector(entropy, "entropy", T, f), _vector(stats, "stats", 2 * T, f), top,
-        _vector(top_id, "top_id", T * top, torch.int32), _vector(top_logp, "top_logp", T * top, f),
+        sp, _type(logits.dtype, "logits"), lp, T, V, ldl, bits, tp,
+        _vector(logp, "logp", T, f, on), _vector(entropy, "entropy", T, f, on), _vector(stats, "stats", 2 * T, f, on), top,
+        _vector(top_id, "top_id", T * top, torch.int32, on), _vector(top_logp, "top_logp", T * top, f, on),
         wsp, wsb), allow_maxiter=False)
 
 
@@ -444,13 +468,14 @@ def kmp_token_logprobs_backward(logits, tokens, stats, dlogp, dlogits, entropy=N
     None. dlogits may be logits itself."""
     import torch
     lp, T, V, ldl = _matrix(logits, "logits")
-    dp, _, _, ldd = _matrix(dlogits, "dlogits", T, V, logits.dtype)
-    bits, tp = _tokens(tokens, T)
+    on, sp = _place(logits, "logits", stream)
+    dp, _, _, ldd = _matrix(dlogits, "dlogits", T, V, logits.dtype, on)
+    bits, tp = _tokens(tokens, T, on)
     f = torch.float32
     _check(lib().kmp_token_logprobs_backward(
-        _stream_ptr(stream), _type(logits.dtype, "logits"), lp, T, V, ldl, bits, tp,
-        _vector(stats, "stats", 2 * T, f), _vector(entropy, "entropy", T, f), _vector(dlogp, "dlogp", T, f),
-        _vector(dentropy, "dentropy", T, f), dp, ldd), allow_maxiter=False)
+        sp, _type(logits.dtype, "logits"), lp, T, V, ldl, bits, tp,
+        _vector(stats, "stats", 2 * T, f, on), _vector(entropy, "entropy", T, f, on), _vector(dlogp, "dlogp", T, f, on),
+        _vector(dentropy, "dentropy", T, f, on), dp, ldd), allow_maxiter=False)
 
 
 def kmp_fit_path(stream, spec, X, y, sigmas, taus, lambdas, fold_id, V, workspace, ws_bytes,

@@ -79,3 +79,67 @@ def test_tokens_are_signed_whole_numbers(km):
     for dt in (torch.complex64, torch.uint64, torch.uint32, torch.complex32, torch.int16, torch.bool, torch.float64):
         with pytest.raises(km.KmpError, match="tokens have type"):
             km._tokens(Fake(4, dtype=dt), 4)
+
+
+def _calls(km, on, odd=None, stream=None):
+    """Every operator's call as (function, arguments by name), with all its tensors
+    on device `on` but the one named `odd`, which is on the next."""
+    import torch
+    f32, i8 = torch.float32, torch.int8
+
+    def t(name, *shape, dtype=f32):
+        return Fake(*shape, dtype=dtype, index=on + (name == odd))
+
+    m = lambda *names: {n: t(n, 4, 8) for n in names}
+    v = lambda n, *names: {k: t(k, n) for k in names}
+    ws = {"workspace": t("workspace", 1 << 20, dtype=torch.uint8)}
+    tok = {"tokens": t("tokens", 4, dtype=torch.int64)}
+    top = {"top_id": t("top_id", 4, 2, dtype=torch.int32), "top_logp": t("top_logp", 4, 2)}
+    stats = {"stats": t("stats", 4, 2)}
+    return [
+        (km.kmp_layer_norm, {**m("x", "y"), **v(8, "gamma", "beta"), "eps": 1e-5, **v(4, "mean", "rstd")}),
+        (km.kmp_layer_norm, {**m("x"), **v(8, "gamma", "beta"), "eps": 1e-5, "y": t("y", 4, 8, dtype=i8), **v(4, "scale")}),
+        (km.kmp_layer_norm_backward, {**m("dy", "x", "dx"), **v(8, "gamma", "dgamma", "dbeta"), **v(4, "mean", "rstd"), **ws}),
+        (km.kmp_quantize_rows, {**m("x"), "q": t("q", 4, 8, dtype=i8), **v(4, "scale")}),
+        (km.kmp_quantized_product, {"xq": t("xq", 4, 8, dtype=i8), "wq": t("wq", 6, 8, dtype=i8), **v(4, "xscale"),
+                                    **v(6, "wscale", "bias"), "out": t("out", 4, 6)}),
+        (km.kmp_token_logprobs, {**m("logits"), **tok, **v(4, "logp", "entropy"), **stats, **top, **ws}),
+        (km.kmp_token_logprobs_backward, {**m("logits", "dlogits"), **tok, **stats, **v(4, "dlogp", "entropy", "dentropy")}),
+    ]
+
+
+class Stream:
+    cuda_stream = 0
+
+    def __init__(self, index):
+        self.device_index = index
+
+
+def test_tensors_and_streams_of_other_devices_are_refused(km, monkeypatch):
+    """A call with every tensor on the current device passes to the library; with
+    all of them, any one of them, or the stream on another device it does not."""
+    passed = []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: passed.append(name) or 0
+
+    import torch
+    monkeypatch.setattr(km, "_current", (lambda: 1, lambda d: 0))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(km, "lib", Lib)
+    for i, (call, args) in enumerate(_calls(km, 1)):
+        call(**args)
+        call(**args, stream=Stream(1))
+        assert passed == [call.__name__] * 2
+        passed.clear()
+        with pytest.raises(km.KmpError, match="stream"):
+            call(**args, stream=Stream(0))
+        for on in (0, 2):
+            with pytest.raises(km.KmpError, match="device"):
+                call(**_calls(km, on)[i][1])
+        for name in args:
+            if name != "eps":
+                with pytest.raises(km.KmpError, match=rf"\b{name} (is|must) .*device"):
+                    call(**_calls(km, 1, odd=name)[i][1])
+        assert passed == []
