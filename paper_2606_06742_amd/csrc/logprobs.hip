@@ -37,11 +37,16 @@ __device__ __forceinline__ Part join(const Part& a, const Part& b) {
   r.u = fa * (a.u + da * a.s) + fb * (b.u + db * b.s);
   return r;
 }
+// (A join rounds differently with its two parts exchanged, so the lanes' results
+// differ in their last bits: lane 0's for all, whichever writes something with it.)
+__device__ __forceinline__ float first_lane(float v) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v)));
+}
 __device__ __forceinline__ Part wave_join(Part p) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1)
     p = join(p, Part{__shfl_xor(p.m, off, kWave), __shfl_xor(p.s, off, kWave), __shfl_xor(p.u, off, kWave)});
-  return p;
+  return Part{first_lane(p.m), first_lane(p.s), first_lane(p.u)};
 }
 __device__ __forceinline__ Part block_join(Part p, Part* red) {
   p = wave_join(p);

@@ -30,3 +30,28 @@ def test_one_workspace_for_all_batches():
         own = torch.empty(km.kmp_token_logprobs_workspace_bytes(T, V, top), dtype=torch.uint8, device=device())
         assert all(torch.equal(a, b) for a, b in zip(call(kept[:need]), call(own)))
         assert bool((kept[need:] == 77).all())
+
+
+@pytest.mark.parametrize("T,V,top", [(64, 70001, 7), (64, 70001, 20), (16, 128000, 64), (128, 50003, 40), (3, 32000, 20),
+                                     (600, 9001, 33)])
+def test_alternatives_have_the_bits_of_the_token(T, V, top):
+    """An alternative's log probability is the same number as the log probability
+    of that token asked for by itself, whichever thread writes it; and the same
+    call gives the same bits again."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    announce(f"alternatives as tokens {T} x {V} top {top}")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T + V)
+    x = torch.randn(T, V, generator=gen, device=device()) * 3.0
+    ws = torch.empty(km.kmp_token_logprobs_workspace_bytes(T, V, top), dtype=torch.uint8, device=device())
+    f = lambda *s: torch.empty(*s, device=device())
+    tl, again, ti = f(T, top), f(T, top), torch.empty(T, top, dtype=torch.int32, device=device())
+    km.kmp_token_logprobs(x, None, None, top_id=ti, top_logp=tl, workspace=ws)
+    for _ in range(4):
+        km.kmp_token_logprobs(x, None, None, top_id=ti, top_logp=again, workspace=ws)
+        assert torch.equal(again, tl)
+    for r in range(0, top, 3):
+        lp = f(T)
+        km.kmp_token_logprobs(x, ti[:, r].contiguous(), lp, workspace=ws)
+        assert torch.equal(lp, tl[:, r]), r
