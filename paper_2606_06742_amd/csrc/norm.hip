@@ -563,26 +563,31 @@ __global__ __launch_bounds__(BT) void norm_back_columns_kernel(NormBackArgs a, i
   p[a.d + j] = db;
 }
 
-// Adds the partial sums in a fixed order: 64 columns a workgroup, each of its 16
-// wavefronts every sixteenth part, then the sixteen.
+// Adds the partial sums in a fixed order: 64 columns a workgroup at a time, each of
+// its 16 wavefronts every sixteenth part, then the sixteen. At most 2^20 workgroups: a
+// launch takes less than 2^32 threads.
 template <typename A, typename W>
 __global__ __launch_bounds__(1024) void norm_back_join_kernel(const A* partial, int64_t parts, int64_t d,
                                                               W* dgamma, W* dbeta) {
   __shared__ A red[16][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t j = (int64_t)blockIdx.x * 64 + lane;
   W* out = blockIdx.y == 0 ? dgamma : dbeta;
-  A s = 0;
-  if (j < d && out) {
+  if (!out) return;
+  for (int64_t j0 = (int64_t)blockIdx.x * 64; j0 < d; j0 += (int64_t)gridDim.x * 64) {
+    const int64_t j = j0 + lane;
+    A s = 0;
+    if (j < d) {
 #pragma unroll 8
-    for (int64_t p = w; p < parts; p += 16) s += partial[(p * 2 + blockIdx.y) * d + j];
-  }
-  red[w][lane] = s;
-  __syncthreads();
-  if (w == 0 && j < d && out) {
+      for (int64_t p = w; p < parts; p += 16) s += partial[(p * 2 + blockIdx.y) * d + j];
+    }
+    red[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && j < d) {
 #pragma unroll
-    for (int i = 1; i < 16; ++i) s += red[i][lane];
-    out[j] = (W)s;
+      for (int i = 1; i < 16; ++i) s += red[i][lane];
+      out[j] = (W)s;
+    }
+    __syncthreads();
   }
 }
 
@@ -684,9 +689,9 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
   }
 #undef KMP_NORM_CASE
   if (!weights || one) return 0;
-  hipLaunchKernelGGL((norm_back_join_kernel<A, W>), dim3((unsigned)ceil_div(a.d, 64), 2), dim3(1024), 0, s,
-                     static_cast<const A*>(a.partial), a.rows > 0 ? parts : 0, a.d, static_cast<W*>(a.dgamma),
-                     static_cast<W*>(a.dbeta));
+  hipLaunchKernelGGL((norm_back_join_kernel<A, W>), dim3((unsigned)std::min<int64_t>(ceil_div(a.d, 64), 1 << 20), 2),
+                     dim3(1024), 0, s, static_cast<const A*>(a.partial), a.rows > 0 ? parts : 0, a.d,
+                     static_cast<W*>(a.dgamma), static_cast<W*>(a.dbeta));
   KMP_LAUNCH_CHECK();
   return 0;
 }

@@ -55,3 +55,24 @@ def test_alternatives_have_the_bits_of_the_token(T, V, top):
         lp = f(T)
         km.kmp_token_logprobs(x, ti[:, r].contiguous(), lp, workspace=ws)
         assert torch.equal(lp, tl[:, r]), r
+
+
+def test_layer_norm_weight_gradients_of_a_very_long_row():
+    """More columns than 2^32 threads take at one workgroup for 64 of them. One
+    row: dgamma is dy xh (x - mu and two products: 3 roundings), dbeta is dy."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    d = 2 ** 28 + 65
+    announce(f"layer norm backward f32 1 x {d}")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(2)
+    x, dy = (torch.randn(1, d, generator=gen, device=device()) for _ in range(2))
+    mean, rstd = torch.full((1,), 0.125, device=device()), torch.full((1,), 0.75, device=device())
+    ws = torch.empty(km.kmp_layer_norm_workspace_bytes(1, d, torch.float32), dtype=torch.uint8, device=device())
+    dg, db = torch.full((d,), 7.0, device=device()), torch.full((d,), 7.0, device=device())
+    km.kmp_layer_norm_backward(dy, x, None, mean, rstd, None, dg, db, ws)
+    assert torch.equal(db, dy[0])
+    for i in range(0, d, 1 << 26):               # (in parts, for memory)
+        part = slice(i, i + (1 << 26))
+        want = dy[0, part].double() * (x[0, part].double() - 0.125) * 0.75
+        assert bool(((dg[part].double() - want).abs() <= 4 * 2.0 ** -24 * want.abs() + 2.0 ** -149).all())
