@@ -55,9 +55,12 @@ __device__ __forceinline__ void over_row(int64_t d, F f) {
 __device__ __forceinline__ float inv_sqrt(float v) { return 1.0f / sqrtf(v); }
 __device__ __forceinline__ double inv_sqrt(double v) { return 1.0 / sqrt(v); }
 
-// The factor (1 / a) 127 that takes a row into 8 bits, and its scale a / 127.
-// Below 2^-100 the factor would overflow: such rows are brought up by 2^100
-// first. A row with an infinity or NaN gets factor 0 and scale NaN.
+// The factor (1 / a) 127 that takes a row into 8 bits, and its scale a / 127. Three
+// roundings with the product by x: a result differs from the nearest to x 127 / a only
+// where that lies within 127 * 3 * 2^-24 of a half (65 of 4e7 normal numbers in 32
+// bits, 45 with the factor 127 / a). Below 2^-100 the factor would overflow: such rows
+// are brought up by 2^100 first. A row with an infinity or NaN gets factor 0 and scale
+// NaN.
 struct ByteScale {
   float lift, factor, scale;
   __device__ explicit ByteScale(float a) {
