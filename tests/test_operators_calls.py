@@ -143,3 +143,29 @@ def test_tensors_and_streams_of_other_devices_are_refused(km, monkeypatch):
                 with pytest.raises(km.KmpError, match=rf"\b{name} (is|must) .*device"):
                     call(**_calls(km, 1, odd=name)[i][1])
         assert passed == []
+
+
+def test_workspaces_of_the_largest_arguments(km):
+    """Sizes at the largest accepted arguments are what their formulas give in
+    whole numbers without a limit; one past them is refused."""
+    import torch
+    most = 2 ** 31 - 1
+    L = km.lib()
+    # 512 workgroups' sums of dgamma and dbeta, each a row
+    for dtype, b in ((torch.float64, 8), (torch.float32, 4), (torch.bfloat16, 4), (torch.float16, 4)):
+        assert km.kmp_layer_norm_workspace_bytes(most, most, dtype) == 512 * 2 * most * b
+        assert km.kmp_layer_norm_workspace_bytes(0, most, dtype) == 2 * most * b
+        assert km.kmp_layer_norm_workspace_bytes(most + 1, 1, dtype) == 0
+        assert km.kmp_layer_norm_workspace_bytes(1, most + 1, dtype) == 0
+    # 1024 segments: three 32-bit numbers and 64 keys of 64 bits each
+    assert km.kmp_token_logprobs_workspace_bytes(most, most, 64) == 1024 * (12 + 64 * 8)
+    assert L.kmp_token_logprobs_workspace_bytes(most + 1, 1, 0) == 0 and L.kmp_token_logprobs_workspace_bytes(1, most + 1, 0) == 0
+    # refused with the largest arguments beside a wrong one
+    P = 0x1000
+    ld = 1 << 40
+    assert L.kmp_layer_norm(None, 1, P, most, most, ld, 1, P, P, -1.0, 1, P, ld, None, None, None) == km.KMP_EINVAL
+    assert L.kmp_layer_norm_backward(None, 1, P, ld, P, ld, most, most, 1, P, P, P, P, ld, P, P, P, 512 * 8 * most - 1) == km.KMP_EWORKSPACE
+    assert L.kmp_quantize_rows(None, 1, None, most, most, ld, P, ld, P) == km.KMP_EINVAL
+    assert L.kmp_quantized_product(None, P, ld, P, most, P, ld, P, most, 131071, None, 1, P, ld) == km.KMP_EINVAL
+    assert L.kmp_token_logprobs(None, 1, P, most, most, ld, 64, P, P, P, P, 64, P, P, P, 1024 * (12 + 64 * 8) - 1) == km.KMP_EWORKSPACE
+    assert L.kmp_token_logprobs_backward(None, 1, P, most, most, ld, 64, None, P, P, P, P, P, ld) == km.KMP_EINVAL
