@@ -390,7 +390,9 @@ int kmp_quantize_rows(void* stream, int32_t xtype, const void* x, int64_t rows, 
  * (KMP_F32, KMP_BF16 or KMP_F16). The sums are exact in 32-bit integers:
  * K <= 131071 (KMP_EINVAL above). K = 0 gives the bias. Rows that start at
  * multiples of 16 bytes (ldx, ldw multiples of 16) are read fastest; K itself
- * may be any number.                                                        */
+ * may be any number. An output has at most 2^23 tiles of 64 x 64, counted by
+ * ceil(M / 64) ceil(N / 64) (KMP_EINVAL above): 2^35 elements and, for a few
+ * tokens, 2^29 channels.                                                    */
 int kmp_quantized_product(void* stream, const int8_t* x, int64_t ldx, const float* xscale, int64_t M,
                           const int8_t* w, int64_t ldw, const float* wscale, int64_t N, int64_t K,
                           const float* bias, int32_t otype, void* out, int64_t ldo);

@@ -169,3 +169,18 @@ def test_workspaces_of_the_largest_arguments(km):
     assert L.kmp_quantized_product(None, P, ld, P, most, P, ld, P, most, 131071, None, 1, P, ld) == km.KMP_EINVAL
     assert L.kmp_token_logprobs(None, 1, P, most, most, ld, 64, P, P, P, P, 64, P, P, P, 1024 * (12 + 64 * 8) - 1) == km.KMP_EWORKSPACE
     assert L.kmp_token_logprobs_backward(None, 1, P, most, most, ld, 64, None, P, P, P, P, P, ld) == km.KMP_EINVAL
+
+
+def test_most_tiles_of_a_product(km):
+    """2^23 tiles of 64 x 64 pass the checks (the null output is found after them),
+    one more does not."""
+    P = 0x1000
+
+    def call(M, N):
+        code = km.lib().kmp_quantized_product(None, P, 8, P, M, P, 8, P, N, 8, None, 1, None, N)
+        return code, km.kmp_strerror(code)
+
+    for M, N in ((64, 2 ** 29), (1, 2 ** 29), (2 ** 14, 2 ** 21), (2 ** 29, 64)):
+        assert call(M, N) == (km.KMP_EINVAL, "kmp_quantized_product: null pointer")
+    for M, N in ((64, 2 ** 29 + 1), (65, 2 ** 29), (2 ** 14 + 1, 2 ** 21), (2 ** 29 + 1, 1)):
+        assert call(M, N) == (km.KMP_EINVAL, "kmp_quantized_product: more than 2^23 tiles of 64 x 64")
