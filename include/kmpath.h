@@ -331,10 +331,11 @@ int kmp_dgemm_grouped(void* stream, int32_t G, int32_t M, int32_t N, int32_t K,
  * Operators at a language model's end: the layer norm of its hidden states,
  * the 8-bit product with its vocabulary head, and the log probabilities of its
  * tokens. A kernel machine's features often come from there (hidden states;
- * log probability and entropy of an answer's tokens), and the gradients go
- * back through them. Unlike the entry points above they work in 16 or 32 bits
- * (sums and statistics in 32, or 64 for doubles), never allocate, never wait
- * for the device and may be captured into a HIP graph. Element types:       */
+ * log probability and entropy of an answer's tokens). Their gradients train the
+ * model's end itself: the path above gives none with respect to its features.
+ * Unlike the entry points above they work in 16 or 32 bits (sums and statistics
+ * in 32, or 64 for doubles, which the layer norm takes), never allocate, never
+ * wait for the device and may be captured into a HIP graph. Element types:  */
 #define KMP_F64 0
 #define KMP_F32 1
 #define KMP_BF16 2

@@ -645,6 +645,8 @@ int backward_as(hipStream_t s, const NormBackArgs& a) {
   // in 16 bits 21.8 / 17.2, 2000 x 512 12.4 / 10.7 (and 3 us of launch on the host). Rows
   // too long for the registers, in one and in three: 4 x 13134 in 16 bits 6.0 / 10.0,
   // 116 x 14770 10.1 / 17.9, 250 x 16384 19.6 / 23.7, 100 x 16384 in 32 bits 10.1 / 18.2.
+  // Doubles: 300 x 512 4.4 / 7.2, 500 x 2000 11.5 / 13.9, 100 x 10000 11.5 / 19.2, but
+  // slower between 513 and 2048 rows: 1000 x 500 13.9 / 10.5, 2000 x 250 20.2 / 10.9.
   const int64_t size = a.rows * a.d * (int64_t)sizeof(T);
   const bool small = a.rows <= 512 ? size <= 8 << 20 : a.rows <= 2048 && size <= 4 << 20;
   const bool one = weights && a.rows > 0 && small;

@@ -517,6 +517,16 @@ int ahead_as(hipStream_t s, const QProductArgs& a) {
 //   1024 x 3584 x 4096        26.7   23.9
 //   2000 x 2000 x 8192        47.6   43.5
 //   2048 x 2048 x 2048        17.1   16.1
+// Few tokens with more channels than the first table's have 192 tiles of 256 and take
+// them (in a recorded graph, w from HBM), though smaller ones are ahead (reading alone
+// is a little faster than the copy that the floor's rate is of):
+//                        few  32x64  64,3  64,2  64,1   128   256  floor
+//   1 x 50257 x 2048    19.4  28.0  28.3  24.6  21.4  22.8  31.6  21.4
+//   64 x 50257 x 2048         43.2  34.6  30.2  30.3  29.0  34.6  22.8
+//   16 x 128256 x 4096   141   105   108   107   108   109   133   110
+//   64 x 128256 x 4096         164   128   122   123   121   138   113
+//   1 x 151936 x 4096    103   126   134   139   152   155   180   129
+//   64 x 151936 x 4096         191   159   152   152   162   187   133
 // Rows that are not aligned: few tokens; tiles of 32 x 64 (four groups), 64 and 128
 // (one; 128 with eight wavefronts, with four 97 for 87 at 1244 x 1824 x 10909):
 //                        few  32x64    64   128  floor
