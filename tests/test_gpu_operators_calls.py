@@ -76,3 +76,54 @@ def test_layer_norm_weight_gradients_of_a_very_long_row():
         part = slice(i, i + (1 << 26))
         want = dy[0, part].double() * (x[0, part].double() - 0.125) * 0.75
         assert bool(((dg[part].double() - want).abs() <= 4 * 2.0 ** -24 * want.abs() + 2.0 ** -149).all())
+
+
+def test_several_launches_replayed_from_a_graph():
+    """Calls of more than one launch (rows split over workgroups and joined, weight
+    gradients over many rows), captured and replayed on new inputs with eager work
+    between the replays: the eager results every time, bit by bit."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    announce("calls of several launches in a graph")
+    dev = device()
+    T, V, top, rows, d = 5, 70001, 20, 2500, 1000
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(6)
+    x, tok = torch.empty(T, V, device=dev), torch.tensor([1, 70000, -1, 5, 9], device=dev)
+    h, dy = (torch.empty(rows, d, device=dev, dtype=torch.bfloat16) for _ in range(2))
+    g = torch.ones(d, device=dev)
+    grad = torch.full((T,), -0.2, device=dev)
+
+    def fill():
+        x.copy_(torch.randn(T, V, generator=gen, device=dev) * 3)
+        h.copy_(torch.randn(rows, d, generator=gen, device=dev))
+        dy.copy_(torch.randn(rows, d, generator=gen, device=dev))
+
+    def buffers():
+        f = lambda *s: torch.zeros(*s, device=dev)
+        return dict(lp=f(T), H=f(T), st=f(T, 2), ti=torch.zeros(T, top, dtype=torch.int32, device=dev), tl=f(T, top), dl=f(T, V),
+                    y=torch.zeros_like(h), m=f(rows), r=f(rows), dx=torch.zeros_like(h), dg=f(d), db=f(d),
+                    ws=torch.zeros(km.kmp_token_logprobs_workspace_bytes(T, V, top), dtype=torch.uint8, device=dev),
+                    wn=torch.zeros(km.kmp_layer_norm_workspace_bytes(rows, d, torch.bfloat16), dtype=torch.uint8, device=dev))
+
+    def work(v):
+        km.kmp_token_logprobs(x, tok, v["lp"], entropy=v["H"], stats=v["st"], top_id=v["ti"], top_logp=v["tl"], workspace=v["ws"])
+        km.kmp_token_logprobs_backward(x, tok, v["st"], grad, v["dl"], entropy=v["H"], dentropy=grad)
+        km.kmp_layer_norm(h, g, None, 1e-5, v["y"], mean=v["m"], rstd=v["r"])
+        km.kmp_layer_norm_backward(dy, h, g, v["m"], v["r"], v["dx"], v["dg"], v["db"], v["wn"])
+
+    eager, kept = buffers(), buffers()
+    fill()
+    work(kept)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        work(kept)
+    for i in range(4):
+        fill()
+        graph.replay()
+        torch.cuda.synchronize()
+        work(eager)
+        torch.cuda.synchronize()
+        for k in eager:
+            if k not in ("ws", "wn"):
+                assert torch.equal(eager[k], kept[k]), (i, k)
