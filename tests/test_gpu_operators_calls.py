@@ -127,3 +127,106 @@ def test_several_launches_replayed_from_a_graph():
         for k in eager:
             if k not in ("ws", "wn"):
                 assert torch.equal(eager[k], kept[k]), (i, k)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows 2^31 and some elements apart, in every matrix argument: the results of
+    the same rows packed."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    dev, far = device(), 2 ** 31 + 48
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(8)
+
+    def apart(a, fill=None):
+        """a's rows far apart (nothing between them is touched)."""
+        t = torch.empty((a.shape[0] - 1) * far + a.shape[1], dtype=a.dtype, device=dev).as_strided(a.shape, (far, 1))
+        return t.copy_(a) if fill is None else t.fill_(fill)
+
+    f = lambda *s: torch.empty(*s, device=dev)
+    bf = torch.bfloat16
+    for d in (1000, 20000):                       # rows in registers, and longer ones
+        announce(f"layer norm 3 x {d}, rows {far} elements apart")
+        x, dy = (torch.randn(3, d, generator=gen, device=dev).to(bf) for _ in range(2))
+        g, b = torch.randn(d, generator=gen, device=dev), torch.randn(d, generator=gen, device=dev)
+        ws = torch.empty(km.kmp_layer_norm_workspace_bytes(3, d, bf), dtype=torch.uint8, device=dev)
+        outs = []
+        for put in (lambda a, fill=None: a.clone() if fill is None else torch.full_like(a, fill), apart):
+            xs, dys, y, dx = put(x), put(dy), put(x, 7.0), put(x, 7.0)
+            q, mean, rstd, dg, db, s1, s2 = put(torch.zeros(3, d, dtype=torch.int8, device=dev), 7), f(3), f(3), f(d), f(d), f(3), f(3)
+            km.kmp_layer_norm(xs, g, b, 1e-5, y, mean=mean, rstd=rstd)
+            km.kmp_layer_norm_backward(dys, xs, g, mean, rstd, dx, dg, db, ws)
+            km.kmp_layer_norm(xs, g, b, 1e-5, q, scale=s1)
+            out = [y.clone(), mean, rstd, dx.clone(), dg, db, q.clone(), s1]
+            km.kmp_quantize_rows(xs, q, s2)
+            outs.append(out + [q.clone(), s2])
+            del xs, dys, y, dx, q
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+    for M, N, K in ((3, 40, 600), (3, 9000, 600), (3, 9000, 601)):
+        announce(f"quantized product {M} x {N} x {K}, rows {far} elements apart")
+        x, w = (torch.randint(-128, 128, (r, K), dtype=torch.int8, generator=gen, device=dev) for r in (M, 3))
+        xs = torch.rand(M, generator=gen, device=dev)
+        for few in (True, False):                # few channels far apart, or many packed
+            wq = w if few else torch.randint(-128, 128, (N, K), dtype=torch.int8, generator=gen, device=dev)
+            sc = torch.rand(wq.shape[0], generator=gen, device=dev)
+            packed, spread = torch.empty(M, wq.shape[0], dtype=bf, device=dev), apart(torch.zeros(M, wq.shape[0], dtype=bf, device=dev), 7.0)
+            km.kmp_quantized_product(x, xs, wq, sc, packed)
+            km.kmp_quantized_product(apart(x), xs, apart(wq) if few else wq, sc, spread)
+            assert torch.equal(packed, spread), (M, wq.shape[0], K)
+
+    for V, top in ((1003, 5), (70001, 20)):
+        announce(f"token logprobs 3 x {V}, rows {far} elements apart")
+        x, tok = (torch.randn(3, V, generator=gen, device=dev) * 3).to(bf), torch.tensor([V - 1, 5, -1], device=dev)
+        ws = torch.empty(km.kmp_token_logprobs_workspace_bytes(3, V, top), dtype=torch.uint8, device=dev)
+        grad = torch.tensor([1.0, -0.5, 2.0], device=dev)
+        outs = []
+        for xs, dx in ((x, torch.full_like(x, 7.0)), (apart(x), apart(x, 7.0))):
+            lp, H, st, ti, tl = f(3), f(3), f(3, 2), torch.empty(3, top, dtype=torch.int32, device=dev), f(3, top)
+            km.kmp_token_logprobs(xs, tok, lp, entropy=H, stats=st, top_id=ti, top_logp=tl, workspace=ws)
+            km.kmp_token_logprobs_backward(xs, tok, st, grad, dx, entropy=H, dentropy=grad)
+            outs.append((lp, H, st, ti, tl, dx.clone()))
+        assert all(torch.equal(a, b) for a, b in zip(*outs))
+        del xs, dx
+
+
+def test_outputs_beyond_32_bits():
+    """More than 2^31 elements in a packed output: the last rows are those of a call
+    of their own, and so are some across the border."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    dev = device()
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(9)
+    M, N, K = 70001, 32000, 130
+    announce(f"quantized product {M} x {N} x {K}")
+    x, w = (torch.randint(-128, 128, (r, K + 14), dtype=torch.int8, generator=gen, device=dev)[:, :K] for r in (M, N))
+    xs, sc = torch.rand(M, generator=gen, device=dev), torch.rand(N, generator=gen, device=dev)
+    out = torch.empty(M, N, dtype=torch.bfloat16, device=dev)
+    km.kmp_quantized_product(x, xs, w, sc, out)
+    for i in (0, 2 ** 31 // N - 3, 2 ** 32 // N - 3 if 2 ** 32 // N < M else M // 2, M - 7):
+        part = torch.empty(7, N, dtype=torch.bfloat16, device=dev)
+        km.kmp_quantized_product(x[i:i + 7], xs[i:i + 7], w, sc, part)
+        assert torch.equal(out[i:i + 7], part), i
+    # the same memory as logits
+    announce(f"token logprobs {M} x {N}")
+    tok = torch.randint(0, N, (M,), generator=gen, device=dev)
+
+    def call(x, tok):
+        n = x.shape[0]
+        lp, H, st, ti, tl = (torch.empty(n, *s, device=dev) for s in ((), (), (2,), (5,), (5,)))
+        ti = ti.int()
+        ws = torch.empty(km.kmp_token_logprobs_workspace_bytes(n, N, 5), dtype=torch.uint8, device=dev)
+        km.kmp_token_logprobs(x, tok, lp, entropy=H, stats=st, top_id=ti, top_logp=tl, workspace=ws)
+        return lp, H, st, ti, tl
+
+    whole = call(out, tok)
+    grad = torch.ones(M, device=dev)
+    dx = torch.empty_like(out)
+    km.kmp_token_logprobs_backward(out, tok, whole[2], grad, dx, entropy=whole[1], dentropy=grad)
+    for i in (0, 2 ** 31 // N - 300, M - 600):
+        j = slice(i, i + 600)
+        assert all(torch.equal(a[j], b) for a, b in zip(whole, call(out[j], tok[j]))), i
+        part = torch.empty_like(dx[j])
+        km.kmp_token_logprobs_backward(out[j], tok[j], whole[2][j], grad[j], part, entropy=whole[1][j], dentropy=grad[j])
+        assert torch.equal(dx[j], part), i
