@@ -376,6 +376,60 @@ int kmp_layer_norm_backward(void* stream, int32_t xtype, const void* dy, int64_t
                             const void* mean, const void* rstd, void* dx, int64_t lddx, void* dgamma,
                             void* dbeta, void* workspace, size_t workspace_bytes);
 
+/* The norms around a block of a model, fused with the block's gate and the residual
+ * stream: from the block's output b and the stream res (DEVICE, rows x d, xtype)
+ *   n = N(b; gamma_after, beta_after) with KMP_NORM_AFTER, else b
+ *   h = rscale res + gate n          (the stream after the block)
+ *   y = N(h; gamma, beta)            (what the next block reads)
+ * with N the layer norm as above or, with KMP_NORM_RMS, mu = 0 and r = 1 /
+ * sqrt(mean_j x^2 + eps). y is formed from h's 32-bit values.
+ *   xtype      KMP_F32, KMP_BF16 or KMP_F16
+ *   flags      of KMP_NORM_RMS (both norms) and KMP_NORM_AFTER
+ *   res        NULL: no residual
+ *   gamma_after, beta_after, gamma, beta  DEVICE [d] of type wtype (xtype, or
+ *              KMP_F32 for 16-bit x), each may be NULL (ones, zeros)
+ *   gate       NULL (ones); with ldg = 0 DEVICE [d] of wtype, for every row; with
+ *              ldg >= d DEVICE, rows x d of xtype
+ *   h          DEVICE, xtype; may be NULL; h == res with ldh == ldr is allowed
+ *   y          DEVICE, of type ytype = xtype or KMP_I8 (as by kmp_quantize_rows,
+ *              scales in scale [rows]); may be NULL: no norm of h. h or y
+ *   stats      DEVICE [rows][4]: mu and r of b's norm, mu and r of h's (0 and 1
+ *              where there is no such norm); may be NULL; the backward pass reads it */
+#define KMP_NORM_RMS 1
+#define KMP_NORM_AFTER 2
+int kmp_block_norm(void* stream, int32_t xtype, int32_t flags, const void* b, int64_t ldb, const void* res,
+                   int64_t ldr, int64_t rows, int64_t d, int32_t wtype, const void* gamma_after,
+                   const void* beta_after, const void* gate, int64_t ldg, double rscale, const void* gamma,
+                   const void* beta, double eps, void* h, int64_t ldh, int32_t ytype, void* y, int64_t ldy,
+                   float* stats, float* scale);
+
+/* Bytes of DEVICE workspace of kmp_block_norm_backward; 0: bad arguments.     */
+size_t kmp_block_norm_workspace_bytes(int32_t xtype, int64_t rows, int64_t d);
+
+/* Gradients of kmp_block_norm from dy and dh (DEVICE, rows x d, xtype; the
+ * gradients of y and of h itself; one of them may be NULL: zero). With s = dh +
+ * the gradient of y's norm at h, and t = gate s,
+ *   dres = rscale s, db = t or the gradient of b's norm from t   (rows x d, xtype)
+ *   dgate = sum over rows of s n, or s n itself for a gate per row (rows x d, xtype)
+ *   dgamma = sum over rows of dy (h - mu) r, dbeta = sum over rows of dy
+ *   dgamma_after, dbeta_after: the same from t and b              ([d], wtype)
+ * b, h, gamma_after, beta_after, gate, rscale, gamma and stats as of the forward
+ * call (h as it was rounded to xtype). Without dy, h is not read and gamma's and
+ * beta's gradients are zero. Every output may be NULL; dgate is [d] of wtype with
+ * ldg = 0 and refused without a gate; the gradients of gamma_after and beta_after
+ * are refused without KMP_NORM_AFTER. No output overlaps an input or another
+ * output. The workspace (16-byte aligned) is needed for any [d] gradient. The sums
+ * over the rows are taken in a fixed order: the same call gives the same bits.
+ * With rows = 0 the [d] gradients are set to zero.                           */
+int kmp_block_norm_backward(void* stream, int32_t xtype, int32_t flags, const void* dy, int64_t lddy,
+                            const void* dh, int64_t lddh, const void* b, int64_t ldb, const void* h,
+                            int64_t ldh, int64_t rows, int64_t d, int32_t wtype, const void* gamma_after,
+                            const void* beta_after, const void* gate, int64_t ldg, double rscale,
+                            const void* gamma, const float* stats, void* db, int64_t lddb, void* dres,
+                            int64_t lddres, void* dgate, int64_t lddg, void* dgamma_after,
+                            void* dbeta_after, void* dgamma, void* dbeta, void* workspace,
+                            size_t workspace_bytes);
+
 /* Rows of x (DEVICE, rows x d; KMP_F32, KMP_BF16 or KMP_F16) in 8 bits:
  * q = rint(x f), f = (1 / a) 127, scale = a / 127, a the row's largest |x|, every
  * operation rounded to 32 bits (DEVICE, q rows x d, scale [rows]). A zero row

@@ -28,6 +28,51 @@ def layer_norm_backward(dy, x, gamma, mean, rstd):
     return dx, (dy * xh).sum(axis=0), dy.sum(axis=0)
 
 
+def block_norm(b, res, gamma_after, beta_after, gate, gamma, beta, eps, rscale=1.0, after=True, rms=False):
+    """(h, y, stats): h = rscale res + gate N(b), y = N(h), stats (rows, 4) the mean
+    and factor of either norm (0 and 1 without `after`)."""
+    def norm(x, g, c):
+        mean = np.zeros(len(x)) if rms else x.mean(axis=1)
+        r = 1.0 / np.sqrt(((x - mean[:, None]) ** 2).mean(axis=1) + eps)
+        y = (x - mean[:, None]) * r[:, None]
+        y = y if g is None else y * np.asarray(g, np.float64)
+        return (y if c is None else y + np.asarray(c, np.float64)), mean, r
+
+    b = np.asarray(b, np.float64)
+    n, m1, r1 = norm(b, gamma_after, beta_after) if after else (b, np.zeros(len(b)), np.ones(len(b)))
+    h = n if gate is None else np.asarray(gate, np.float64) * n
+    if res is not None:
+        h = rscale * np.asarray(res, np.float64) + h
+    y, m2, r2 = norm(h, gamma, beta)
+    return h, y, np.stack([m1, r1, m2, r2], axis=1)
+
+
+def block_norm_backward(dy, dh, b, h, stats, gamma_after, beta_after, gate, gamma, rscale=1.0, after=True, rms=False):
+    """dict of db, dres, dgate (per row and element), dgamma_after, dbeta_after,
+    dgamma, dbeta at the given h and stats; s, t as intermediate results."""
+    f = lambda a, none: none if a is None else np.asarray(a, np.float64)
+    b = f(b, None)
+    m1, r1, m2, r2 = (stats[:, i:i + 1].astype(np.float64) for i in range(4))
+    ga, ca, g0, g2 = f(gamma_after, 1.0), f(beta_after, 0.0), f(gate, 1.0), f(gamma, 1.0)
+
+    def back(w, xh, r):
+        dx = w - xh * (w * xh).mean(axis=1, keepdims=True)
+        return r * (dx if rms else dx - w.mean(axis=1, keepdims=True))
+
+    s = f(dh, np.zeros_like(b))
+    out = dict(dgamma=np.zeros(b.shape[1]), dbeta=np.zeros(b.shape[1]))
+    if dy is not None:
+        xh2 = (np.asarray(h, np.float64) - m2) * r2
+        s = s + back(f(dy, None) * g2, xh2, r2)
+        out.update(dgamma=(dy * xh2).sum(axis=0), dbeta=np.asarray(dy, np.float64).sum(axis=0))
+    t = s * g0
+    xh1 = (b - m1) * r1 if after else b
+    n = xh1 * ga + ca if after else b
+    out.update(s=s, t=t, dres=rscale * s, dgate=s * n, db=back(t * ga, xh1, r1) if after else t,
+               dgamma_after=(t * xh1).sum(axis=0), dbeta_after=t.sum(axis=0))
+    return out
+
+
 def quantize_rows(x):
     """(q, scale): the definition in 32-bit arithmetic, every operation rounded
     once, as the result is a whole number that depends on those roundings."""

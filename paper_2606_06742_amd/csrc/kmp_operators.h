@@ -1,7 +1,7 @@
-// Internal interface of the operators at a language model's end: layer norm,
-// products in 8-bit integers, log probabilities of tokens. Element types,
-// 16-byte vectors of them, and the launchers (norm.hip, quantized.hip,
-// logprobs.hip; arguments checked in operators_api.cpp).
+// Internal interface of the operators at a language model's end: layer norm, the
+// norms around a block, products in 8-bit integers, log probabilities of tokens.
+// Element types, 16-byte vectors of them, and the launchers (norm.hip, block.hip,
+// quantized.hip, logprobs.hip; arguments checked in operators_api.cpp).
 #pragma once
 
 #include <algorithm>
@@ -74,6 +74,50 @@ struct NormBackArgs {
 };
 int64_t norm_partials(int xtype, int64_t rows, int64_t d);
 int norm_backward(hipStream_t s, const NormBackArgs& a);
+
+// ------------------------------------------- the norms around a model's block
+struct BlockArgs {
+  int xtype, wtype;
+  bool rms, after;
+  const void* b; int64_t ldb;
+  const void* res; int64_t ldr;         // may be null
+  int64_t rows, d;
+  const void* gamma_after; const void* beta_after;  // may be null (ones, zeros)
+  const void* gate; int64_t ldg;        // may be null (ones); ldg = 0: one for all rows
+  float rscale;
+  const void* gamma; const void* beta;  // may be null
+  float eps;
+  void* h; int64_t ldh;                 // may be null
+  bool bytes;                           // y in 8 bits
+  void* y; int64_t ldy;                 // may be null
+  float* stats;                         // rows x 4, may be null
+  float* scale;
+};
+int block_forward(hipStream_t s, const BlockArgs& a);
+
+struct BlockBackArgs {
+  int xtype, wtype;
+  bool rms, after;
+  const void* dy; int64_t lddy;         // may be null
+  const void* dh; int64_t lddh;         // may be null
+  const void* b; int64_t ldb;
+  const void* h; int64_t ldh;
+  int64_t rows, d;
+  const void* gamma_after; const void* beta_after;
+  const void* gate; int64_t ldg;
+  float rscale;
+  const void* gamma;
+  const float* stats;
+  void* db; int64_t lddb;               // each output may be null
+  void* dres; int64_t lddres;
+  void* dgate; int64_t lddg;
+  void* dgamma_after; void* dbeta_after; void* dgamma; void* dbeta;
+  float* partial;                       // block_partials(..) x 4 x d
+  float* means;                         // rows x 2 (rows too long for the registers)
+};
+int64_t block_partials(int xtype, int64_t rows, int64_t d);
+bool block_long(int xtype, int64_t d);  // such rows
+int block_backward(hipStream_t s, const BlockBackArgs& a);
 
 // ------------------------------------------------- products in 8-bit integers
 struct QProductArgs {

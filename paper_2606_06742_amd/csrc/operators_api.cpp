@@ -32,6 +32,7 @@ bool float_type(int32_t t) { return t == KMP_F32 || t == KMP_BF16 || t == KMP_F1
 bool norm_types(int32_t x, int32_t w) {
   return (x >= KMP_F64 && x <= KMP_F16) && (w == x || (w == KMP_F32 && x != KMP_F64));
 }
+bool pitch_ok(int64_t ld, int64_t d) { return ld >= d && ld <= kMostLd; }
 size_t acc_bytes(int32_t t) { return t == KMP_F64 ? 8 : 4; }
 
 }  // namespace
@@ -84,6 +85,75 @@ int kmp_layer_norm_backward(void* stream, int32_t xtype, const void* dy, int64_t
     }
     NormBackArgs a{xtype, wtype, dy, lddy, x, ldx, rows, d, gamma, mean, rstd, dx, lddx, dgamma, dbeta, workspace};
     return norm_backward((hipStream_t)stream, a);
+  });
+}
+
+int kmp_block_norm(void* stream, int32_t xtype, int32_t flags, const void* b, int64_t ldb, const void* res,
+                   int64_t ldr, int64_t rows, int64_t d, int32_t wtype, const void* gamma_after,
+                   const void* beta_after, const void* gate, int64_t ldg, double rscale, const void* gamma,
+                   const void* beta, double eps, void* h, int64_t ldh, int32_t ytype, void* y, int64_t ldy,
+                   float* stats, float* scale) {
+  return guarded([&]() -> int {
+    const char* name = "kmp_block_norm";
+    if (!float_type(xtype) || !norm_types(xtype, wtype)) return refuse(name, "types of x and of the weights do not go together");
+    if (flags & ~(KMP_NORM_RMS | KMP_NORM_AFTER)) return refuse(name, "unknown flags");
+    if (y && ytype != xtype && ytype != KMP_I8) return refuse(name, "y has the type of x or 8 bits");
+    if (rows < 0 || rows > kMost || d < 1 || d > kMost || !pitch_ok(ldb, d) || (res && !pitch_ok(ldr, d)) ||
+        (h && !pitch_ok(ldh, d)) || (y && !pitch_ok(ldy, d)) || (gate && ldg != 0 && !pitch_ok(ldg, d)))
+      return refuse(name, "rows, d or a leading dimension out of range");
+    if (!(eps >= 0.0) || !std::isfinite(eps)) return refuse(name, "eps must be finite and not negative");
+    if (!std::isfinite(rscale)) return refuse(name, "rscale must be finite");
+    if (rows == 0) return KMP_OK;
+    if (!h && !y) return refuse(name, "h or y must be given");
+    if (h && h == res && ldh != ldr) return refuse(name, "h may be res with the same leading dimension only");
+    if (!b || (y && ytype == KMP_I8 && !scale)) return refuse(name, "null pointer");
+    BlockArgs a{xtype, wtype, (flags & KMP_NORM_RMS) != 0, (flags & KMP_NORM_AFTER) != 0, b, ldb, res, ldr, rows, d,
+                gamma_after, beta_after, gate, ldg, (float)rscale, gamma, beta, (float)eps, h, ldh,
+                y && ytype == KMP_I8, y, ldy, stats, scale};
+    return block_forward((hipStream_t)stream, a);
+  });
+}
+
+size_t kmp_block_norm_workspace_bytes(int32_t xtype, int64_t rows, int64_t d) {
+  if (!float_type(xtype) || rows < 0 || rows > kMost || d < 1 || d > kMost) return 0;
+  const size_t sums = (size_t)block_partials(xtype, rows, d) * 4 * (size_t)d * 4;
+  return std::max<size_t>(256, round_up((int64_t)sums, 16) + (block_long(xtype, d) ? (size_t)rows * 8 : 0));
+}
+
+int kmp_block_norm_backward(void* stream, int32_t xtype, int32_t flags, const void* dy, int64_t lddy,
+                            const void* dh, int64_t lddh, const void* b, int64_t ldb, const void* h,
+                            int64_t ldh, int64_t rows, int64_t d, int32_t wtype, const void* gamma_after,
+                            const void* beta_after, const void* gate, int64_t ldg, double rscale,
+                            const void* gamma, const float* stats, void* db, int64_t lddb, void* dres,
+                            int64_t lddres, void* dgate, int64_t lddg, void* dgamma_after,
+                            void* dbeta_after, void* dgamma, void* dbeta, void* workspace,
+                            size_t workspace_bytes) {
+  return guarded([&]() -> int {
+    const char* name = "kmp_block_norm_backward";
+    if (!float_type(xtype) || !norm_types(xtype, wtype)) return refuse(name, "types of x and of the weights do not go together");
+    if (flags & ~(KMP_NORM_RMS | KMP_NORM_AFTER)) return refuse(name, "unknown flags");
+    const bool after = (flags & KMP_NORM_AFTER) != 0, each = gate && ldg != 0;
+    if (rows < 0 || rows > kMost || d < 1 || d > kMost || !pitch_ok(ldb, d) || (dy && !(pitch_ok(lddy, d) && pitch_ok(ldh, d))) ||
+        (dh && !pitch_ok(lddh, d)) || (each && !pitch_ok(ldg, d)) || (db && !pitch_ok(lddb, d)) ||
+        (dres && !pitch_ok(lddres, d)) || (dgate && each && !pitch_ok(lddg, d)))
+      return refuse(name, "rows, d or a leading dimension out of range");
+    if (!std::isfinite(rscale)) return refuse(name, "rscale must be finite");
+    if (dgate && !gate) return refuse(name, "there is no gate for dgate");
+    if ((dgamma_after || dbeta_after) && !after) return refuse(name, "there is no norm of b without KMP_NORM_AFTER");
+    if (rows > 0 && (!b || !stats || (!dy && !dh) || (dy && !h))) return refuse(name, "null pointer");
+    const bool sums = (dgate && !each) || dgamma_after || dbeta_after || dgamma || dbeta;
+    if (!sums && !db && !dres && !dgate) return KMP_OK;
+    float* partial = sums ? static_cast<float*>(workspace) : nullptr;
+    if (sums) {
+      const size_t need = kmp_block_norm_workspace_bytes(xtype, rows, d);
+      if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15))
+        return refuse(name, "the workspace is missing, too small or not aligned to 16 bytes", KMP_EWORKSPACE);
+    }
+    const int64_t at = round_up(block_partials(xtype, rows, d) * 4 * d * 4, 16) / 4;
+    BlockBackArgs a{xtype, wtype, (flags & KMP_NORM_RMS) != 0, after, dy, lddy, dh, lddh, b, ldb, h, ldh, rows, d,
+                    gamma_after, beta_after, gate, ldg, (float)rscale, gamma, stats, db, lddb, dres, lddres, dgate, lddg,
+                    dgamma_after, dbeta_after, dgamma, dbeta, partial, partial ? partial + at : nullptr};
+    return block_backward((hipStream_t)stream, a);
   });
 }
 

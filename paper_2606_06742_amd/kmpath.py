@@ -30,6 +30,7 @@ KMP_FLAG_EAGER = 32
 KMP_WNOTEXACT = 2
 KMP_F64, KMP_F32, KMP_BF16, KMP_F16, KMP_I8 = 0, 1, 2, 3, 4
 KMP_MAX_TOP = 64
+KMP_NORM_RMS, KMP_NORM_AFTER = 1, 2
 KMP_NKC = 10
 KERNEL_CLASSES = ("gram", "panel", "panel_wy", "trail_update", "q_form", "precompute", "gemm_f",
                   "gemm_zhat", "update", "finalize")
@@ -125,6 +126,15 @@ def lib():
         L.kmp_layer_norm_backward.argtypes = [_VP, I32, _VP, I64, _VP, I64, I64, I64, I32, _VP, _VP,
                                               _VP, _VP, I64, _VP, _VP, _VP, C.c_size_t]
         L.kmp_layer_norm_backward.restype = C.c_int
+        L.kmp_block_norm.argtypes = [_VP, I32, I32, _VP, I64, _VP, I64, I64, I64, I32, _VP, _VP, _VP, I64,
+                                     C.c_double, _VP, _VP, C.c_double, _VP, I64, I32, _VP, I64, _VP, _VP]
+        L.kmp_block_norm.restype = C.c_int
+        L.kmp_block_norm_workspace_bytes.argtypes = [I32, I64, I64]
+        L.kmp_block_norm_workspace_bytes.restype = C.c_size_t
+        L.kmp_block_norm_backward.argtypes = [_VP, I32, I32, _VP, I64, _VP, I64, _VP, I64, _VP, I64, I64, I64, I32,
+                                              _VP, _VP, _VP, I64, C.c_double, _VP, _VP, _VP, I64, _VP, I64, _VP, I64,
+                                              _VP, _VP, _VP, _VP, _VP, C.c_size_t]
+        L.kmp_block_norm_backward.restype = C.c_int
         L.kmp_quantize_rows.argtypes = [_VP, I32, _VP, I64, I64, I64, _VP, I64, _VP]
         L.kmp_quantize_rows.restype = C.c_int
         L.kmp_quantized_product.argtypes = [_VP, _VP, I64, _VP, I64, _VP, I64, _VP, I64, I64, _VP,
@@ -152,7 +162,8 @@ EXPORTED = ("kmp_default_spec", "kmp_workspace_bytes", "kmp_fit_path", "kmp_make
             "kmp_rbf_gram", "kmp_rbf_gram_noalloc", "kmp_tridiag", "kmp_band_reduce",
             "kmp_path_step",
             "kmp_dgemm_grouped", "kmp_layer_norm", "kmp_layer_norm_workspace_bytes",
-            "kmp_layer_norm_backward", "kmp_quantize_rows", "kmp_quantized_product",
+            "kmp_layer_norm_backward", "kmp_block_norm", "kmp_block_norm_workspace_bytes",
+            "kmp_block_norm_backward", "kmp_quantize_rows", "kmp_quantized_product",
             "kmp_token_logprobs", "kmp_token_logprobs_workspace_bytes",
             "kmp_token_logprobs_backward", "kmp_strerror", "kmp_version", "kmp_kernel_class_name")
 KMP_BAND = 16
@@ -406,6 +417,93 @@ def kmp_layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspa
         _vector(mean, "mean", rows, sd, on), _vector(rstd, "rstd", rows, sd, on), dxp, lddx,
         _vector(dgamma, "dgamma", d, wd, on), _vector(dbeta, "dbeta", d, wd, on), wsp, wsb),
         allow_maxiter=False)
+
+
+def _gate(t, name, rows, d, xdtype, wdtype, on):
+    """(pointer, leading dimension) of a gate: (d) of the weights' type, leading
+    dimension 0, or (rows, d) of x's type; None stays None."""
+    if t is None:
+        return None, 0
+    if t.dim() == 2:
+        p, _, _, ld = _matrix(t, name, rows, d, xdtype, on)
+        return p, max(ld, d)
+    return _vector(t, name, d, wdtype, on), 0
+
+
+def _block_weights(x, *weights):
+    """The weights' type: the first given one's, else x's."""
+    return next((t.dtype for t in weights if t is not None and t.dim() == 1), x.dtype)
+
+
+def kmp_block_norm(b, res, h, y, eps, gamma_after=None, beta_after=None, gate=None, gamma=None, beta=None,
+                   rscale=1.0, after=True, rms=False, stats=None, scale=None, stream=None) -> None:
+    """h = rscale res + gate n and y = N(h; gamma, beta), n = N(b; gamma_after,
+    beta_after) with `after`, else b; N the layer norm or, with `rms`, the norm by
+    the root mean square. b, res, h (rows, d) of one type, y of that type or int8
+    with the rows' scales in `scale`; res, h or y may be None; h may be res. The
+    weights (d) and a gate (d) are of b's type or float32, a gate (rows, d) of b's;
+    stats (rows, 4) float32 takes what the backward reads."""
+    bp, rows, d, ldb = _matrix(b, "b")
+    on, sp = _place(b, "b", stream)
+    rp = hp = yp = None
+    ldr = ldh = ldy = d
+    if res is not None:
+        rp, _, _, ldr = _matrix(res, "res", rows, d, b.dtype, on)
+    if h is not None:
+        hp, _, _, ldh = _matrix(h, "h", rows, d, b.dtype, on)
+    yt = _type(b.dtype, "b")
+    if y is not None:
+        yp, _, _, ldy = _matrix(y, "y", rows, d, None, on)
+        yt = _type(y.dtype, "y")
+    wd = _block_weights(b, gamma_after, beta_after, gamma, beta, gate)
+    gp, ldg = _gate(gate, "gate", rows, d, b.dtype, wd, on)
+    import torch
+    f = torch.float32
+    _check(lib().kmp_block_norm(
+        sp, _type(b.dtype, "b"), (KMP_NORM_RMS if rms else 0) | (KMP_NORM_AFTER if after else 0), bp, ldb, rp, ldr,
+        rows, d, _type(wd, "gamma"), _vector(gamma_after, "gamma_after", d, wd, on),
+        _vector(beta_after, "beta_after", d, wd, on), gp, ldg, float(rscale), _vector(gamma, "gamma", d, wd, on),
+        _vector(beta, "beta", d, wd, on), float(eps), hp, ldh, yt, yp, ldy,
+        _vector(stats, "stats", 4 * rows, f, on), _vector(scale, "scale", rows, f, on)), allow_maxiter=False)
+
+
+def kmp_block_norm_workspace_bytes(rows: int, d: int, dtype) -> int:
+    return int(lib().kmp_block_norm_workspace_bytes(_type(dtype, "b"), int(rows), int(d)))
+
+
+def kmp_block_norm_backward(dy, dh, b, h, stats, db, dres, gamma_after=None, beta_after=None, gate=None, gamma=None,
+                            rscale=1.0, after=True, rms=False, dgate=None, dgamma_after=None, dbeta_after=None,
+                            dgamma=None, dbeta=None, workspace=None, stream=None) -> None:
+    """Gradients of kmp_block_norm from dy and dh (rows, d), the gradients of y and
+    of h (one may be None): db and dres (rows, d) of b's type, dgate of the gate's
+    shape, dgamma_after, dbeta_after, dgamma, dbeta (d) of the weights' type; each may
+    be None. h and stats are the forward call's (h may be None without dy). The
+    workspace has kmp_block_norm_workspace_bytes(rows, d, b.dtype) bytes."""
+    import torch
+    bp, rows, d, ldb = _matrix(b, "b")
+    on, sp = _place(b, "b", stream)
+
+    def matrix(t, name):
+        if t is None:
+            return None, d
+        p, _, _, ld = _matrix(t, name, rows, d, b.dtype, on)
+        return p, ld
+
+    (dyp, lddy), (dhp, lddh), (hp, ldh) = matrix(dy, "dy"), matrix(dh, "dh"), matrix(h, "h")
+    (dbp, lddb), (drp, lddr) = matrix(db, "db"), matrix(dres, "dres")
+    wd = _block_weights(b, gamma_after, beta_after, gamma, gate, dgate, dgamma_after, dbeta_after, dgamma, dbeta)
+    gp, ldg = _gate(gate, "gate", rows, d, b.dtype, wd, on)
+    if gate is not None and dgate is not None and dgate.dim() != gate.dim():
+        _refuse("dgate has the shape of the gate")
+    dgp, lddg = _gate(dgate, "dgate", rows, d, b.dtype, wd, on)
+    wsp, wsb = _workspace(workspace, on)
+    v = lambda t, name: _vector(t, name, d, wd, on)  # noqa: E731
+    _check(lib().kmp_block_norm_backward(
+        sp, _type(b.dtype, "b"), (KMP_NORM_RMS if rms else 0) | (KMP_NORM_AFTER if after else 0), dyp, lddy, dhp, lddh,
+        bp, ldb, hp, ldh, rows, d, _type(wd, "gamma"), v(gamma_after, "gamma_after"), v(beta_after, "beta_after"), gp, ldg,
+        float(rscale), v(gamma, "gamma"), _vector(stats, "stats", 4 * rows, torch.float32, on), dbp, lddb, drp, lddr,
+        dgp, lddg, v(dgamma_after, "dgamma_after"), v(dbeta_after, "dbeta_after"), v(dgamma, "dgamma"),
+        v(dbeta, "dbeta"), wsp, wsb), allow_maxiter=False)
 
 
 def kmp_quantize_rows(x, q, scale, stream=None) -> None:
