@@ -329,8 +329,8 @@ int kmp_dgemm_grouped(void* stream, int32_t G, int32_t M, int32_t N, int32_t K,
 
 /* ------------------------------------------------------------------------
  * Operators at a language model's end: the layer norm of its hidden states,
- * the 8-bit product with its vocabulary head, and the log probabilities of its
- * tokens. A kernel machine's features often come from there (hidden states;
+ * the norms around its blocks, the 8-bit product with its vocabulary head, the log
+ * probabilities of its tokens and their choice. A kernel machine's features often come from there (hidden states;
  * log probability and entropy of an answer's tokens). Their gradients train the
  * model's end itself: the path above gives none with respect to its features.
  * Unlike the entry points above they work in 16 or 32 bits (sums and statistics
@@ -493,6 +493,38 @@ int kmp_token_logprobs_backward(void* stream, int32_t type, const void* logits, 
                                 int64_t ldl, int32_t token_bits, const void* tokens, const float* stats,
                                 const float* entropy, const float* dlogp, const float* dentropy,
                                 void* dlogits, int64_t ldd);
+
+/* Bytes of DEVICE workspace of kmp_sample_tokens (at least 256); 0: bad arguments.
+ * The size does not fall as T or V grows.                                    */
+size_t kmp_sample_tokens_workspace_bytes(int64_t T, int64_t V);
+
+/* Tokens drawn from the rows of logits (DEVICE, T x V; KMP_F32, KMP_BF16 or
+ * KMP_F16) with given random numbers. With m the row's maximum, the weights w_j =
+ * exp((x_j - m) / temperature) and the order of the tokens (logit descending, equal
+ * ones by the lowest index first) there are kept
+ *   the first top_k tokens,
+ *   of these the shortest run whose weights' sum reaches top_p times the sum of all
+ *   of these (one token at least),
+ *   of these the tokens with w >= min_p (the first one has w = 1),
+ * and drawn is the first kept token, by index, at which the running sum of the kept
+ * weights exceeds u times their total Z.
+ *   u            DEVICE [T], in [0, 1) (below 0 as 0; from 1 on the last kept token
+ *                that has a weight)
+ *   temperature  DEVICE [T]; NULL: 1; from 0 down: the first token of the order
+ *   top_k        DEVICE [T], int32; NULL, from 0 down or V and more: all
+ *   top_p        DEVICE [T]; NULL or 1 and more: all; from 0 down: one token
+ *   min_p        DEVICE [T]; NULL or from 0 down: all; above 1 as 1
+ *   tokens       DEVICE [T], int32 or int64 (token_bits 32 or 64)
+ *   logp         DEVICE [T], log(w / Z) of the drawn token; may be NULL
+ *   workspace    DEVICE, 16-byte aligned
+ * Each row has choices of its own. Weights and sums are in 64 bits, in a fixed order:
+ * the same call draws the same tokens. A logit of -inf has w = 0 and is not drawn. A
+ * row of nothing but -inf has token -1 and logp -inf; a row with a NaN or +inf, or
+ * with a NaN among its choices, token -1 and logp NaN.                        */
+int kmp_sample_tokens(void* stream, int32_t type, const void* logits, int64_t T, int64_t V, int64_t ldl,
+                      const float* u, const float* temperature, const int32_t* top_k, const float* top_p,
+                      const float* min_p, int32_t token_bits, void* tokens, float* logp, void* workspace,
+                      size_t workspace_bytes);
 
 /* Message for a return code, or the last HIP error text for KMP_EHIP. */
 const char* kmp_strerror(int code);

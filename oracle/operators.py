@@ -1,6 +1,7 @@
 """The operators at a language model's end in numpy, 64 bits, straight from
 their definitions: layer norm and its gradients, rows in 8 bits and their
-product, log probabilities of tokens with entropy, alternatives and gradient."""
+product, the norms around a block, log probabilities of tokens with entropy,
+alternatives and gradient, tokens drawn from given random numbers."""
 from __future__ import annotations
 
 import numpy as np
@@ -146,3 +147,52 @@ def token_logprobs_backward(x, tokens, stats, dlogp=None, entropy=None, dentropy
             dx[t, live] -= dlogp[t] * p
             dx[t, k] += dlogp[t]
     return dx
+
+
+def sample_tokens(x, u, temperature=None, top_k=None, top_p=None, min_p=None):
+    """(tokens, logp, margin): tokens drawn from the rows of x as defined. margin is how
+    near, relative to the sums, a comparison came that decides the token."""
+    x = np.asarray(x, dtype=np.float64)
+    T, V = x.shape
+    tokens, logp, margin = np.full(T, -1, np.int64), np.full(T, np.nan), np.full(T, np.inf)
+    at = lambda a, t, none: none if a is None else float(a[t])
+    for t in range(T):
+        r = x[t]
+        c = at(temperature, t, 1.0), at(top_p, t, 1.0), at(min_p, t, 0.0), float(u[t])
+        k = V if top_k is None or top_k[t] <= 0 else min(int(top_k[t]), V)
+        if np.isnan(c).any() or np.isnan(r).any() or np.any(r == np.inf):
+            continue
+        if np.all(r == -np.inf):
+            logp[t] = -np.inf
+            continue
+        order = np.lexsort((np.arange(V), -r))
+        if c[0] <= 0:
+            tokens[t], logp[t] = order[0], 0.0
+            continue
+        w = np.zeros(V)
+        live = r > -np.inf
+        with np.errstate(under="ignore"):
+            w[live] = np.exp((r[live] - r.max()) / c[0])
+        order = order[:k]
+        if c[1] < 1:
+            sums = np.cumsum(w[order].astype(np.longdouble))
+            reach = c[1] * sums[-1]
+            n = int(np.searchsorted(sums, reach, side="left")) + 1 if c[1] > 0 else 1
+            if 0 < c[1]:
+                margin[t] = min(margin[t], float(np.abs(sums - reach).min() / sums[-1]))
+            order = order[:min(n, len(order))]
+        if c[2] > 0:
+            floor = min(c[2], 1.0)
+            near = np.abs(w[order] / floor - 1)
+            near = near[w[order] != floor]
+            margin[t] = min(margin[t], float(near.min()) if near.size else np.inf)
+            order = order[w[order] >= floor]
+        kept = np.sort(order)
+        sums = np.cumsum(w[kept].astype(np.longdouble))
+        goal = min(max(c[3], 0.0), 1.0) * sums[-1]
+        over = np.flatnonzero(sums > goal)
+        i = int(over[0]) if over.size else int(np.flatnonzero(w[kept] > 0)[-1])
+        if goal > 0:
+            margin[t] = min(margin[t], float(np.abs(sums - goal)[:-1].min() / sums[-1]) if len(sums) > 1 else np.inf)
+        tokens[t], logp[t] = kept[i], np.log(w[kept[i]]) - float(np.log(sums[-1]))
+    return tokens, logp, margin

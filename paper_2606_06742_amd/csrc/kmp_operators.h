@@ -151,4 +151,17 @@ struct LogprobBackArgs {
 };
 int token_logprobs_backward(hipStream_t s, const LogprobBackArgs& a);
 
+// ----------------------------------------------------------- choice of tokens
+struct SampleArgs {
+  int type;
+  const void* logits; int64_t T, V, ld;
+  const float* u;
+  const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p;  // each may be null
+  bool wide; void* tokens;              // int64 tokens
+  float* logp;                          // may be null
+  void* workspace;
+};
+size_t sample_workspace(int64_t T, int64_t V);
+int sample_tokens(hipStream_t s, const SampleArgs& a);
+
 }  // namespace kmp

@@ -232,4 +232,28 @@ int kmp_token_logprobs_backward(void* stream, int32_t type, const void* logits, 
   });
 }
 
+size_t kmp_sample_tokens_workspace_bytes(int64_t T, int64_t V) {
+  if (T < 0 || T > kMost || V < 1 || V > kMost) return 0;
+  return sample_workspace(T, V);
+}
+
+int kmp_sample_tokens(void* stream, int32_t type, const void* logits, int64_t T, int64_t V, int64_t ldl,
+                      const float* u, const float* temperature, const int32_t* top_k, const float* top_p,
+                      const float* min_p, int32_t token_bits, void* tokens, float* logp, void* workspace,
+                      size_t workspace_bytes) {
+  return guarded([&]() -> int {
+    const char* name = "kmp_sample_tokens";
+    if (!float_type(type)) return refuse(name, "logits must be of type KMP_F32, KMP_BF16 or KMP_F16");
+    if (T < 0 || T > kMost || V < 1 || V > kMost || !pitch_ok(ldl, V))
+      return refuse(name, "T, V or the leading dimension out of range");
+    if (token_bits != 32 && token_bits != 64) return refuse(name, "tokens have 32 or 64 bits");
+    if (T == 0) return KMP_OK;
+    if (!logits || !u || !tokens) return refuse(name, "null pointer");
+    if (!workspace || workspace_bytes < sample_workspace(T, V) || (reinterpret_cast<uintptr_t>(workspace) & 15))
+      return refuse(name, "the workspace is missing, too small or not aligned to 16 bytes", KMP_EWORKSPACE);
+    SampleArgs a{type, logits, T, V, ldl, u, temperature, top_k, top_p, min_p, token_bits == 64, tokens, logp, workspace};
+    return sample_tokens((hipStream_t)stream, a);
+  });
+}
+
 }  // extern "C"

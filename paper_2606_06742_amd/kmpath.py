@@ -148,6 +148,11 @@ def lib():
         L.kmp_token_logprobs_backward.argtypes = [_VP, I32, _VP, I64, I64, I64, I32, _VP, _VP, _VP,
                                                   _VP, _VP, _VP, I64]
         L.kmp_token_logprobs_backward.restype = C.c_int
+        L.kmp_sample_tokens_workspace_bytes.argtypes = [I64, I64]
+        L.kmp_sample_tokens_workspace_bytes.restype = C.c_size_t
+        L.kmp_sample_tokens.argtypes = [_VP, I32, _VP, I64, I64, I64, _VP, _VP, _VP, _VP, _VP, I32, _VP, _VP, _VP,
+                                        C.c_size_t]
+        L.kmp_sample_tokens.restype = C.c_int
         L.kmp_strerror.argtypes = [C.c_int]
         L.kmp_strerror.restype = C.c_char_p
         L.kmp_version.argtypes = []
@@ -165,7 +170,8 @@ EXPORTED = ("kmp_default_spec", "kmp_workspace_bytes", "kmp_fit_path", "kmp_make
             "kmp_layer_norm_backward", "kmp_block_norm", "kmp_block_norm_workspace_bytes",
             "kmp_block_norm_backward", "kmp_quantize_rows", "kmp_quantized_product",
             "kmp_token_logprobs", "kmp_token_logprobs_workspace_bytes",
-            "kmp_token_logprobs_backward", "kmp_strerror", "kmp_version", "kmp_kernel_class_name")
+            "kmp_token_logprobs_backward", "kmp_sample_tokens", "kmp_sample_tokens_workspace_bytes",
+            "kmp_strerror", "kmp_version", "kmp_kernel_class_name")
 KMP_BAND = 16
 
 
@@ -574,6 +580,32 @@ def kmp_token_logprobs_backward(logits, tokens, stats, dlogp, dlogits, entropy=N
         sp, _type(logits.dtype, "logits"), lp, T, V, ldl, bits, tp,
         _vector(stats, "stats", 2 * T, f, on), _vector(entropy, "entropy", T, f, on), _vector(dlogp, "dlogp", T, f, on),
         _vector(dentropy, "dentropy", T, f, on), dp, ldd), allow_maxiter=False)
+
+
+def kmp_sample_tokens_workspace_bytes(T: int, V: int) -> int:
+    return int(lib().kmp_sample_tokens_workspace_bytes(int(T), int(V)))
+
+
+def kmp_sample_tokens(logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, logp=None,
+                      workspace=None, stream=None) -> None:
+    """Tokens (T; int32 or int64) drawn from the rows of logits (T, V) with the
+    random numbers u (T) float32 in [0, 1): kept are the first top_k (T) int32 in
+    the order of the logits, of these the shortest run that has top_p (T) of their
+    weight, of these the tokens with at least min_p (T) of the first one's weight;
+    weights at the temperature (T). Each of these may be None; logp (T) float32 takes
+    the drawn tokens' log probabilities among the kept ones. The workspace has
+    kmp_sample_tokens_workspace_bytes(T, V) bytes."""
+    import torch
+    lp, T, V, ldl = _matrix(logits, "logits")
+    on, sp = _place(logits, "logits", stream)
+    bits, tp = _tokens(tokens, T, on)
+    f = torch.float32
+    wsp, wsb = _workspace(workspace, on)
+    _check(lib().kmp_sample_tokens(
+        sp, _type(logits.dtype, "logits"), lp, T, V, ldl, _vector(u, "u", T, f, on),
+        _vector(temperature, "temperature", T, f, on), _vector(top_k, "top_k", T, torch.int32, on),
+        _vector(top_p, "top_p", T, f, on), _vector(min_p, "min_p", T, f, on), bits, tp, _vector(logp, "logp", T, f, on),
+        wsp, wsb), allow_maxiter=False)
 
 
 def kmp_fit_path(stream, spec, X, y, sigmas, taus, lambdas, fold_id, V, workspace, ws_bytes,
