@@ -452,6 +452,48 @@ int kmp_quantized_product(void* stream, const int8_t* x, int64_t ldx, const floa
                           const int8_t* w, int64_t ldw, const float* wscale, int64_t N, int64_t K,
                           const float* bias, int32_t otype, void* out, int64_t ldo);
 
+/* Activations of kmp_dense_product. */
+#define KMP_ACT_NONE 0
+#define KMP_ACT_RELU 1                 /* max(z, 0) */
+#define KMP_ACT_GELU 2                 /* z (1 + erf(z / sqrt 2)) / 2 */
+#define KMP_ACT_GELU_TANH 3            /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+#define KMP_ACT_SILU 4                 /* z / (1 + exp(-z)) */
+
+/* Product with bias, activation and residual in its epilogue:
+ *   z[m][n] = sum_k x[m][k] w[n][k] + bias[n],  out = act(z) + residual
+ * x DEVICE M x K and w DEVICE N x K (one row per output channel) of type
+ * KMP_F32, KMP_BF16 or KMP_F16; bias DEVICE [N] of type btype (x's type or
+ * KMP_F32) or NULL; out and residual (NULL: none) DEVICE M x N of type otype (x's
+ * type or KMP_F32); zout DEVICE M x N of x's type or NULL: z, which the backward
+ * pass reads. Sums and epilogue are in 32 bits, out and zout are each rounded once.
+ * out may be residual with the same leading dimension. Rows that start at multiples
+ * of 16 bytes are read fastest. K = 0 gives act(bias) + residual. K <= 2^28; at
+ * most 2^23 tiles of 64 x 64 (KMP_EINVAL above).                              */
+int kmp_dense_product(void* stream, int32_t type, const void* x, int64_t ldx, int64_t M, const void* w,
+                      int64_t ldw, int64_t N, int64_t K, int32_t btype, const void* bias, int32_t act,
+                      int32_t otype, const void* residual, int64_t ldr, void* out, int64_t ldo, void* zout,
+                      int64_t ldz);
+
+/* Bytes of DEVICE workspace of kmp_dense_product_backward (at least 256); 0: bad
+ * arguments. The size does not fall as M, N or K grows.                      */
+size_t kmp_dense_product_workspace_bytes(int32_t type, int64_t M, int64_t N, int64_t K);
+
+/* Gradients of kmp_dense_product from dout (DEVICE, M x N, type): with dz = dout
+ * act'(z) (act'(0) = 0 for KMP_ACT_RELU)
+ *   dx[m][k] = sum_n dz[m][n] w[n][k]   (M x K, type)
+ *   dw[n][k] = sum_m dz[m][n] x[m][k]   (N x K, type)
+ *   dbias[n] = sum_m dz[m][n]           ([N], btype)
+ * (the residual's gradient is dout). z as the forward call wrote it (may be NULL
+ * with KMP_ACT_NONE). dx, dw and dbias may each be NULL, and x without dw, w
+ * without dx. In 16 bits dz is rounded to type for the products, as their operands
+ * are, but not for dbias. Sums are in 32 bits and in a fixed order: the same call
+ * gives the same bits. M = 0 gives dw = dbias = 0, N = 0 dx = 0. M, N and K <= 2^28.
+ * The workspace is aligned to 16 bytes.                                       */
+int kmp_dense_product_backward(void* stream, int32_t type, const void* dout, int64_t lddo, int64_t M, int64_t N,
+                               int64_t K, int32_t act, const void* z, int64_t ldz, const void* x, int64_t ldx,
+                               const void* w, int64_t ldw, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                               int32_t btype, void* dbias, void* workspace, size_t workspace_bytes);
+
 /* Most alternatives per token. */
 #define KMP_MAX_TOP 64
 

@@ -1,6 +1,6 @@
 """The operators at a language model's end in numpy, 64 bits, straight from
 their definitions: layer norm and its gradients, rows in 8 bits and their
-product, the norms around a block, log probabilities of tokens with entropy,
+product, products with an activation, the norms around a block, log probabilities of tokens with entropy,
 alternatives and gradient, tokens drawn from given random numbers."""
 from __future__ import annotations
 
@@ -93,6 +93,43 @@ def quantized_product(xq, xscale, wq, wscale, bias=None):
     y = np.asarray(xq, np.float64) @ np.asarray(wq, np.float64).T        # whole numbers below 2^53: exact
     y = y * np.asarray(xscale, np.float64)[:, None] * np.asarray(wscale, np.float64)[None, :]
     return y if bias is None else y + np.asarray(bias, np.float64)
+
+
+def activation(z, act):
+    """(act(z), act'(z))."""
+    from scipy.special import erf
+    z = np.asarray(z, np.float64)
+    if act == "relu":
+        return np.maximum(z, 0.0), (z > 0).astype(np.float64)
+    if act == "gelu":
+        p = 0.5 * (1.0 + erf(z / np.sqrt(2.0)))
+        return z * p, p + z * np.exp(-0.5 * z * z) / np.sqrt(2.0 * np.pi)
+    if act == "gelu_tanh":
+        c = np.sqrt(2.0 / np.pi)
+        t = np.tanh(c * (z + 0.044715 * z ** 3))
+        return 0.5 * z * (1.0 + t), 0.5 * (1.0 + t) + 0.5 * z * (1.0 - t * t) * c * (1.0 + 3 * 0.044715 * z * z)
+    if act == "silu":
+        with np.errstate(over="ignore"):
+            p = 1.0 / (1.0 + np.exp(-z))
+        return z * p, p * (1.0 + z * (1.0 - p))
+    return z, np.ones_like(z)
+
+
+def dense_product(x, w, bias=None, act="none", residual=None):
+    """(out, z): out = act(z) + residual, z = x w' + bias."""
+    z = np.asarray(x, np.float64) @ np.asarray(w, np.float64).T
+    if bias is not None:
+        z = z + np.asarray(bias, np.float64)
+    y = activation(z, act)[0]
+    return (y if residual is None else y + np.asarray(residual, np.float64)), z
+
+
+def dense_product_backward(dout, x, w, z, act="none"):
+    """(dx, dw, dbias, dz) at the given z."""
+    dz = np.asarray(dout, np.float64)
+    if act != "none":
+        dz = dz * activation(z, act)[1]
+    return dz @ np.asarray(w, np.float64), dz.T @ np.asarray(x, np.float64), dz.sum(axis=0), dz
 
 
 def token_logprobs(x, tokens, top=0):

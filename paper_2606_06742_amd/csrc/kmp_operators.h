@@ -1,7 +1,8 @@
 // Internal interface of the operators at a language model's end: layer norm, the
-// norms around a block, products in 8-bit integers, log probabilities of tokens.
-// Element types, 16-byte vectors of them, and the launchers (norm.hip, block.hip,
-// quantized.hip, logprobs.hip; arguments checked in operators_api.cpp).
+// norms around a block, products in 8-bit integers and in 16 and 32 bits, log
+// probabilities of tokens and their choice. Element types, 16-byte vectors of them, and
+// the launchers (norm.hip, block.hip, quantized.hip, linear.hip, logprobs.hip,
+// sample.hip; arguments checked in operators_api.cpp).
 #pragma once
 
 #include <algorithm>
@@ -128,6 +129,36 @@ struct QProductArgs {
   int otype; void* out; int64_t ldo;
 };
 int quantized_product(hipStream_t s, const QProductArgs& a);
+
+// ------------------------------ products with bias, activation and residual
+struct DenseArgs {
+  int type;
+  const void* x; int64_t ldx;           // M x K
+  const void* w; int64_t ldw;           // N x K
+  int64_t M, N, K;
+  int btype; const void* bias;          // N, may be null
+  int act, otype;
+  const void* residual; int64_t ldr;    // may be null
+  void* out; int64_t ldo;
+  void* z; int64_t ldz;                 // may be null
+};
+int dense_product(hipStream_t s, const DenseArgs& a);
+
+struct DenseBackArgs {
+  int type;
+  const void* dout; int64_t lddo;
+  int64_t M, N, K;
+  int act;
+  const void* z; int64_t ldz;
+  const void* x; int64_t ldx;
+  const void* w; int64_t ldw;
+  void* dx; int64_t lddx;               // each output may be null
+  void* dw; int64_t lddw;
+  int btype; void* dbias;
+  void* workspace;
+};
+size_t dense_workspace(int type, int64_t M, int64_t N, int64_t K);
+int dense_backward(hipStream_t s, const DenseBackArgs& a);
 
 // ------------------------------------------------- log probabilities of tokens
 constexpr int kMaxTop = KMP_MAX_TOP;

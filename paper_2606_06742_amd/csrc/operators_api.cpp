@@ -25,6 +25,7 @@ int guarded(F&& f) noexcept {
 }
 
 constexpr int64_t kMost = INT32_MAX;              // rows, columns, tokens
+constexpr int64_t kMostDepth = (int64_t)1 << 28;  // elements that a product sums over
 constexpr int64_t kMostLd = (int64_t)1 << 40;     // elements between two rows
 
 bool float_type(int32_t t) { return t == KMP_F32 || t == KMP_BF16 || t == KMP_F16; }
@@ -186,6 +187,60 @@ int kmp_quantized_product(void* stream, const int8_t* x, int64_t ldx, const floa
     if ((K > 0 && (!x || !w)) || !xscale || !wscale || !out) return refuse(name, "null pointer");
     QProductArgs a{x, ldx, xscale, w, ldw, wscale, bias, M, N, K, otype, out, ldo};
     return quantized_product((hipStream_t)stream, a);
+  });
+}
+
+int kmp_dense_product(void* stream, int32_t type, const void* x, int64_t ldx, int64_t M, const void* w,
+                      int64_t ldw, int64_t N, int64_t K, int32_t btype, const void* bias, int32_t act,
+                      int32_t otype, const void* residual, int64_t ldr, void* out, int64_t ldo, void* zout,
+                      int64_t ldz) {
+  return guarded([&]() -> int {
+    const char* name = "kmp_dense_product";
+    if (!float_type(type)) return refuse(name, "x and w must be of type KMP_F32, KMP_BF16 or KMP_F16");
+    if ((btype != type && btype != KMP_F32) || (otype != type && otype != KMP_F32))
+      return refuse(name, "bias and output have the type of x or KMP_F32");
+    if (act < KMP_ACT_NONE || act > KMP_ACT_SILU) return refuse(name, "unknown activation");
+    if (M < 0 || N < 0 || K < 0 || M > kMost || N > kMost || K > kMostDepth || !pitch_ok(ldx, K) || !pitch_ok(ldw, K) ||
+        !pitch_ok(ldo, N) || (residual && !pitch_ok(ldr, N)) || (zout && !pitch_ok(ldz, N)))
+      return refuse(name, "a size or a leading dimension out of range");
+    if (M == 0 || N == 0) return KMP_OK;
+    if (ceil_div(M, 64) * ceil_div(N, 64) > (int64_t)1 << 23) return refuse(name, "more than 2^23 tiles of 64 x 64");
+    if ((K > 0 && (!x || !w)) || !out) return refuse(name, "null pointer");
+    if (out == residual && ldo != ldr) return refuse(name, "out may be residual with the same leading dimension only");
+    DenseArgs a{type, x, ldx, w, ldw, M, N, K, btype, bias, act, otype, residual, ldr, out, ldo, zout, ldz};
+    return dense_product((hipStream_t)stream, a);
+  });
+}
+
+size_t kmp_dense_product_workspace_bytes(int32_t type, int64_t M, int64_t N, int64_t K) {
+  if (!float_type(type) || M < 0 || N < 0 || K < 0 || M > kMostDepth || N > kMostDepth || K > kMostDepth) return 0;
+  return dense_workspace(type, M, N, K);
+}
+
+int kmp_dense_product_backward(void* stream, int32_t type, const void* dout, int64_t lddo, int64_t M, int64_t N,
+                               int64_t K, int32_t act, const void* z, int64_t ldz, const void* x, int64_t ldx,
+                               const void* w, int64_t ldw, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                               int32_t btype, void* dbias, void* workspace, size_t workspace_bytes) {
+  return guarded([&]() -> int {
+    const char* name = "kmp_dense_product_backward";
+    if (!float_type(type)) return refuse(name, "x and w must be of type KMP_F32, KMP_BF16 or KMP_F16");
+    if (btype != type && btype != KMP_F32) return refuse(name, "dbias has the type of x or KMP_F32");
+    if (act < KMP_ACT_NONE || act > KMP_ACT_SILU) return refuse(name, "unknown activation");
+    if (M < 0 || N < 0 || K < 0 || M > kMostDepth || N > kMostDepth || K > kMostDepth || !pitch_ok(lddo, N) ||
+        (act != KMP_ACT_NONE && !pitch_ok(ldz, N)) || (dw && (!pitch_ok(ldx, K) || !pitch_ok(lddw, K))) ||
+        (dx && (!pitch_ok(ldw, K) || !pitch_ok(lddx, K))))
+      return refuse(name, "a size or a leading dimension out of range");
+    const int64_t most = (int64_t)1 << 23;
+    if (ceil_div(M, 64) * ceil_div(N, 64) > most || (dx && ceil_div(M, 64) * ceil_div(K, 64) > most) ||
+        (dw && ceil_div(N, 64) * ceil_div(K, 64) > most))
+      return refuse(name, "more than 2^23 tiles of 64 x 64");
+    if (!dx && !dw && !dbias) return KMP_OK;
+    if (M > 0 && N > 0 && (!dout || (act != KMP_ACT_NONE && !z))) return refuse(name, "null pointer");
+    if (M > 0 && N > 0 && K > 0 && ((dw && !x) || (dx && !w))) return refuse(name, "null pointer");
+    if (!workspace || workspace_bytes < dense_workspace(type, M, N, K) || (reinterpret_cast<uintptr_t>(workspace) & 15))
+      return refuse(name, "the workspace is missing, too small or not aligned to 16 bytes", KMP_EWORKSPACE);
+    DenseBackArgs a{type, dout, lddo, M, N, K, act, z, ldz, x, ldx, w, ldw, dx, lddx, dw, lddw, btype, dbias, workspace};
+    return dense_backward((hipStream_t)stream, a);
   });
 }
 

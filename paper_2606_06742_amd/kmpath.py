@@ -34,6 +34,7 @@ KMP_NORM_RMS, KMP_NORM_AFTER = 1, 2
 KMP_NKC = 10
 KERNEL_CLASSES = ("gram", "panel", "panel_wy", "trail_update", "q_form", "precompute", "gemm_f",
                   "gemm_zhat", "update", "finalize")
+ACT_CODES = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 LOSS_CODES = {"hinge": KMP_HINGE, "logistic": KMP_LOGISTIC, "check": KMP_CHECK}
 
 
@@ -140,6 +141,14 @@ def lib():
         L.kmp_quantized_product.argtypes = [_VP, _VP, I64, _VP, I64, _VP, I64, _VP, I64, I64, _VP,
                                             I32, _VP, I64]
         L.kmp_quantized_product.restype = C.c_int
+        L.kmp_dense_product.argtypes = [_VP, I32, _VP, I64, I64, _VP, I64, I64, I64, I32, _VP, I32, I32, _VP, I64, _VP,
+                                        I64, _VP, I64]
+        L.kmp_dense_product.restype = C.c_int
+        L.kmp_dense_product_workspace_bytes.argtypes = [I32, I64, I64, I64]
+        L.kmp_dense_product_workspace_bytes.restype = C.c_size_t
+        L.kmp_dense_product_backward.argtypes = [_VP, I32, _VP, I64, I64, I64, I64, I32, _VP, I64, _VP, I64, _VP, I64,
+                                                 _VP, I64, _VP, I64, I32, _VP, _VP, C.c_size_t]
+        L.kmp_dense_product_backward.restype = C.c_int
         L.kmp_token_logprobs_workspace_bytes.argtypes = [I64, I64, I32]
         L.kmp_token_logprobs_workspace_bytes.restype = C.c_size_t
         L.kmp_token_logprobs.argtypes = [_VP, I32, _VP, I64, I64, I64, I32, _VP, _VP, _VP, _VP, I32,
@@ -169,6 +178,7 @@ EXPORTED = ("kmp_default_spec", "kmp_workspace_bytes", "kmp_fit_path", "kmp_make
             "kmp_dgemm_grouped", "kmp_layer_norm", "kmp_layer_norm_workspace_bytes",
             "kmp_layer_norm_backward", "kmp_block_norm", "kmp_block_norm_workspace_bytes",
             "kmp_block_norm_backward", "kmp_quantize_rows", "kmp_quantized_product",
+            "kmp_dense_product", "kmp_dense_product_workspace_bytes", "kmp_dense_product_backward",
             "kmp_token_logprobs", "kmp_token_logprobs_workspace_bytes",
             "kmp_token_logprobs_backward", "kmp_sample_tokens", "kmp_sample_tokens_workspace_bytes",
             "kmp_strerror", "kmp_version", "kmp_kernel_class_name")
@@ -536,6 +546,66 @@ def kmp_quantized_product(xq, xscale, wq, wscale, out, bias=None, stream=None) -
         sp, xp, ldx, _vector(xscale, "xscale", M, f, on), M, wp, ldw,
         _vector(wscale, "wscale", N, f, on), N, K, _vector(bias, "bias", N, f, on), _type(out.dtype, "out"), op,
         ldo), allow_maxiter=False)
+
+
+def _act(act) -> int:
+    code = ACT_CODES.get(act)
+    if code is None:
+        _refuse(f"activation {act!r} is not one of {', '.join(ACT_CODES)}")
+    return code
+
+
+def kmp_dense_product(x, w, out, bias=None, act="none", residual=None, z=None, stream=None) -> None:
+    """out (M, N) = act(z) + residual, z = x w' + bias, for x (M, K) and w (N, K) of one
+    type up to 32 bits; out and residual of that type or float32, bias (N), too; z
+    (M, N) of x's type takes what the backward reads. act: none, relu, gelu, gelu_tanh
+    or silu. out may be residual."""
+    xp, M, K, ldx = _matrix(x, "x")
+    on, sp = _place(x, "x", stream)
+    wp, N, _, ldw = _matrix(w, "w", None, K, x.dtype, on)
+    op, _, _, ldo = _matrix(out, "out", M, N, None, on)
+    rp = zp = None
+    ldr = ldz = ldo
+    if residual is not None:
+        rp, _, _, ldr = _matrix(residual, "residual", M, N, out.dtype, on)
+    if z is not None:
+        zp, _, _, ldz = _matrix(z, "z", M, N, x.dtype, on)
+    t = _type(x.dtype, "x")
+    bt = t if bias is None else _type(bias.dtype, "bias")
+    _check(lib().kmp_dense_product(sp, t, xp, ldx, M, wp, ldw, N, K, bt, _vector(bias, "bias", N, None, on), _act(act),
+                                   _type(out.dtype, "out"), rp, ldr, op, ldo, zp, ldz), allow_maxiter=False)
+
+
+def kmp_dense_product_workspace_bytes(M: int, N: int, K: int, dtype) -> int:
+    return int(lib().kmp_dense_product_workspace_bytes(_type(dtype, "x"), int(M), int(N), int(K)))
+
+
+def kmp_dense_product_backward(dout, x, w, z, dx, dw, dbias, act="none", workspace=None, stream=None) -> None:
+    """Gradients of kmp_dense_product from dout (M, N): dx (M, K) and dw (N, K) of
+    x's type, dbias (N) of that type or float32; each may be None, and x without dw, w
+    without dx. z is what the forward call wrote (None for act "none"). The workspace
+    has kmp_dense_product_workspace_bytes(M, N, K, dtype) bytes."""
+    dp, M, N, lddo = _matrix(dout, "dout")
+    on, sp = _place(dout, "dout", stream)
+    code = _act(act)
+    t = _type(dout.dtype, "dout")
+    K = next((m.shape[-1] for m in (x, w, dx, dw) if m is not None), 0)
+
+    def matrix(m, name, rows, cols):
+        if m is None:
+            return None, cols
+        p, _, _, ld = _matrix(m, name, rows, cols, dout.dtype, on)
+        return p, ld
+
+    zp, ldz = matrix(z, "z", M, N)
+    xp, ldx = matrix(x, "x", M, K)
+    wp, ldw = matrix(w, "w", N, K)
+    dxp, lddx = matrix(dx, "dx", M, K)
+    dwp, lddw = matrix(dw, "dw", N, K)
+    bt = t if dbias is None else _type(dbias.dtype, "dbias")
+    wsp, wsb = _workspace(workspace, on)
+    _check(lib().kmp_dense_product_backward(sp, t, dp, lddo, M, N, K, code, zp, ldz, xp, ldx, wp, ldw, dxp, lddx, dwp, lddw,
+                                            bt, _vector(dbias, "dbias", N, None, on), wsp, wsb), allow_maxiter=False)
 
 
 def kmp_token_logprobs_workspace_bytes(T: int, V: int, top: int = 0) -> int:
