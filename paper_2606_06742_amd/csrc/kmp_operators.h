@@ -117,7 +117,6 @@ struct BlockBackArgs {
   float* means;                         // rows x 2 (rows too long for the registers)
 };
 int64_t block_partials(int xtype, int64_t rows, int64_t d);
-bool block_long(int xtype, int64_t d);  // such rows
 int block_backward(hipStream_t s, const BlockBackArgs& a);
 
 // ------------------------------------------------- products in 8-bit integers

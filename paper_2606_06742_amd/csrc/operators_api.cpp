@@ -118,7 +118,7 @@ int kmp_block_norm(void* stream, int32_t xtype, int32_t flags, const void* b, in
 size_t kmp_block_norm_workspace_bytes(int32_t xtype, int64_t rows, int64_t d) {
   if (!float_type(xtype) || rows < 0 || rows > kMost || d < 1 || d > kMost) return 0;
   const size_t sums = (size_t)block_partials(xtype, rows, d) * 4 * (size_t)d * 4;
-  return std::max<size_t>(256, round_up((int64_t)sums, 16) + (block_long(xtype, d) ? (size_t)rows * 8 : 0));
+  return std::max<size_t>(256, round_up((int64_t)sums, 16) + (size_t)rows * 8);
 }
 
 int kmp_block_norm_backward(void* stream, int32_t xtype, int32_t flags, const void* dy, int64_t lddy,
