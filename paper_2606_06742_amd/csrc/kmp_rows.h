@@ -1,5 +1,5 @@
 // Rows over the threads of a workgroup: sums and largest values of a row, its
-// vectors in registers, its elements in 8 bits (norm.hip, block.hip).
+// vectors in registers, its elements in 8 bits (norm.hip, kmp_block.h).
 #pragma once
 
 #include "kmp_operators.h"

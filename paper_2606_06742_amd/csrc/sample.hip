@@ -17,13 +17,24 @@ namespace {
 constexpr int NT = 1024, NW = NT / 64; // threads and wavefronts of a workgroup
 constexpr int BINS = 256, COLS = 32;   // bins of a histogram, columns of each
 
+constexpr int GRID = 512;              // bins of a segment's histogram
+constexpr int kMostSegs = 64;
+constexpr int LISTED = 4 * NT;         // tokens near the cuts that are listed at most
+
 struct Shared {
   union {
     struct {                           // two lanes share a column, on a bank of their own
       unsigned long long sum[BINS][COLS];
       uint32_t count[BINS][COLS];
     } h;
-    key_t list[NT];
+    struct {
+      key_t list[NT];
+      key_t listed[LISTED];
+      double sums[LISTED];             // running sums of their weights
+      double weight[GRID];             // running sums of the bins, relative to the row's maximum
+      double tokens[GRID];
+      double before[kMostSegs];
+    };
   };
   double red[NW];
   double bin_sum[BINS];
@@ -312,26 +323,33 @@ struct Row {
     }
   }
 
-  // The token drawn from the keys from `cut` up, and log(w / Z).
-  __device__ int64_t draw(key_t cut, double u, double& logp) {
-    const auto kept = [&](int64_t j, float v) -> double {
-      if (key_of(v, (uint32_t)j) < cut) return 0.0;
-      const double w = weight(v);
-      return w >= min_p ? w : 0.0;
-    };
-    int64_t from = 0, to = V;
-    double before = 0.0, goal = 0.0, Z = 0.0;
-    for (bool whole = true;; whole = false) {     // the wavefront's run in which the sum passes
+  // The token drawn from the keys from `cut` up, and its weight over their total.
+  __device__ int64_t draw(key_t cut, double u, double& share) {
+    double Z = 0.0;
+    visit(x, 0, V, [&](int64_t j, float v) { Z += kept(cut, j, v); });
+    Z = block_sum<NW>(Z, sh.red);
+    double w;
+    const int64_t token = pass(cut, 0, V, 0.0, u < 1.0 ? u * Z : INFINITY, w);
+    share = w / Z;
+    return token;
+  }
+
+  __device__ double kept(key_t cut, int64_t j, float v) const {
+    if (key_of(v, (uint32_t)j) < cut) return 0.0;
+    const double w = weight(v);
+    return w >= min_p ? w : 0.0;
+  }
+
+  // The first of the elements [from, to) at which `before` and the running sum of the
+  // weights from the key `cut` up exceed `goal`, or the last that has a weight.
+  __device__ int64_t pass(key_t cut, int64_t from, int64_t to, double before, double goal, double& weight_of) {
+    while (to - from > 16 * NT) {                 // the wavefront's run in which the sum passes
       double s = 0.0;
-      visit(x, from, to, [&](int64_t j, float v) { s += kept(j, v); });
+      visit(x, from, to, [&](int64_t j, float v) { s += kept(cut, j, v); });
       s = wave_sum(s);
       __syncthreads();
       if ((threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = s;
       __syncthreads();
-      if (whole) {
-        for (int i = 0; i < NW; ++i) Z += sh.red[i];
-        goal = u < 1.0 ? u * Z : INFINITY;
-      }
       int at = -1;
       double sum = before, start = before;
       for (int i = 0; i < NW; ++i) {
@@ -342,23 +360,24 @@ struct Row {
       before = start;
       from += max(at, 0) * run;
       to = min(to, from + run);
-      if (to - from <= 16 * NT) break;
     }
-    const int64_t per = ceil_div(to - from, NT), j0 = from + threadIdx.x * per, j1 = min(to, j0 + per);
+    // 16 neighbouring elements a thread at most
+    const int per = (int)ceil_div(to - from, NT);
+    const int64_t j0 = from + threadIdx.x * per;
+    const int n = (int)max((int64_t)0, min((int64_t)per, to - j0));
     double s = 0.0, total;
-    for (int64_t j = j0; j < j1; ++j) s += kept(j, (float)x[j]);
+    for (int e = 0; e < n; ++e) s += kept(cut, j0 + e, (float)x[j0 + e]);
     const double running = block_running(sh, s, total);
     int who = block_first(sh, s > 0.0 && before + running > goal);
     if (who == NT) who = block_last(sh, s > 0.0);
     __syncthreads();
     if ((int)threadIdx.x == who) {
-      double sum = before + (running - s);
+      double sum = before + (running - s), own = 0.0;
       int64_t token = -1;
-      double own = 0.0;
-      for (int64_t j = j0; j < j1; ++j) {
-        const double w = kept(j, (float)x[j]);
+      for (int e = 0; e < n; ++e) {
+        const double w = kept(cut, j0 + e, (float)x[j0 + e]);
         if (w <= 0.0) continue;
-        token = j;
+        token = j0 + e;
         own = w;
         sum += w;
         if (sum > goal) break;
@@ -368,31 +387,423 @@ struct Row {
     }
     __syncthreads();
     const int64_t token = (int64_t)sh.top[0];
-    logp = log(sh.red[0] / Z);
+    weight_of = sh.red[0];
     __syncthreads();
     return token;
   }
 };
 
+// ---- Histograms of segments
+// A segment's weights are counted on a grid that all segments of a row share without
+// knowing its maximum: with y = 16 x / temperature, bin floor(y) and in it the weight
+// exp(f / 16), f = y - floor(y); 512 bins down from the segment's largest logit's span 32
+// e-foldings. A bin's count and the sum of its exp(f / 16) - 1 are one 64-bit whole
+// number, added to by one LDS atomic: the sum in steps of 2^-q below, the count from bit
+// 64 - c up, c bits being enough for a column's elements (each four lanes' own).
+constexpr int COLUMNS = 16;
+constexpr int SEG = 16 * NT;           // elements of a segment, 16 a thread
+constexpr double kFine = 16.0;
+
+struct Segment {
+  double weight[GRID];                 // sums of exp(f / 16), the first bin that of the maximum
+  uint32_t count[GRID];
+  double tail;                         // the weight below them, relative to the maximum
+  key_t top;                           // its largest key
+  uint32_t tail_count;
+  uint32_t pad[3];
+};
+
+__host__ __device__ constexpr int64_t segment_length(int64_t V) {
+  return V <= (int64_t)SEG * kMostSegs ? SEG : round_up(ceil_div(V, kMostSegs), SEG);
+}
+__host__ __device__ constexpr int64_t segments(int64_t V) { return ceil_div(V, segment_length(V)); }
+
+// exp(f / 16) - 1 for f in [0, 1]: Taylor's terms up to (f / 16)^7, the next is below
+// 2^-47.
+__device__ __forceinline__ double grow(double f) {
+  const double r = f * (1.0 / kFine);
+  double p = 1.0 / 5040.0;
+  p = fma(p, r, 1.0 / 720.0);
+  p = fma(p, r, 1.0 / 120.0);
+  p = fma(p, r, 1.0 / 24.0);
+  p = fma(p, r, 1.0 / 6.0);
+  p = fma(p, r, 0.5);
+  p = fma(p, r, 1.0);
+  return p * r;
+}
+
+// One workgroup per segment of a row; its elements stay in registers between the maximum
+// and the histogram where they are at most SEG.
 template <typename T>
-__global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
+__global__ __launch_bounds__(NT, 8) void sample_count_kernel(SampleArgs a) {
+  constexpr int VEC = vec_of<T>(), U = 16 / VEC;
+  __shared__ unsigned long long bins[GRID][COLUMNS];
+  __shared__ key_t tops[NW];
+  __shared__ double red[NW];
+  __shared__ uint32_t counts[NW];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t length = segment_length(a.V), from = blockIdx.x * length, to = min(a.V, from + length);
+  for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
+    const T* x = static_cast<const T*>(a.logits) + t * a.ld;
+    Segment* out = static_cast<Segment*>(a.workspace) + t * gridDim.x + blockIdx.x;
+    for (int i = threadIdx.x; i < GRID * COLUMNS; i += NT) (&bins[0][0])[i] = 0;
+    float v[U][VEC];
+    const auto load = [&](int64_t j0) {           // 16 elements from a run of SEG, -inf past the end
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int64_t j = j0 + ((int64_t)i * NT + threadIdx.x) * VEC;
+        if (j + VEC <= to) {
+          load_n(x + j, v[i]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) v[i][e] = j + e < to ? (float)x[j + e] : -INFINITY;
+        }
+      }
+    };
+    float best = -INFINITY;
+    int64_t at = from;
+    for (int64_t j0 = from; j0 < to; j0 += SEG) {
+      load(j0);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (v[i][e] > best || v[i][e] != v[i][e]) best = v[i][e], at = j0 + ((int64_t)i * NT + threadIdx.x) * VEC + e;
+    }
+    key_t top = key_of(best, (uint32_t)at);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) top = max(top, (key_t)__shfl_xor(top, off, kWave));
+    if (lane == 0) tops[w] = top;
+    __syncthreads();
+    top = tops[0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) top = max(top, tops[i]);
+    const float m = key_value((uint32_t)(top >> 32)), temperature = a.temperature ? a.temperature[t] : 1.0f;
+    double tail = 0.0;
+    uint32_t tail_count = 0;
+    // (rows that are greedy, not finite or have no choice need no more than the maximum)
+    const bool some = m > -INFINITY && m < INFINITY && temperature > 0.0f;
+    const int c = 64 - __clzll((unsigned long long)ceil_div(min(length, a.V), COLUMNS)) + 1, q = min(67 - 2 * c, 51);
+    if (some) {
+      const double it = 1.0 / (double)temperature, scale = kFine * it, first = floor((double)m * scale);
+      // p + 2^(52 - q) holds p in steps of 2^-q in its last bits; the count's one is added
+      // and the sum's exponent taken off at once
+      const double magic = ldexp(1.0, 52 - q);
+      const unsigned long long one = ((unsigned long long)1 << (64 - c)) - (unsigned long long)__double_as_longlong(magic);
+      unsigned long long* column = &bins[0][lane & (COLUMNS - 1)];
+      for (int64_t j0 = from; j0 < to; j0 += SEG) {
+        if (to - from > SEG) load(j0);
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const double y = (double)v[i][e] * scale, bin = floor(y), place = first - bin;
+            if (place < (double)GRID) {
+              const double p = grow(fma((double)v[i][e], scale, -bin));
+              atomicAdd(column + (int)place * COLUMNS, (unsigned long long)__double_as_longlong(p + magic) + one);
+            } else if (v[i][e] > -INFINITY) {
+              tail += exp(((double)v[i][e] - (double)m) * it);
+              ++tail_count;
+            }
+            if (e & 1) __builtin_amdgcn_sched_barrier(0);   // (two at a time: sixteen at once would not fit the registers)
+          }
+      }
+    }
+    tail = wave_sum(tail);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) tail_count += __shfl_xor(tail_count, off, kWave);
+    if (lane == 0) red[w] = tail, counts[w] = tail_count;
+    __syncthreads();
+    if (threadIdx.x < GRID) {
+      unsigned long long sum = 0;
+      uint32_t n = 0;
+      if (some) {
+        const unsigned long long low = ((unsigned long long)1 << (64 - c)) - 1;
+#pragma unroll
+        for (int k = 0; k < COLUMNS; ++k) {       // (staggered over the banks)
+          const unsigned long long b = bins[threadIdx.x][(k + threadIdx.x) & (COLUMNS - 1)];
+          sum += b & low;
+          n += (uint32_t)(b >> (64 - c));
+        }
+      }
+      out->weight[threadIdx.x] = (double)n + ldexp((double)sum, -q);
+      out->count[threadIdx.x] = n;
+    }
+    if (threadIdx.x == 0) {
+      double s = 0.0;
+      uint32_t n = 0;
+      for (int i = 0; i < NW; ++i) s += red[i], n += counts[i];
+      out->tail = s;
+      out->tail_count = n;
+      out->top = top;
+    }
+    __syncthreads();
+  }
+}
+
+// ---- The draw, one workgroup per row
+// The first n keys of sh.listed in descending order (n <= LISTED; the rest up to the next
+// power of two is cleared).
+__device__ __forceinline__ void sort_list(Shared& sh, int n) {
+  int size = NT;
+  while (size < n) size *= 2;
+  for (int i = n + threadIdx.x; i < size; i += NT) sh.listed[i] = 0;
+  __syncthreads();
+  if (size == NT) {
+    const key_t mine = sorted(sh, sh.listed[threadIdx.x]);
+    sh.listed[threadIdx.x] = mine;
+    __syncthreads();
+    return;
+  }
+  for (int k = 2; k <= size; k <<= 1)
+    for (int s = k >> 1; s > 0; s >>= 1) {
+      for (int i = threadIdx.x; i < size / 2; i += NT) {
+        const int p = 2 * i - (i & (s - 1)), r = p + s;   // a pair s apart
+        const key_t u = sh.listed[p], v = sh.listed[r];
+        if (((p & k) == 0) == (u < v)) sh.listed[p] = v, sh.listed[r] = u;
+      }
+      __syncthreads();
+    }
+}
+// sh.sums: running sums of weight(key) over the first n of sh.listed.
+template <typename F>
+__device__ __forceinline__ void sum_list(Shared& sh, int n, F weight) {
+  const int per = (n + NT - 1) / NT, j0 = threadIdx.x * per;
+  double s = 0.0, total;
+  for (int e = 0; e < per; ++e)
+    if (j0 + e < n) s += weight(sh.listed[j0 + e]);
+  double running = block_running(sh, s, total) - s;
+  for (int e = 0; e < per; ++e)
+    if (j0 + e < n) sh.sums[j0 + e] = running += weight(sh.listed[j0 + e]);
+  __syncthreads();
+}
+// The first i < n for which is(i) holds, n where there is none (is() once true stays so
+// but for rounding).
+template <typename F>
+__device__ __forceinline__ int first_of(Shared& sh, int n, F is) {
+  const int per = (n + NT - 1) / NT, j0 = threadIdx.x * per;
+  int at = n;
+  for (int e = per - 1; e >= 0; --e)
+    if (j0 + e < n && is(j0 + e)) at = j0 + e;
+  const int who = block_first(sh, at < n);
+  if (who == NT) return n;
+  __syncthreads();
+  if ((int)threadIdx.x == who) sh.n = at;
+  __syncthreads();
+  return sh.n;
+}
+
+// A row's token by its segments' histograms, or -1 where its cuts are not in them (below
+// 32 e-foldings, or with more than LISTED tokens in their bins). The bins that hold the
+// cuts are known from running sums over the bins; only their tokens are looked for in
+// the row and put in order, and where all that is kept is few, these, too.
+template <typename T>
+__device__ __forceinline__ int64_t pick(Shared& sh, Row<T>& row, const Segment* seg, int segs, int64_t length, int64_t k, double p,
+                        double u, double& share) {
+  const double scale = kFine * row.it, y = (double)row.m * scale, first = floor(y), f0 = fma((double)row.m, scale, -first);
+  const int g = threadIdx.x;
+  // a bin's weights relative to the row's maximum, from those relative to its border
+  const auto border_weight = [&](double bin) { return exp(-(first - bin + f0) * (1.0 / kFine)); };
+  const auto offset = [&](int s) {                // of segment s's first bin; GRID: none of it is on the row's grid
+    const float m = key_value((uint32_t)(seg[s].top >> 32));
+    const double d = m > -INFINITY ? first - floor((double)m * scale) : (double)GRID;
+    return d < (double)GRID ? (int)d : GRID;
+  };
+  // running counts and weights over the row's bins; what lies below them
+  double w = 0.0, n = 0.0, below = 0.0;
+  if (g < GRID) {
+    for (int s = 0; s < segs; ++s) {
+      const int off = offset(s);
+      if (g >= off) {
+        w += seg[s].weight[g - off];
+        n += (double)seg[s].count[g - off];
+      }
+      if (off > 0) {                              // thread g: the segment's bin g, if that is below
+        const float m = key_value((uint32_t)(seg[s].top >> 32));
+        if (m > -INFINITY && g + off >= GRID) below += seg[s].weight[g] * border_weight(floor((double)m * scale) - g);
+      }
+      if (g == 0) {
+        const float m = key_value((uint32_t)(seg[s].top >> 32));
+        if (m > -INFINITY) below += seg[s].tail * row.weight(m);
+      }
+    }
+    w *= border_weight(first - g);
+  }
+  below = block_sum<NW>(below, sh.red);
+  double total, tokens;
+  const double runw = block_running(sh, w, total), runn = block_running(sh, n, tokens);
+  if (g < GRID) sh.weight[g] = runw, sh.tokens[g] = runn;
+  __syncthreads();
+  const auto weight_to = [&](int b) { return b >= 0 ? sh.weight[b] : 0.0; };   // of the bins up to b
+  const auto count_to = [&](int b) { return b >= 0 ? (int64_t)sh.tokens[b] : 0; };
+  // the bins in which the cuts lie: the k-th token's, those where the sum may reach p of
+  // the first k tokens' (their weight is not known before they are in order), those
+  // around min_p
+  const bool by_k = k < row.V, by_p = p < 1.0, by_m = row.min_p > 0.0;
+  int kb = GRID, lo = GRID, hi = GRID - 1;
+  double least = total + below, most = least;
+  if (by_k) {
+    kb = first_of(sh, GRID, [&](int b) { return sh.tokens[b] >= (double)k; });
+    if (kb == GRID) return -1;
+    least = weight_to(kb - 1), most = weight_to(kb);
+    lo = hi = kb;
+  }
+  if (by_p) {
+    const int plo = first_of(sh, GRID, [&](int b) { return sh.weight[b] >= p * least * (1.0 - 1e-9); });
+    const int phi = first_of(sh, GRID, [&](int b) { return sh.weight[b] >= p * most * (1.0 + 1e-9); });
+    if (phi == GRID && !by_k) return -1;
+    lo = min(lo, plo), hi = min(hi, phi);
+  }
+  if (by_m) {                                     // a token of bin b has -16 log w = b + f0 - f, 0 <= f < 1
+    const double edge = -kFine * log(row.min_p) - f0;
+    if (!(edge + 2.0 < (double)GRID)) return -1;
+    lo = min(lo, (int)floor(max(edge - 1e-6, -1.0)) + 1);
+    hi = min(hi, (int)ceil(edge + 1.0 + 1e-6));
+  }
+  key_t cut = 0;
+  int listed = 0;
+  double Z = total + below;
+  if (by_k || by_p || by_m) {
+    lo = min(lo, first_of(sh, GRID, [&](int b) { return sh.tokens[b] >= sh.tokens[hi]; }));   // (a bin that has tokens)
+    const bool far = by_k && by_p && kb > hi;     // the k-th token's bin as well, for the weight of the first k
+    if (count_to(hi) + (far ? count_to(kb) - count_to(kb - 1) : 0) <= LISTED) lo = 0;
+    const int64_t near = count_to(hi) - count_to(lo - 1), more = far ? count_to(kb) - count_to(kb - 1) : 0;
+    if (near + more > LISTED) return -1;
+    // list them: logits below `low` are of later bins (a little lower than the border, for
+    // its rounding; the bin decides)
+    const int last = far ? kb : hi;
+    const double border = (first - last) / scale;
+    const float low = scale > 0.0 ? nextafterf((float)(border - fabs(border) * 0x1p-40), -INFINITY) : -INFINITY;
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    const auto bin_of = [&](float v) {
+      const double d = first - floor((double)v * scale);
+      return d < (double)GRID ? (int)d : GRID;
+    };
+    for (int s = 0; s < segs; ++s) {
+      if (key_value((uint32_t)(seg[s].top >> 32)) < low) continue;
+      const int64_t from = s * length, to = min(row.V, from + length);
+      visit(row.x, from, to, [&](int64_t j, float v) {
+        if (!(v >= low) || v == -INFINITY) return;
+        const int b = bin_of(v);
+        if (!((b >= lo && b <= hi) || (far && b == kb))) return;
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < LISTED) sh.listed[at] = key_of(v, (uint32_t)j);
+      });
+    }
+    __syncthreads();
+    const int size = min(sh.n, LISTED);
+    __syncthreads();
+    sort_list(sh, size);
+    const auto weight = [&](key_t key) { return row.weight(key_value((uint32_t)(key >> 32))); };
+    sum_list(sh, size, weight);
+    const int run = (int)near;                    // the first of them, bins lo to hi
+    const double before = weight_to(lo - 1);
+    int end = run;                                // kept of them
+    double of = total + below;
+    if (by_k) {
+      const int64_t rank = k - (far ? count_to(kb - 1) - run : count_to(lo - 1));   // the k-th token's place in the list
+      if (rank >= 1 && rank <= size) {
+        of = far ? weight_to(kb - 1) + (sh.sums[rank - 1] - sh.sums[run - 1]) : before + sh.sums[rank - 1];
+        end = (int)min((int64_t)end, rank);
+      } else if (by_p) {
+        return -1;
+      }
+    }
+    if (by_p) {
+      const double reach = p * of;
+      const int r = first_of(sh, run, [&](int i) { return before + sh.sums[i] >= reach; });
+      end = min(end, r + 1);
+    }
+    if (by_m) end = min(end, first_of(sh, run, [&](int i) { return weight(sh.listed[i]) < row.min_p; }));
+    if (end <= 0) return -1;
+    cut = sh.listed[end - 1];
+    Z = before + sh.sums[end - 1];
+    listed = end;
+    __syncthreads();
+  }
+  const double goal = u < 1.0 ? u * Z : INFINITY;
+  if (listed > 0) {                               // by index: the complemented index above the value's bits
+    for (int i = threadIdx.x; i < listed; i += NT) sh.listed[i] = sh.listed[i] << 32 | sh.listed[i] >> 32;
+    __syncthreads();
+    sort_list(sh, listed);
+    sum_list(sh, listed, [&](key_t key) { return row.weight(key_value((uint32_t)key)); });
+    if (lo == 0) {                                // all that is kept
+      int i = first_of(sh, listed, [&](int i) { return sh.sums[i] > goal; });
+      if (i == listed) i = listed - 1;
+      // (the last that has a weight, and not one of none)
+      while (i > 0 && row.weight(key_value((uint32_t)sh.listed[i])) <= 0.0) --i;
+      share = row.weight(key_value((uint32_t)sh.listed[i])) / Z;
+      return (int64_t)(uint32_t)~(uint32_t)(sh.listed[i] >> 32);
+    }
+  }
+  // the segment in which the sum passes: its bins before `lo` (all of it without cuts)
+  // and its listed tokens
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int s = wave; s < segs; s += NW) {
+    const int off = offset(s), bins = cut != 0 ? lo : GRID;
+    const float m = key_value((uint32_t)(seg[s].top >> 32));
+    double sum = 0.0;
+    if (m > -INFINITY) {
+      const double base = floor((double)m * scale);
+      for (int i = lane; i < GRID; i += 64)
+        if (cut == 0 || i + off < bins) sum += seg[s].weight[i] * border_weight(base - i);
+      if (lane == 0 && cut == 0) sum += seg[s].tail * row.weight(m);
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) sh.before[s] = sum;
+  }
+  __syncthreads();
+  if (listed > 0 && (int)threadIdx.x < segs) {    // thread s: the listed tokens of segment s
+    const auto end_of = [&](int s) {              // how many lie before segment s + 1
+      const uint32_t index = (uint32_t)((s + 1) * length);
+      int a = 0, b = listed;
+      while (a < b) {
+        const int c = (a + b) / 2;
+        if ((uint32_t)~(uint32_t)(sh.listed[c] >> 32) < index) a = c + 1;
+        else b = c;
+      }
+      return a;
+    };
+    const int a = threadIdx.x == 0 ? 0 : end_of(threadIdx.x - 1), b = end_of(threadIdx.x);
+    sh.before[threadIdx.x] += (b > 0 ? sh.sums[b - 1] : 0.0) - (a > 0 ? sh.sums[a - 1] : 0.0);
+  }
+  __syncthreads();
+  int at = -1;
+  double sum = 0.0, start = 0.0;
+  for (int s = 0; s < segs; ++s) {
+    const double own = sh.before[s];
+    if (own > 0.0 && (at < 0 || start + sh.before[at] <= goal)) at = s, start = sum;
+    sum += own;
+  }
+  __syncthreads();
+  if (at < 0) return -1;
+  double own;
+  const double keep = row.min_p;
+  row.min_p = 0.0;                                // (the cut has it)
+  const int64_t token = row.pass(cut, at * length, min(row.V, (at + 1) * length), start, goal, own);
+  row.min_p = keep;
+  share = own / Z;
+  return token;
+}
+
+template <typename T>
+__global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs) {
   __shared__ Shared sh;
+  const int64_t length = segment_length(a.V);
   for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
     const T* x = static_cast<const T*>(a.logits) + t * a.ld;
-    float best = -INFINITY;
-    int64_t at = -1;
-    visit(x, 0, a.V, [&](int64_t j, float v) {
-      if (v > best || v != v) best = v, at = j;
-    });
-    // (-inf alone has a key, too: the first of a row of nothing else)
-    const key_t top = block_top(sh, at < 0 ? 0 : key_of(best, (uint32_t)at));
-    const float m = top == 0 ? -INFINITY : key_value((uint32_t)(top >> 32));
+    const Segment* seg = static_cast<const Segment*>(a.workspace) + t * segs;
+    key_t top = 0;
+    for (int s = 0; s < segs; ++s) top = max(top, seg[s].top);
+    const float m = key_value((uint32_t)(top >> 32));
     const float temperature = a.temperature ? a.temperature[t] : 1.0f, p = a.top_p ? a.top_p[t] : 1.0f;
     const float min_p = a.min_p ? a.min_p[t] : 0.0f, u = a.u[t];
     const int64_t k = a.top_k && a.top_k[t] > 0 && a.top_k[t] < a.V ? a.top_k[t] : a.V;
+    const bool nan = temperature != temperature || p != p || min_p != min_p || u != u || m != m || m == INFINITY;
     int64_t token = -1;
     double logp = __builtin_nan("");
-    const bool nan = temperature != temperature || p != p || min_p != min_p || u != u || m != m || m == INFINITY;
     if (!nan && m == -INFINITY) {
       logp = -INFINITY;
     } else if (!nan && (temperature <= 0.0f || p <= 0.0f || k == 1)) {
@@ -400,10 +811,16 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
       logp = 0.0;
     } else if (!nan) {
       Row<T> row{sh, x, a.V, m, 1.0 / (double)temperature, min((double)max(min_p, 0.0f), 1.0)};
-      key_t cut = 0;
-      if (k < a.V) cut = row.kth(k, top);
-      if (p < 1.0f) cut = row.reach_p((double)p, cut);
-      token = row.draw(cut, max((double)u, 0.0), logp);
+      const double goal_of = max((double)u, 0.0);
+      double share;
+      token = pick(sh, row, seg, segs, length, k, (double)p, goal_of, share);
+      if (token < 0) {                            // the cuts are not where the histograms see them
+        key_t cut = 0;
+        if (k < a.V) cut = row.kth(k, top);
+        if (p < 1.0f) cut = row.reach_p((double)p, cut);
+        token = row.draw(cut, goal_of, share);
+      }
+      logp = log(share);
     }
     if (threadIdx.x == 0) {
       if (a.wide) static_cast<int64_t*>(a.tokens)[t] = token;
@@ -416,14 +833,18 @@ __global__ __launch_bounds__(NT) void sample_kernel(SampleArgs a) {
 
 template <typename T>
 int sample_as(hipStream_t s, const SampleArgs& a) {
-  hipLaunchKernelGGL(sample_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T, 4096)), dim3(NT), 0, s, a);
+  const int segs = (int)segments(a.V);
+  hipLaunchKernelGGL(sample_count_kernel<T>, dim3(segs, (unsigned)std::min<int64_t>(a.T, 65535)), dim3(NT), 0, s, a);
+  hipLaunchKernelGGL(sample_pick_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T, 65535)), dim3(NT), 0, s, a, segs);
   KMP_LAUNCH_CHECK();
   return 0;
 }
 
 }  // namespace
 
-size_t sample_workspace(int64_t T, int64_t V) { return 256; }
+size_t sample_workspace(int64_t T, int64_t V) {
+  return std::max<int64_t>(256, T * segments(V) * (int64_t)sizeof(Segment));
+}
 
 int sample_tokens(hipStream_t s, const SampleArgs& a) {
   switch (a.type) {
