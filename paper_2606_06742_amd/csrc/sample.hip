@@ -14,50 +14,63 @@
 namespace kmp {
 namespace {
 
-constexpr int NT = 1024, NW = NT / 64; // threads and wavefronts of a workgroup
+constexpr int NT = 512, NW = NT / 64;  // threads and wavefronts of a workgroup
 constexpr int BINS = 256, COLS = 32;   // bins of a histogram, columns of each
 
 constexpr int GRID = 512;              // bins of a segment's histogram
 constexpr int kMostSegs = 64;
-constexpr int LISTED = 4 * NT;         // tokens near the cuts that are listed at most
+constexpr int LISTED = 4096;           // tokens near the cuts that are listed at most
 
-struct Shared {
+struct Common {
+  double red[NW];
+  key_t top[NW];
+  int first[NW];
+  int n;
+};
+struct Shared : Common {               // of passes over a row alone
   union {
     struct {                           // two lanes share a column, on a bank of their own
       unsigned long long sum[BINS][COLS];
       uint32_t count[BINS][COLS];
     } h;
-    struct {
-      key_t list[NT];
-      key_t listed[LISTED];
-      double sums[LISTED];             // running sums of their weights
-      double weight[GRID];             // running sums of the bins, relative to the row's maximum
-      double tokens[GRID];
-      double before[kMostSegs];
-    };
+    key_t list[NT];
   };
-  double red[NW];
-  double bin_sum[BINS];
-  uint32_t bin_count[BINS];
-  key_t top[NW];
-  int first[NW];
-  int n;
+  double bin_sum[2];
+  uint32_t bin_count;
+};
+struct PickShared : Common {           // with the histograms of its segments
+  key_t listed[LISTED];
+  double sums[LISTED];                 // running sums of their weights
+  double weight[GRID];                 // running sums of the bins, relative to the row's maximum
+  double tokens[GRID];
+  double before[kMostSegs];
 };
 
-// f(j, x_j) for the row's elements [from, to): wavefront w takes the w-th of sixteen
-// neighbouring runs, in vectors of 16 bytes.
-template <typename T>
+// f(j, x_j) for the row's elements [from, to): wavefront w takes the w-th of WAVES
+// neighbouring runs, in vectors of 16 bytes, U of them in flight.
+template <typename T, int WAVES = NW>
 __device__ __forceinline__ int64_t run_length(int64_t n) {
   constexpr int64_t STEP = 64 * vec_of<T>();
-  return round_up(ceil_div(n, NW), STEP);
+  return round_up(ceil_div(n, WAVES), STEP);
 }
-template <typename T, typename F>
+template <int U, int WAVES = NW, typename T, typename F>
 __device__ __forceinline__ void visit(const T* x, int64_t from, int64_t to, F f) {
-  constexpr int VEC = vec_of<T>();
-  const int64_t run = run_length<T>(to - from), start = from + (threadIdx.x >> 6) * run, end = min(to, start + run);
+  constexpr int VEC = vec_of<T>(), STEP = 64 * VEC;
+  const int64_t run = run_length<T, WAVES>(to - from), start = from + (threadIdx.x >> 6) * run, end = min(to, start + run);
   int64_t j = start + (threadIdx.x & 63) * VEC;
-#pragma unroll 2
-  for (; j + VEC <= end; j += 64 * VEC) {
+  if constexpr (U > 1) {
+    for (; j + (U - 1) * STEP + VEC <= end; j += U * STEP) {
+      T v[U][VEC];
+#pragma unroll
+      for (int i = 0; i < U; ++i) __builtin_memcpy(v[i], x + j + i * STEP, 16);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f(j + i * STEP + e, (float)v[i][e]);
+    }
+  }
+#pragma unroll 1
+  for (; j + VEC <= end; j += STEP) {
     float v[VEC];
     load_n(x + j, v);
 #pragma unroll
@@ -67,7 +80,7 @@ __device__ __forceinline__ void visit(const T* x, int64_t from, int64_t to, F f)
 }
 
 // The block's largest key, its sum, its running sum; each starts with a barrier.
-__device__ __forceinline__ key_t block_top(Shared& sh, key_t v) {
+__device__ __forceinline__ key_t block_top(Common& sh, key_t v) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) v = max(v, (key_t)__shfl_xor(v, off, kWave));
   __syncthreads();
@@ -86,7 +99,7 @@ __device__ __forceinline__ double wave_running(double v) {
   }
   return v;
 }
-__device__ __forceinline__ double block_running(Shared& sh, double v, double& total) {
+__device__ __forceinline__ double block_running(Common& sh, double v, double& total) {
   v = wave_running(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 63) sh.red[threadIdx.x >> 6] = v;
@@ -101,7 +114,7 @@ __device__ __forceinline__ double block_running(Shared& sh, double v, double& to
   return before + v;
 }
 // The first thread with `is`, NT where there is none; the last one, -1.
-__device__ __forceinline__ int block_first(Shared& sh, bool is) {
+__device__ __forceinline__ int block_first(Common& sh, bool is) {
   const unsigned long long b = __ballot(is);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh.first[threadIdx.x >> 6] = b ? (int)(threadIdx.x & ~63) + __ffsll(b) - 1 : NT;
@@ -111,7 +124,7 @@ __device__ __forceinline__ int block_first(Shared& sh, bool is) {
   for (int i = 0; i < NW; ++i) at = min(at, sh.first[i]);
   return at;
 }
-__device__ __forceinline__ int block_last(Shared& sh, bool is) {
+__device__ __forceinline__ int block_last(Common& sh, bool is) {
   const unsigned long long b = __ballot(is);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh.first[threadIdx.x >> 6] = b ? (int)(threadIdx.x & ~63) + 63 - __clzll(b) : -1;
@@ -144,10 +157,10 @@ __device__ __forceinline__ key_t sorted(Shared& sh, key_t mine) {
   return mine;
 }
 
-// One row's drawing.
+// One row.
 template <typename T>
 struct Row {
-  Shared& sh;
+  Common& sh;
   const T* x;
   int64_t V;
   float m;                             // its maximum
@@ -155,6 +168,78 @@ struct Row {
   double min_p;                        // 0: none
 
   __device__ double weight(float v) const { return v == -INFINITY ? 0.0 : exp(((double)v - (double)m) * it); }
+
+  __device__ double kept(key_t cut, int64_t j, float v) const {
+    if (key_of(v, (uint32_t)j) < cut) return 0.0;
+    const double w = weight(v);
+    return w >= min_p ? w : 0.0;
+  }
+
+  // The first of the elements [from, to) at which `before` and the running sum of the
+  // weights from the key `cut` up exceed `goal`, or the last that has a weight.
+  __device__ int64_t pass(key_t cut, int64_t from, int64_t to, double before, double goal, double& weight_of) {
+    while (to - from > 32 * NT) {                 // the wavefront's run in which the sum passes
+      double s = 0.0;
+      visit<1>(x, from, to, [&](int64_t j, float v) { s += kept(cut, j, v); });
+      s = wave_sum(s);
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = s;
+      __syncthreads();
+      int at = -1;
+      double sum = before, start = before;
+      for (int i = 0; i < NW; ++i) {
+        if (sh.red[i] > 0.0 && (at < 0 || start + sh.red[at] <= goal)) at = i, start = sum;
+        sum += sh.red[i];
+      }
+      const int64_t run = run_length<T>(to - from);
+      before = start;
+      from += max(at, 0) * run;
+      to = min(to, from + run);
+    }
+    // 32 neighbouring elements a thread at most
+    const int per = (int)ceil_div(to - from, NT);
+    const int64_t j0 = from + threadIdx.x * per;
+    const int n = (int)max((int64_t)0, min((int64_t)per, to - j0));
+    double s = 0.0, total;
+    for (int e = 0; e < n; ++e) s += kept(cut, j0 + e, (float)x[j0 + e]);
+    const double running = block_running(sh, s, total);
+    int who = block_first(sh, s > 0.0 && before + running > goal);
+    if (who == NT) who = block_last(sh, s > 0.0);
+    __syncthreads();
+    if ((int)threadIdx.x == who) {
+      double sum = before + (running - s), own = 0.0;
+      int64_t token = -1;
+      for (int e = 0; e < n; ++e) {
+        const double w = kept(cut, j0 + e, (float)x[j0 + e]);
+        if (w <= 0.0) continue;
+        token = j0 + e;
+        own = w;
+        sum += w;
+        if (sum > goal) break;
+      }
+      sh.top[0] = (key_t)token;
+      sh.red[0] = own;
+    }
+    __syncthreads();
+    const int64_t token = (int64_t)sh.top[0];
+    weight_of = sh.red[0];
+    __syncthreads();
+    return token;
+  }
+};
+
+// Its cuts and its draw by passes over the row alone.
+template <typename T>
+struct Passes : Row<T> {
+  using Row<T>::x;
+  using Row<T>::V;
+  using Row<T>::m;
+  using Row<T>::it;
+  using Row<T>::weight;
+  using Row<T>::kept;
+  using Row<T>::pass;
+  Shared& sh;
+  __device__ Passes(Shared& shared, const Row<T>& row) : Row<T>(row), sh(shared) {}
 
   // The keys for which is(key, x) holds, at most NT of them, one a thread, in
   // descending order (0: none).
@@ -164,7 +249,7 @@ struct Row {
     sh.list[threadIdx.x] = 0;
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
-    visit(x, 0, V, [&](int64_t j, float v) {
+    visit<1>(x, 0, V, [&](int64_t j, float v) {
       const key_t key = key_of(v, (uint32_t)j);
       if (!is(key, v)) return;
       const int at = atomicAdd(&sh.n, 1);
@@ -206,7 +291,7 @@ struct Row {
     while (n > NT && lo < hi) {
       const int bits = 64 - __clzll(hi - lo), shift = max(0, bits - 8);
       clear_bins();
-      visit(x, 0, V, [&](int64_t j, float v) {
+      visit<1>(x, 0, V, [&](int64_t j, float v) {
         const key_t key = key_of(v, (uint32_t)j);
         if (key < lo || key > hi || !is(key, v)) return;
         add((int)((hi - key) >> shift), WEIGHED ? (unsigned long long)rint(ldexp(scaled(v), q)) : 1ull);
@@ -219,10 +304,10 @@ struct Row {
       const double running = block_running(sh, threadIdx.x < BINS ? own : 0.0, total);
       int b = block_first(sh, threadIdx.x < BINS && count > 0 && reach(above + running));
       if (b == NT) b = block_last(sh, threadIdx.x < BINS && count > 0);       // (rounding)
-      if ((int)threadIdx.x == b) sh.bin_sum[0] = running - own, sh.bin_count[0] = count;
+      if ((int)threadIdx.x == b) sh.bin_sum[0] = running - own, sh.bin_count = count;
       __syncthreads();
       above += sh.bin_sum[0];
-      n = sh.bin_count[0];
+      n = sh.bin_count;
       const key_t top = hi - ((key_t)b << shift), width = ((key_t)1 << shift) - 1;
       lo = top - lo > width ? top - width : lo;
       hi = top;
@@ -257,7 +342,7 @@ struct Row {
       clear_bins();
       double tail = 0.0;
       float below = -INFINITY;
-      visit(x, 0, V, [&](int64_t j, float v) {
+      visit<1>(x, 0, V, [&](int64_t j, float v) {
         if (v > top || v == -INFINITY || key_of(v, (uint32_t)j) < cut) return;
         const double at = ((double)top - (double)v) * fine;
         if (at < (double)BINS) {
@@ -287,12 +372,12 @@ struct Row {
       if ((int)threadIdx.x == bin) {
         sh.bin_sum[0] = running - own;
         sh.bin_sum[1] = unit;
-        sh.bin_count[0] = count;
+        sh.bin_count = count;
       }
       __syncthreads();
       above += sh.bin_sum[0];
       const double of = sh.bin_sum[1];
-      uint32_t n = sh.bin_count[0];
+      uint32_t n = sh.bin_count;
       __syncthreads();
       const auto is = [&](key_t key, float v) {
         if (v > top || v == -INFINITY || key < cut) return false;
@@ -326,69 +411,11 @@ struct Row {
   // The token drawn from the keys from `cut` up, and its weight over their total.
   __device__ int64_t draw(key_t cut, double u, double& share) {
     double Z = 0.0;
-    visit(x, 0, V, [&](int64_t j, float v) { Z += kept(cut, j, v); });
+    visit<1>(x, 0, V, [&](int64_t j, float v) { Z += kept(cut, j, v); });
     Z = block_sum<NW>(Z, sh.red);
     double w;
     const int64_t token = pass(cut, 0, V, 0.0, u < 1.0 ? u * Z : INFINITY, w);
     share = w / Z;
-    return token;
-  }
-
-  __device__ double kept(key_t cut, int64_t j, float v) const {
-    if (key_of(v, (uint32_t)j) < cut) return 0.0;
-    const double w = weight(v);
-    return w >= min_p ? w : 0.0;
-  }
-
-  // The first of the elements [from, to) at which `before` and the running sum of the
-  // weights from the key `cut` up exceed `goal`, or the last that has a weight.
-  __device__ int64_t pass(key_t cut, int64_t from, int64_t to, double before, double goal, double& weight_of) {
-    while (to - from > 16 * NT) {                 // the wavefront's run in which the sum passes
-      double s = 0.0;
-      visit(x, from, to, [&](int64_t j, float v) { s += kept(cut, j, v); });
-      s = wave_sum(s);
-      __syncthreads();
-      if ((threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = s;
-      __syncthreads();
-      int at = -1;
-      double sum = before, start = before;
-      for (int i = 0; i < NW; ++i) {
-        if (sh.red[i] > 0.0 && (at < 0 || start + sh.red[at] <= goal)) at = i, start = sum;
-        sum += sh.red[i];
-      }
-      const int64_t run = run_length<T>(to - from);
-      before = start;
-      from += max(at, 0) * run;
-      to = min(to, from + run);
-    }
-    // 16 neighbouring elements a thread at most
-    const int per = (int)ceil_div(to - from, NT);
-    const int64_t j0 = from + threadIdx.x * per;
-    const int n = (int)max((int64_t)0, min((int64_t)per, to - j0));
-    double s = 0.0, total;
-    for (int e = 0; e < n; ++e) s += kept(cut, j0 + e, (float)x[j0 + e]);
-    const double running = block_running(sh, s, total);
-    int who = block_first(sh, s > 0.0 && before + running > goal);
-    if (who == NT) who = block_last(sh, s > 0.0);
-    __syncthreads();
-    if ((int)threadIdx.x == who) {
-      double sum = before + (running - s), own = 0.0;
-      int64_t token = -1;
-      for (int e = 0; e < n; ++e) {
-        const double w = kept(cut, j0 + e, (float)x[j0 + e]);
-        if (w <= 0.0) continue;
-        token = j0 + e;
-        own = w;
-        sum += w;
-        if (sum > goal) break;
-      }
-      sh.top[0] = (key_t)token;
-      sh.red[0] = own;
-    }
-    __syncthreads();
-    const int64_t token = (int64_t)sh.top[0];
-    weight_of = sh.red[0];
-    __syncthreads();
     return token;
   }
 };
@@ -401,16 +428,15 @@ struct Row {
 // number, added to by one LDS atomic: the sum in steps of 2^-q below, the count from bit
 // 64 - c up, c bits being enough for a column's elements (each four lanes' own).
 constexpr int COLUMNS = 16;
-constexpr int SEG = 16 * NT;           // elements of a segment, 16 a thread
+constexpr int CT = 512, CW = CT / 64;  // threads and wavefronts that count one
+constexpr int SEG = 16384;             // elements of a segment of rows that are not longer than 64 such
 constexpr double kFine = 16.0;
 
 struct Segment {
   double weight[GRID];                 // sums of exp(f / 16), the first bin that of the maximum
   uint32_t count[GRID];
   double tail;                         // the weight below them, relative to the maximum
-  key_t top;                           // its largest key
-  uint32_t tail_count;
-  uint32_t pad[3];
+  key_t top;                           // its largest logit's key (the index of greedy rows only, else 0)
 };
 
 __host__ __device__ constexpr int64_t segment_length(int64_t V) {
@@ -432,110 +458,117 @@ __device__ __forceinline__ double grow(double f) {
   return p * r;
 }
 
-// One workgroup per segment of a row; its elements stay in registers between the maximum
-// and the histogram where they are at most SEG.
+// A row's choices.
+struct Choice {
+  float temperature, p, min_p, u;
+  int64_t k;
+  bool nan, greedy;                    // greedy: the first token of the order
+  __device__ Choice(const SampleArgs& a, int64_t t) {
+    temperature = a.temperature ? a.temperature[t] : 1.0f;
+    p = a.top_p ? a.top_p[t] : 1.0f;
+    min_p = a.min_p ? a.min_p[t] : 0.0f;
+    u = a.u[t];
+    k = a.top_k && a.top_k[t] > 0 && a.top_k[t] < a.V ? a.top_k[t] : a.V;
+    nan = temperature != temperature || p != p || min_p != min_p || u != u;
+    greedy = !nan && (temperature <= 0.0f || p <= 0.0f || k == 1);
+  }
+  template <typename T>
+  __device__ Row<T> row(Common& sh, const T* x, int64_t V, float m) const {
+    return Row<T>{sh, x, V, m, 1.0 / (double)temperature, min((double)max(min_p, 0.0f), 1.0)};
+  }
+};
+
+// One workgroup per segment of a row: a pass for the maximum, one for the histogram, one
+// for what lies below it where there is any; all but the first find the segment in the
+// cache.
 template <typename T>
-__global__ __launch_bounds__(NT, 8) void sample_count_kernel(SampleArgs a) {
-  constexpr int VEC = vec_of<T>(), U = 16 / VEC;
+__global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
   __shared__ unsigned long long bins[GRID][COLUMNS];
-  __shared__ key_t tops[NW];
-  __shared__ double red[NW];
-  __shared__ uint32_t counts[NW];
+  __shared__ float tops[CW];
+  __shared__ double red[CW];
+  __shared__ uint32_t counts[CW];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t length = segment_length(a.V), from = blockIdx.x * length, to = min(a.V, from + length);
+  const int c = 64 - __clzll((unsigned long long)ceil_div(min(length, a.V), COLUMNS)) + 1, q = min(67 - 2 * c, 51);
   for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
     const T* x = static_cast<const T*>(a.logits) + t * a.ld;
     Segment* out = static_cast<Segment*>(a.workspace) + t * gridDim.x + blockIdx.x;
-    for (int i = threadIdx.x; i < GRID * COLUMNS; i += NT) (&bins[0][0])[i] = 0;
-    float v[U][VEC];
-    const auto load = [&](int64_t j0) {           // 16 elements from a run of SEG, -inf past the end
+    for (int i = threadIdx.x; i < GRID * COLUMNS; i += CT) (&bins[0][0])[i] = 0;
+    float m = -INFINITY;
+    visit<4, CW>(x, from, to, [&](int64_t, float v) { m = __builtin_elementwise_maximum(m, v); });   // NaN where one is
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        const int64_t j = j0 + ((int64_t)i * NT + threadIdx.x) * VEC;
-        if (j + VEC <= to) {
-          load_n(x + j, v[i]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) v[i][e] = j + e < to ? (float)x[j + e] : -INFINITY;
-        }
-      }
-    };
-    float best = -INFINITY;
-    int64_t at = from;
-    for (int64_t j0 = from; j0 < to; j0 += SEG) {
-      load(j0);
-#pragma unroll
-      for (int i = 0; i < U; ++i)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (v[i][e] > best || v[i][e] != v[i][e]) best = v[i][e], at = j0 + ((int64_t)i * NT + threadIdx.x) * VEC + e;
-    }
-    key_t top = key_of(best, (uint32_t)at);
-#pragma unroll
-    for (int off = 32; off >= 1; off >>= 1) top = max(top, (key_t)__shfl_xor(top, off, kWave));
-    if (lane == 0) tops[w] = top;
+    for (int off = 32; off >= 1; off >>= 1) m = __builtin_elementwise_maximum(m, __shfl_xor(m, off, kWave));
+    if (lane == 0) tops[w] = m;
     __syncthreads();
-    top = tops[0];
+    m = tops[0];
 #pragma unroll
-    for (int i = 1; i < NW; ++i) top = max(top, tops[i]);
-    const float m = key_value((uint32_t)(top >> 32)), temperature = a.temperature ? a.temperature[t] : 1.0f;
-    double tail = 0.0;
+    for (int i = 1; i < CW; ++i) m = __builtin_elementwise_maximum(m, tops[i]);
+    const Choice choice(a, t);
+    uint32_t at = UINT32_MAX;                     // a greedy row's token: the first with the maximum
+    if (choice.greedy) {
+#pragma unroll 1
+      for (int64_t j = from + threadIdx.x; j < to && at == UINT32_MAX; j += CT)
+        if ((float)x[j] == m) at = (uint32_t)j;
+#pragma unroll
+      for (int off = 32; off >= 1; off >>= 1) at = min(at, (uint32_t)__shfl_xor((int)at, off, kWave));
+      if (lane == 0) counts[w] = at;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < CW; ++i) at = min(at, counts[i]);
+      __syncthreads();
+    }
     uint32_t tail_count = 0;
     // (rows that are greedy, not finite or have no choice need no more than the maximum)
-    const bool some = m > -INFINITY && m < INFINITY && temperature > 0.0f;
-    const int c = 64 - __clzll((unsigned long long)ceil_div(min(length, a.V), COLUMNS)) + 1, q = min(67 - 2 * c, 51);
+    const bool some = m > -INFINITY && m < INFINITY && !choice.greedy;
+    const double it = 1.0 / (double)choice.temperature, scale = kFine * it, first = floor((double)m * scale);
     if (some) {
-      const double it = 1.0 / (double)temperature, scale = kFine * it, first = floor((double)m * scale);
       // p + 2^(52 - q) holds p in steps of 2^-q in its last bits; the count's one is added
       // and the sum's exponent taken off at once
       const double magic = ldexp(1.0, 52 - q);
       const unsigned long long one = ((unsigned long long)1 << (64 - c)) - (unsigned long long)__double_as_longlong(magic);
       unsigned long long* column = &bins[0][lane & (COLUMNS - 1)];
-      for (int64_t j0 = from; j0 < to; j0 += SEG) {
-        if (to - from > SEG) load(j0);
-#pragma unroll
-        for (int i = 0; i < U; ++i)
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            const double y = (double)v[i][e] * scale, bin = floor(y), place = first - bin;
-            if (place < (double)GRID) {
-              const double p = grow(fma((double)v[i][e], scale, -bin));
-              atomicAdd(column + (int)place * COLUMNS, (unsigned long long)__double_as_longlong(p + magic) + one);
-            } else if (v[i][e] > -INFINITY) {
-              tail += exp(((double)v[i][e] - (double)m) * it);
-              ++tail_count;
-            }
-            if (e & 1) __builtin_amdgcn_sched_barrier(0);   // (two at a time: sixteen at once would not fit the registers)
-          }
-      }
+      visit<1, CW>(x, from, to, [&](int64_t, float v) {
+        const double bin = floor((double)v * scale), place = first - bin;
+        if (place < (double)GRID) {
+          const double p = grow(fma((double)v, scale, -bin));
+          atomicAdd(column + (int)place * COLUMNS, (unsigned long long)__double_as_longlong(p + magic) + one);
+        } else if (v > -INFINITY) {
+          ++tail_count;
+        }
+      });
     }
-    tail = wave_sum(tail);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) tail_count += __shfl_xor(tail_count, off, kWave);
-    if (lane == 0) red[w] = tail, counts[w] = tail_count;
+    if (lane == 0) counts[w] = tail_count;
     __syncthreads();
-    if (threadIdx.x < GRID) {
+    tail_count = 0;
+#pragma unroll
+    for (int i = 0; i < CW; ++i) tail_count += counts[i];
+    double tail = 0.0;
+    if (tail_count > 0) {
+#pragma unroll 1
+      for (int64_t j = from + threadIdx.x; j < to; j += CT) {
+        const float v = (float)x[j];
+        if (v > -INFINITY && !(first - floor((double)v * scale) < (double)GRID)) tail += exp(((double)v - (double)m) * it);
+      }
+      tail = block_sum<CW>(tail, red);
+    }
+    for (int g = threadIdx.x; g < GRID; g += CT) {
       unsigned long long sum = 0;
       uint32_t n = 0;
-      if (some) {
-        const unsigned long long low = ((unsigned long long)1 << (64 - c)) - 1;
-#pragma unroll
-        for (int k = 0; k < COLUMNS; ++k) {       // (staggered over the banks)
-          const unsigned long long b = bins[threadIdx.x][(k + threadIdx.x) & (COLUMNS - 1)];
-          sum += b & low;
-          n += (uint32_t)(b >> (64 - c));
-        }
+      const unsigned long long low = ((unsigned long long)1 << (64 - c)) - 1;
+#pragma unroll 4
+      for (int k = 0; k < COLUMNS; ++k) {         // (staggered over the banks)
+        const unsigned long long b = bins[g][(k + g) & (COLUMNS - 1)];
+        sum += b & low;
+        n += (uint32_t)(b >> (64 - c));
       }
-      out->weight[threadIdx.x] = (double)n + ldexp((double)sum, -q);
-      out->count[threadIdx.x] = n;
+      out->weight[g] = (double)n + ldexp((double)sum, -q);
+      out->count[g] = n;
     }
     if (threadIdx.x == 0) {
-      double s = 0.0;
-      uint32_t n = 0;
-      for (int i = 0; i < NW; ++i) s += red[i], n += counts[i];
-      out->tail = s;
-      out->tail_count = n;
-      out->top = top;
+      out->tail = tail;
+      out->top = choice.greedy ? key_of(m, at) : key_of(m, 0);
     }
     __syncthreads();
   }
@@ -543,21 +576,37 @@ __global__ __launch_bounds__(NT, 8) void sample_count_kernel(SampleArgs a) {
 
 // ---- The draw, one workgroup per row
 // The first n keys of sh.listed in descending order (n <= LISTED; the rest up to the next
-// power of two is cleared).
-__device__ __forceinline__ void sort_list(Shared& sh, int n) {
-  int size = NT;
+// power of two is cleared). Bitonic merges: up to 64 keys by one wavefront's shuffles.
+__device__ __forceinline__ void sort_list(PickShared& sh, int n) {
+  int size = 64;
   while (size < n) size *= 2;
   for (int i = n + threadIdx.x; i < size; i += NT) sh.listed[i] = 0;
   __syncthreads();
-  if (size == NT) {
-    const key_t mine = sorted(sh, sh.listed[threadIdx.x]);
-    sh.listed[threadIdx.x] = mine;
+  const int t = threadIdx.x;
+  if (size <= NT) {
+    key_t mine = t < size ? sh.listed[t] : 0;
+    for (int k = 2; k <= size; k <<= 1)
+      for (int s = k >> 1; s > 0; s >>= 1) {
+        key_t other;
+        if (s >= 64) {
+          __syncthreads();
+          if (t < size) sh.listed[t] = mine;
+          __syncthreads();
+          other = sh.listed[t & (size - 1) ^ s];
+        } else {
+          if (t >= size) continue;
+          other = __shfl_xor(mine, s, kWave);
+        }
+        mine = ((t & k) == 0) == ((t & s) == 0) ? max(mine, other) : min(mine, other);
+      }
+    __syncthreads();
+    if (t < size) sh.listed[t] = mine;
     __syncthreads();
     return;
   }
   for (int k = 2; k <= size; k <<= 1)
     for (int s = k >> 1; s > 0; s >>= 1) {
-      for (int i = threadIdx.x; i < size / 2; i += NT) {
+      for (int i = t; i < size / 2; i += NT) {
         const int p = 2 * i - (i & (s - 1)), r = p + s;   // a pair s apart
         const key_t u = sh.listed[p], v = sh.listed[r];
         if (((p & k) == 0) == (u < v)) sh.listed[p] = v, sh.listed[r] = u;
@@ -567,8 +616,16 @@ __device__ __forceinline__ void sort_list(Shared& sh, int n) {
 }
 // sh.sums: running sums of weight(key) over the first n of sh.listed.
 template <typename F>
-__device__ __forceinline__ void sum_list(Shared& sh, int n, F weight) {
+__device__ __forceinline__ void sum_list(PickShared& sh, int n, F weight) {
   const int per = (n + NT - 1) / NT, j0 = threadIdx.x * per;
+  if (n <= 64) {
+    if (threadIdx.x < 64) {
+      const double s = wave_running((int)threadIdx.x < n ? weight(sh.listed[threadIdx.x]) : 0.0);
+      if ((int)threadIdx.x < n) sh.sums[threadIdx.x] = s;
+    }
+    __syncthreads();
+    return;
+  }
   double s = 0.0, total;
   for (int e = 0; e < per; ++e)
     if (j0 + e < n) s += weight(sh.listed[j0 + e]);
@@ -580,7 +637,7 @@ __device__ __forceinline__ void sum_list(Shared& sh, int n, F weight) {
 // The first i < n for which is(i) holds, n where there is none (is() once true stays so
 // but for rounding).
 template <typename F>
-__device__ __forceinline__ int first_of(Shared& sh, int n, F is) {
+__device__ __forceinline__ int first_of(PickShared& sh, int n, F is) {
   const int per = (n + NT - 1) / NT, j0 = threadIdx.x * per;
   int at = n;
   for (int e = per - 1; e >= 0; --e)
@@ -598,7 +655,7 @@ __device__ __forceinline__ int first_of(Shared& sh, int n, F is) {
 // cuts are known from running sums over the bins; only their tokens are looked for in
 // the row and put in order, and where all that is kept is few, these, too.
 template <typename T>
-__device__ __forceinline__ int64_t pick(Shared& sh, Row<T>& row, const Segment* seg, int segs, int64_t length, int64_t k, double p,
+__device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segment* seg, int segs, int64_t length, int64_t k, double p,
                         double u, double& share) {
   const double scale = kFine * row.it, y = (double)row.m * scale, first = floor(y), f0 = fma((double)row.m, scale, -first);
   const int g = threadIdx.x;
@@ -681,17 +738,13 @@ __device__ __forceinline__ int64_t pick(Shared& sh, Row<T>& row, const Segment* 
       const double d = first - floor((double)v * scale);
       return d < (double)GRID ? (int)d : GRID;
     };
-    for (int s = 0; s < segs; ++s) {
-      if (key_value((uint32_t)(seg[s].top >> 32)) < low) continue;
-      const int64_t from = s * length, to = min(row.V, from + length);
-      visit(row.x, from, to, [&](int64_t j, float v) {
-        if (!(v >= low) || v == -INFINITY) return;
-        const int b = bin_of(v);
-        if (!((b >= lo && b <= hi) || (far && b == kb))) return;
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < LISTED) sh.listed[at] = key_of(v, (uint32_t)j);
-      });
-    }
+    visit<4>(row.x, 0, row.V, [&](int64_t j, float v) {
+      if (!(v >= low) || v == -INFINITY) return;
+      const int b = bin_of(v);
+      if (!((b >= lo && b <= hi) || (far && b == kb))) return;
+      const int at = atomicAdd(&sh.n, 1);
+      if (at < LISTED) sh.listed[at] = key_of(v, (uint32_t)j);
+    });
     __syncthreads();
     const int size = min(sh.n, LISTED);
     __syncthreads();
@@ -788,9 +841,18 @@ __device__ __forceinline__ int64_t pick(Shared& sh, Row<T>& row, const Segment* 
   return token;
 }
 
+constexpr int64_t kAside = -2;         // in a token's place: the row is left to sample_aside_kernel
+
+__device__ __forceinline__ void put_token(const SampleArgs& a, int64_t t, int64_t token, double logp) {
+  if (threadIdx.x != 0) return;
+  if (a.wide) static_cast<int64_t*>(a.tokens)[t] = token;
+  else static_cast<int32_t*>(a.tokens)[t] = (int32_t)token;
+  if (a.logp) a.logp[t] = (float)logp;
+}
+
 template <typename T>
 __global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs) {
-  __shared__ Shared sh;
+  __shared__ PickShared sh;
   const int64_t length = segment_length(a.V);
   for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
     const T* x = static_cast<const T*>(a.logits) + t * a.ld;
@@ -798,35 +860,45 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs)
     key_t top = 0;
     for (int s = 0; s < segs; ++s) top = max(top, seg[s].top);
     const float m = key_value((uint32_t)(top >> 32));
-    const float temperature = a.temperature ? a.temperature[t] : 1.0f, p = a.top_p ? a.top_p[t] : 1.0f;
-    const float min_p = a.min_p ? a.min_p[t] : 0.0f, u = a.u[t];
-    const int64_t k = a.top_k && a.top_k[t] > 0 && a.top_k[t] < a.V ? a.top_k[t] : a.V;
-    const bool nan = temperature != temperature || p != p || min_p != min_p || u != u || m != m || m == INFINITY;
+    const Choice choice(a, t);
+    const bool nan = choice.nan || m != m || m == INFINITY;
     int64_t token = -1;
     double logp = __builtin_nan("");
     if (!nan && m == -INFINITY) {
       logp = -INFINITY;
-    } else if (!nan && (temperature <= 0.0f || p <= 0.0f || k == 1)) {
+    } else if (!nan && choice.greedy) {
       token = (int64_t)(uint32_t)~(uint32_t)top;
       logp = 0.0;
     } else if (!nan) {
-      Row<T> row{sh, x, a.V, m, 1.0 / (double)temperature, min((double)max(min_p, 0.0f), 1.0)};
-      const double goal_of = max((double)u, 0.0);
+      Row<T> row = choice.row(sh, x, a.V, m);
       double share;
-      token = pick(sh, row, seg, segs, length, k, (double)p, goal_of, share);
-      if (token < 0) {                            // the cuts are not where the histograms see them
-        key_t cut = 0;
-        if (k < a.V) cut = row.kth(k, top);
-        if (p < 1.0f) cut = row.reach_p((double)p, cut);
-        token = row.draw(cut, goal_of, share);
-      }
+      token = pick(sh, row, seg, segs, length, choice.k, (double)choice.p, max((double)choice.u, 0.0), share);
+      if (token < 0) token = kAside;
       logp = log(share);
     }
-    if (threadIdx.x == 0) {
-      if (a.wide) static_cast<int64_t*>(a.tokens)[t] = token;
-      else static_cast<int32_t*>(a.tokens)[t] = (int32_t)token;
-      if (a.logp) a.logp[t] = (float)logp;
-    }
+    put_token(a, t, token, logp);
+    __syncthreads();
+  }
+}
+
+// The rows whose cuts the histograms do not see: by passes over the row alone.
+template <typename T>
+__global__ __launch_bounds__(NT) void sample_aside_kernel(SampleArgs a) {
+  __shared__ Shared sh;
+  for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
+    const int64_t mark = a.wide ? static_cast<const int64_t*>(a.tokens)[t] : static_cast<const int32_t*>(a.tokens)[t];
+    if (mark != kAside) continue;
+    const T* x = static_cast<const T*>(a.logits) + t * a.ld;
+    const Segment* seg = static_cast<const Segment*>(a.workspace) + t * segments(a.V);
+    key_t top = 0, cut = 0;
+    for (int s = 0; s < (int)segments(a.V); ++s) top = max(top, seg[s].top);
+    const Choice choice(a, t);
+    Passes<T> row(sh, choice.row(sh, x, a.V, key_value((uint32_t)(top >> 32))));
+    if (choice.k < a.V) cut = row.kth(choice.k, top | UINT32_MAX);
+    if (choice.p < 1.0f) cut = row.reach_p((double)choice.p, cut);
+    double share;
+    const int64_t token = row.draw(cut, max((double)choice.u, 0.0), share);
+    put_token(a, t, token, log(share));
     __syncthreads();
   }
 }
@@ -834,8 +906,9 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs)
 template <typename T>
 int sample_as(hipStream_t s, const SampleArgs& a) {
   const int segs = (int)segments(a.V);
-  hipLaunchKernelGGL(sample_count_kernel<T>, dim3(segs, (unsigned)std::min<int64_t>(a.T, 65535)), dim3(NT), 0, s, a);
+  hipLaunchKernelGGL(sample_count_kernel<T>, dim3(segs, (unsigned)std::min<int64_t>(a.T, 65535)), dim3(CT), 0, s, a);
   hipLaunchKernelGGL(sample_pick_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T, 65535)), dim3(NT), 0, s, a, segs);
+  hipLaunchKernelGGL(sample_aside_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T, 256)), dim3(NT), 0, s, a);
   KMP_LAUNCH_CHECK();
   return 0;
 }
