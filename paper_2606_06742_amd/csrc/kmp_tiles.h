@@ -288,17 +288,21 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void tile_kernel(TileArgs a, typ
   Epi::template store<MB, NB>(out, acc, m0 + wr * MB * 32, n0 + wc * NB * 32, lane, lds + SUMS + wg * REGION);
 }
 
-// The larger forms, aligned rows: slices as in tile_kernel in a ring of NS
-// stages, and the operands of every 32 bytes of k are read from LDS while the 32
-// before them are multiplied. The barrier of slice s stands before its last 32:
-// their operands are in registers, so that the stage is free for slice s + NS, and
-// slice s + 1 has landed, so that its first operands can be read behind the last
-// products of s: no product waits for LDS or for the barrier. (Slices of 64 bytes
-// through four stages had twice the requests to the second-level cache.)
+// The larger forms, aligned rows: slices as in tile_kernel in a ring of NS stages, and
+// the operands of every 32 bytes of k are read from LDS while the 32 before them are
+// multiplied: reads and loads are issued between the products, whose issue takes an
+// eighth of the time that the matrix cores need for one (all of them ahead of a group of
+// products left the cores idle: 4096 x 8192 x 4096 in 16 bits @BEFORE / @AFTER us). The
+// barrier of slice s stands within its last products: their operands are in registers,
+// so that the stage is free for slice s + NS, and slice s + 1 has landed, so that its
+// first operands can be read behind them. A slice past the end is the last one again,
+// unused, which keeps the number of loads under way the same. (Slices of 64 bytes
+// through four or five stages: 4 % slower.)
 template <typename E, typename Epi, int TM, int TN, int WR, int WC, int NS>
 __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typename Epi::Args out, int tm, int tn) {
   constexpr int NW = WR * WC, MB = TM / WR / 32, NB = TN / WC / 32, QA = TM / 8 / NW, QB = TN / 8 / NW;
   constexpr int SL = 128, STAGE = (TM + TN) * SL;
+  constexpr int READS = MB + NB, MULS = MB * NB, LOADS = QA + QB;
   static_assert(QA % 2 == 0 && QB % 2 == 0, "pairs of eight rows");
   static_assert(NW * Epi::template region_bytes<MB, NB>() <= NS * STAGE, "the regions fit the ring");
   __shared__ __align__(16) int8_t lds[NS * STAGE];
@@ -315,55 +319,62 @@ __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typenam
 #pragma unroll
   for (int q = 0; q < QB; ++q) pb[q] = a.w + min(n0 + (w * QB + q) * 8 + lr, a.N - 1) * a.ldw + lc[q & 1];
   const uint32_t base = (uint32_t)(uintptr_t)lds;                     // LDS addresses have 32 bits
-  const auto fetch = [&](int s) {
+  const int whole = (int)a.K / SL, tail = (int)a.K % SL;
+  const auto fetch_one = [&](int s, int i) {                          // load i of LOADS of slice s
     const uint32_t at = base + s % NS * STAGE;
-#pragma unroll
-    for (int q = 0; q < QA; ++q) load_to_lds(pa[q] + s * SL, at + (w * QA + q) * 1024);
-#pragma unroll
-    for (int q = 0; q < QB; ++q) load_to_lds(pb[q] + s * SL, at + TM * SL + (w * QB + q) * 1024);
+    const int k = min(s, whole - 1) * SL;
+    if (i < QA) load_to_lds(pa[i < QA ? i : 0] + k, at + (w * QA + i) * 1024);
+    else load_to_lds(pb[i < QA ? 0 : i - QA] + k, at + TM * SL + (w * QB + i - QA) * 1024);
   };
   typename Blocks<E>::acc_t acc[MB][NB] = {};
   const int row = lane & 31, half = lane >> 5;
   const int8_t* la = lds + (wr * MB * 32 + row) * SL;
   const int8_t* lb = lds + TM * SL + (wc * NB * 32 + row) * SL;
   int4v fa[2][MB], fb[2][NB];
-  const auto read = [&](int s, int h) {                               // bytes 32 h .. of slice s
+  const auto read_one = [&](int s, int h, int i) {                    // operand i of READS: bytes 32 h .. of slice s
     const int c = ((2 * h + half) ^ (row >> 1 & 7)) * 16 + s % NS * STAGE;
-#pragma unroll
-    for (int i = 0; i < MB; ++i) fa[h & 1][i] = *reinterpret_cast<const int4v*>(la + i * 32 * SL + c);
-#pragma unroll
-    for (int j = 0; j < NB; ++j) fb[h & 1][j] = *reinterpret_cast<const int4v*>(lb + j * 32 * SL + c);
-    __builtin_amdgcn_sched_barrier(0);                                // (else the reads sink to their uses)
+    if (i < NB) fb[h & 1][i < NB ? i : 0] = *reinterpret_cast<const int4v*>(lb + i * 32 * SL + c);
+    else fa[h & 1][i < NB ? 0 : i - NB] = *reinterpret_cast<const int4v*>(la + (i - NB) * 32 * SL + c);
   };
-  const auto multiply = [&](int h) {
-#pragma unroll
-    for (int i = 0; i < MB; ++i)
-#pragma unroll
-      for (int j = 0; j < NB; ++j)
-        acc[i][j] = Blocks<E>::multiply(fb[h & 1][j], fa[h & 1][i], acc[i][j]);
-    __builtin_amdgcn_sched_barrier(0);
+  const auto multiply_one = [&](int h, int i) {
+    acc[i / NB][i % NB] = Blocks<E>::multiply(fb[h & 1][i % NB], fa[h & 1][i / NB], acc[i / NB][i % NB]);
   };
-  const int whole = (int)a.K / SL, tail = (int)a.K % SL;
+  // products [from, to) of step h, `ops` of op(0), op(1), .. dealt out between them
+  const auto multiply = [&](int h, int from, int to, int ops, auto op) {
+#pragma unroll
+    for (int i = from; i < to; ++i) {
+      multiply_one(h, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int o = ops * (i - from) / (to - from); o < ops * (i - from + 1) / (to - from); ++o) op(o);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
   if (whole > 0) {
-    for (int s = 0; s < min(NS, whole); ++s) fetch(s);
-    if (whole >= NS) wait_loads<(NS - 1) * (QA + QB)>();
-    else wait_loads<0>();
-    barrier();
-    read(0, 0);
-    for (int s = 0; s < whole; ++s) {
 #pragma unroll
-      for (int h = 0; h < 3; ++h) {
-        read(s, h + 1);
-        multiply(h);
-      }
-      if (s + NS <= whole) wait_loads<(NS - 2) * (QA + QB)>();        // s + 1 has landed, the later ones may not have
-      else wait_loads<0>();
+    for (int s = 0; s < NS; ++s)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) fetch_one(s, i);
+    wait_loads<(NS - 1) * LOADS>();
+    barrier();
+#pragma unroll
+    for (int i = 0; i < READS; ++i) read_one(0, 0, i);
+    for (int s = 0; s + 1 < whole; ++s) {
+#pragma unroll
+      for (int h = 0; h < 3; ++h) multiply(h, 0, MULS, READS, [&](int i) { read_one(s, h + 1, i); });
+      multiply(3, 0, MULS / 2, 0, [](int) {});
+      wait_loads<(NS - 2) * LOADS>();                                 // s + 1 has landed, the later ones may not have
       wait_lds();                                                     // the last operands of s are here
       barrier();
-      if (s + NS < whole) fetch(s + NS);
-      if (s + 1 < whole) read(s + 1, 0);
-      multiply(3);
+      multiply(3, MULS / 2, MULS, READS + LOADS, [&](int i) {
+        if (i < READS) read_one(s + 1, 0, i);
+        else fetch_one(s + NS, i - READS);
+      });
     }
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      multiply(h, 0, MULS, h < 3 ? READS : 0, [&](int i) { read_one(whole - 1, h + 1, i); });
+    wait_loads<0>();                                                  // (what was fetched past the end)
   }
   if (tail > 0) {                                                     // zeros past K
     __syncthreads();
@@ -378,8 +389,10 @@ __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typenam
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
-      read(0, h);
-      multiply(h);
+#pragma unroll
+      for (int i = 0; i < READS; ++i) read_one(0, h, i);
+#pragma unroll
+      for (int i = 0; i < MULS; ++i) multiply_one(h, i);
     }
   }
   __syncthreads();                                                    // the ring is free

@@ -129,19 +129,131 @@ struct DenseTile {
   }
 };
 
+// Few tokens: a workgroup takes 16 channels and up to 16 tokens, its four wavefronts
+// each a run of the 64-byte slices of k, both operands from memory to registers, DEEP
+// slices in flight; the wavefronts' sums are added in LDS in their order. w is the first
+// operand of a block of 16 x 16, so that a lane has four channels of one token. Rows past
+// the end repeat the last one and are not stored. Bound by reading w once.
+template <typename E, typename O>
+__global__ __launch_bounds__(256) void dense_few_kernel(TileArgs a, OutArgs o) {
+  constexpr int DEEP = 8;
+  __shared__ float sums[4][4][64];
+  const int t = threadIdx.x, lane = t & 63, w = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int row = lane & 15, c = (lane >> 4) * 16;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int8_t* pw = a.w + min(n0 + row, a.N - 1) * a.ldw;
+  const int8_t* px = a.x + min((int64_t)row, a.M - 1) * a.ldx;
+  // whole slices, dealt to the wavefronts in runs of n from s0 on
+  const int whole = (int)(a.K / 64), run = (whole + 3) / 4;
+  const int s0 = min(w * run, whole), n = min(s0 + run, whole) - s0;
+  typename Blocks<E>::acc16_t acc = {};
+  int4v fw[DEEP], fx[DEEP];
+  const auto fetch = [&](int i, int4v& vw, int4v& vx) {
+    const int k = 64 * (s0 + min(i, n - 1)) + c;  // past the end: the last slice again, unused
+    __builtin_memcpy(&vw, pw + k, 16);
+    __builtin_memcpy(&vx, px + k, 16);
+  };
+  if (n > 0) {
+#pragma unroll
+    for (int p = 0; p < DEEP; ++p) fetch(p, fw[p], fx[p]);
+    int i = 0;
+    for (; i + DEEP < n; i += DEEP) {
+#pragma unroll
+      for (int p = 0; p < DEEP; ++p) {
+        acc = Blocks<E>::multiply16(fw[p], fx[p], acc);
+        fetch(i + DEEP + p, fw[p], fx[p]);
+      }
+    }
+#pragma unroll
+    for (int p = 0; p < DEEP; ++p)
+      if (i + p < n) acc = Blocks<E>::multiply16(fw[p], fx[p], acc);
+  }
+  if (w == 3 && a.K % 64 != 0)                    // the rest of k, zeros past its end
+    acc = Blocks<E>::multiply16(chunk16(pw, 64 * (int64_t)whole + c, a.K), chunk16(px, 64 * (int64_t)whole + c, a.K), acc);
+#pragma unroll
+  for (int r = 0; r < 4; ++r) sums[w][r][lane] = acc[r];
+  __syncthreads();
+  if (w > 0 || row >= a.M) return;
+  const int64_t n1 = n0 + (lane >> 4) * 4;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    if (n1 + r >= a.N) continue;
+    float v = ((sums[0][r][lane] + sums[1][r][lane]) + sums[2][r][lane]) + sums[3][r][lane];
+    if (o.bias) v += bias_at<E>(o, n1 + r);
+    if (o.z) static_cast<E*>(o.z)[row * o.ldz + n1 + r] = (E)v;
+    v = activate(o.act, v);
+    if (o.residual) v += (float)static_cast<const O*>(o.residual)[row * o.ldr + n1 + r];
+    static_cast<O*>(o.out)[row * o.ldo + n1 + r] = (O)v;
+  }
+}
+template <typename E, typename O>
+int few_as(hipStream_t s, const TileArgs& a, const OutArgs& out) {
+  hipLaunchKernelGGL((dense_few_kernel<E, O>), dim3((unsigned)ceil_div(a.N, 16)), dim3(256), 0, s, a, out);
+  KMP_LAUNCH_CHECK();
+  return 0;
+}
+
+// Which form, by what keeps the chip's 256 compute units busy. us per launch at M x N x
+// K, operands from HBM: few tokens; tiles of 32 x 64 (four groups over k, ring of 3), 64 x
+// 64 (two groups, ring of 3, or of 2; one group, ring of 2), operands ahead in tiles of
+// 128 (ring of 4, or of 2), 256 x 128 and 256 x 256; the floor, the larger of the bytes
+// at a copy's 4.93 TB/s and the products at the 1574 TFLOP/s (bf16; f32: 155) of the
+// library's product of order 8192. In bf16:
+//                      few  32x64  64,3  64,2  64,1 128,4 128,2 256,128 256  floor
+//   1 x 4096 x 4096    9.0  11.8  16.5  21.1  30.9  31.7  38.9  47.7  75.4   6.8
+//   1 x 16384 x 4096  24.6  29.8  30.9  37.1  52.4  38.0  61.7  70.0  90.9  27.2
+//   16 x 8192 x 4096  18.9  16.3  18.2  29.3  45.6  32.3  54.9  64.3  80.0  13.7
+//   16 x 32000 x 2048 39.0  34.2  34.8  33.2  34.8  33.9  38.7  43.9  54.6  26.8
+//   64 x 4096 x 4096        14.1  17.5  23.4  31.8  34.5  42.5  53.0  79.8   7.0
+//   64 x 12288 x 4096       37.1  28.0  36.3  51.1  39.3  63.3  73.9  94.2  20.8
+//   256 x 4096 x 4096       26.6  19.6  25.0  33.3  35.7  43.3  57.6  87.5   7.7
+//   512 x 4096 x 4096       51.4  38.1  30.7  37.7  38.0  44.3  57.1  86.8  10.9
+//   600 x 4500 x 704        30.3  19.4  16.0  12.7  14.1  14.8  20.6  35.0   2.6
+//   1000 x 3000 x 4096      71.4  51.6  50.6  43.9  39.5  45.1  57.6  87.2  15.6
+//   1024 x 4096 x 4096      99.3  69.1  56.4  61.8  45.5  48.1  59.0  88.7  21.8
+//   2048 x 2048 x 2048      61.2  41.4  32.7  33.2  26.9  28.9  35.4  53.1  10.9
+//   1024 x 8192 x 4096       236   155   129   126  89.0  79.0  78.8   104  43.7
+//   2048 x 4096 x 4096       182   132   107   113  85.0  78.5  71.3  98.4  43.7
+//   3000 x 5000 x 1000       197   118  87.3  73.2  70.1  58.2  58.5  48.2  19.1
+//   4096 x 4096 x 4096       368   276   225   224   171   154   155   124  87.3
+//   4096 x 8192 x 4096             574   471   462   342   304   313   242   175
+// In f32 (128: of four wavefronts, ring of 2):
+//                      few  32x64  64,2   128  floor
+//   1 x 4096 x 4096   14.1  42.5  76.2   251  13.6
+//   128 x 4096 x 1000       19.0  25.5  75.1   6.8
+//   1024 x 1024 x 1024      31.7  26.4  73.2  13.9
+//   2048 x 2048 x 2048       205   156   137   111
+//   4096 x 4096 x 1024       435   303   274   222
+// Rows that are not aligned, f16: few tokens; tiles of 32 x 64 (four groups), 64 and 128:
+//                      few  32x64    64   128  floor
+//   16 x 4096 x 4097  11.5  17.8  22.1  36.3   6.9
+//   77 x 2051 x 8191        23.9  31.6  59.4   7.1
+//   128 x 4096 x 4097       20.9  24.5  45.4   7.2
+//   512 x 4096 x 4097       75.2  45.8  45.6  11.4
+//   1244 x 1824 x 5001       108  72.5  55.2  15.1
+//   4096 x 4096 x 4097       573   329   206  91.4
 template <typename E, typename O>
 int product_as(hipStream_t s, const TileArgs& a, const OutArgs& out) {
   typedef DenseTile<E, O> S;
   const auto tiles = [&](int tm, int tn) { return ceil_div(a.M, tm) * ceil_div(a.N, tn); };
+  if (a.M <= 16 && (a.N <= 6144 || a.M <= 4)) return few_as<E, O>(s, a, out);
   if (!aligned_rows(a)) {
     if (tiles(32, 64) <= 256) return tiles_as<E, S, 32, 64, 1, 2, 4, 2, false>(s, a, out);
     if (tiles(64, 64) <= 512) return tiles_as<E, S, 64, 64, 2, 2, 1, 2, false>(s, a, out);
     return tiles_as<E, S, 128, 128, 2, 4, 1, 2, false>(s, a, out);
   }
   if (tiles(32, 64) <= 256) return tiles_as<E, S, 32, 64, 1, 2, 4, 3, true>(s, a, out);
-  if (tiles(64, 64) <= 512) return tiles_as<E, S, 64, 64, 2, 2, 2, 2, true>(s, a, out);
-  if (tiles(256, 256) < 192) return ahead_as<E, S, 128, 128, 2, 4, 2>(s, a, out);
-  return ahead_as<E, S, 256, 256, 2, 4, 2>(s, a, out);
+  if constexpr (sizeof(E) == 4) {
+    if (tiles(64, 64) <= 512) return tiles_as<E, S, 64, 64, 2, 2, 2, 2, true>(s, a, out);
+    return ahead_as<E, S, 128, 128, 2, 2, 2>(s, a, out);
+  } else {
+    if (tiles(64, 64) <= 256) return tiles_as<E, S, 64, 64, 2, 2, 2, 3, true>(s, a, out);
+    if (tiles(64, 64) <= 512) return tiles_as<E, S, 64, 64, 2, 2, 2, 2, true>(s, a, out);
+    if (tiles(64, 64) <= 768 && (a.K < 4096 || tiles(128, 128) > 256)) return tiles_as<E, S, 64, 64, 2, 2, 1, 2, true>(s, a, out);
+    if (tiles(128, 128) <= 256) return ahead_as<E, S, 128, 128, 2, 4, 4>(s, a, out);
+    if (tiles(256, 256) < 192) return ahead_as<E, S, 256, 128, 4, 2, 2>(s, a, out);
+    return ahead_as<E, S, 256, 256, 2, 4, 2>(s, a, out);
+  }
 }
 
 // ------------------------------------------------------------------- gradients
@@ -259,6 +371,147 @@ __global__ __launch_bounds__(1024) void bias_join_kernel(const float* partial, i
   }
 }
 
+// Few tokens (M <= MM <= 16) take no part of the above: reading w once for dx and
+// writing dw once is all that counts, and dz stays in 32 bits.
+// dz [M][N] and its column sums, a thread per column.
+template <typename T, typename W>
+__global__ __launch_bounds__(256) void few_dz_kernel(DenseBackArgs a, float* dz) {
+  for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < a.N; n += (int64_t)gridDim.x * 256) {
+    float sum = 0.0f;
+    for (int64_t m = 0; m < a.M; ++m) {
+      float v = (float)static_cast<const T*>(a.dout)[m * a.lddo + n];
+      if (a.act != KMP_ACT_NONE) v *= slope(a.act, (float)static_cast<const T*>(a.z)[m * a.ldz + n]);
+      dz[m * a.N + n] = v;
+      sum += v;
+    }
+    if (a.dbias) static_cast<W*>(a.dbias)[n] = (W)sum;
+  }
+}
+// N elements from k on of a row of K (zeros past its end), as 32-bit floats.
+template <typename T, int N>
+__device__ __forceinline__ void load_part(const T* p, int64_t k, int64_t K, float (&v)[N]) {
+  if (k + N <= K) {
+    load_n(p + k, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = k + e < K ? (float)p[k + e] : 0.0f;
+  }
+}
+// Sums over the run blockIdx.y of w's rows: a wavefront has 64 vectors of columns, the
+// workgroup's four every fourth row; partial[run][m][k].
+template <typename T, int MM>
+__global__ __launch_bounds__(256) void few_dx_kernel(DenseBackArgs a, const float* dz, float* partial, int64_t run) {
+  constexpr int VEC = vec_of<T>(), U = 4;
+  __shared__ float sums[3][MM][VEC][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t k = ((int64_t)blockIdx.x * 64 + lane) * VEC, from = blockIdx.y * run, to = min(a.N, from + run);
+  float acc[MM][VEC] = {};
+  for (int64_t n0 = from + w; n0 < to; n0 += 4 * U) {
+    float v[U][VEC], f[U][MM];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int64_t n = min(n0 + 4 * i, to - 1);
+      load_part(static_cast<const T*>(a.w) + n * a.ldw, k, a.K, v[i]);
+#pragma unroll
+      for (int m = 0; m < MM; ++m) f[i][m] = m < a.M && n0 + 4 * i < to ? dz[m * a.N + n] : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      if (n0 + 4 * i >= to) continue;             // (not 0 times what may be infinite)
+#pragma unroll
+      for (int m = 0; m < MM; ++m)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[m][e] += f[i][m] * v[i][e];
+    }
+  }
+  if (w > 0) {
+#pragma unroll
+    for (int m = 0; m < MM; ++m)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sums[w - 1][m][e][lane] = acc[m][e];
+  }
+  __syncthreads();
+  if (w > 0) return;
+#pragma unroll
+  for (int m = 0; m < MM; ++m) {
+    if (m >= a.M) continue;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float s = ((acc[m][e] + sums[0][m][e][lane]) + sums[1][m][e][lane]) + sums[2][m][e][lane];
+      if (k + e < a.K) partial[((int64_t)blockIdx.y * a.M + m) * a.K + k + e] = s;
+    }
+  }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void few_join_kernel(DenseBackArgs a, const float* partial, int runs) {
+  const int64_t all = a.M * a.K;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    float s = 0.0f;
+#pragma unroll 8
+    for (int r = 0; r < runs; ++r) s += partial[r * all + i];
+    static_cast<T*>(a.dx)[i / a.K * a.lddx + i % a.K] = (T)s;
+  }
+}
+// dw: a wavefront keeps the tokens' 64 vectors of columns and goes along its rows.
+template <typename T, int MM>
+__global__ __launch_bounds__(256) void few_dw_kernel(DenseBackArgs a, const float* dz, int64_t run) {
+  constexpr int VEC = vec_of<T>();
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t k = ((int64_t)blockIdx.x * 64 + lane) * VEC, from = blockIdx.y * run, to = min(a.N, from + run);
+  float x[MM][VEC];
+#pragma unroll
+  for (int m = 0; m < MM; ++m) load_part(static_cast<const T*>(a.x) + min((int64_t)m, a.M - 1) * a.ldx, k, a.K, x[m]);
+  if (k >= a.K) return;
+#pragma unroll 2
+  for (int64_t n = from + w; n < to; n += 4) {
+    float v[VEC] = {};
+#pragma unroll
+    for (int m = 0; m < MM; ++m) {
+      if (m >= a.M) continue;
+      const float f = dz[m * a.N + n];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) v[e] += f * x[m][e];
+    }
+    T* p = static_cast<T*>(a.dw) + n * a.lddw + k;
+    if (k + VEC <= a.K) {
+      store_n(p, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (k + e < a.K) p[e] = (T)v[e];
+    }
+  }
+}
+constexpr int kFew = 16;
+// Runs of w's rows, so that about 1024 workgroups read it, of 64 rows at least.
+int64_t few_runs(int64_t N, int64_t K, int vec) {
+  return std::max<int64_t>(1, std::min<int64_t>({ceil_div(N, 64), 1024 / ceil_div(std::max<int64_t>(K, 1), 64 * vec), 32768}));
+}
+// Bytes of dz and of the runs' sums; never fewer for larger M, N or K.
+int64_t few_bytes(int64_t M, int64_t N, int64_t K) {
+  M = std::min<int64_t>(M, kFew);
+  return round_up(M * N * 4, 256) + M * std::min<int64_t>(ceil_div(std::max<int64_t>(N, 1), 64) * K, 1024 * 512 + K) * 4;
+}
+template <typename T, int MM>
+int few_backward(hipStream_t s, const DenseBackArgs& a) {
+  constexpr int VEC = vec_of<T>();
+  float* dz = static_cast<float*>(a.workspace);
+  float* partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + round_up(a.M * a.N * 4, 256));
+  const dim3 columns((unsigned)std::min<int64_t>(ceil_div(a.N, 256), 1 << 20));
+  if (a.btype == KMP_F32) hipLaunchKernelGGL((few_dz_kernel<T, float>), columns, dim3(256), 0, s, a, dz);
+  else hipLaunchKernelGGL((few_dz_kernel<T, T>), columns, dim3(256), 0, s, a, dz);
+  const int64_t across = ceil_div(a.K, 64 * VEC), runs = few_runs(a.N, a.K, VEC);
+  if (a.dx && a.K > 0) {
+    hipLaunchKernelGGL((few_dx_kernel<T, MM>), dim3((unsigned)across, (unsigned)runs), dim3(256), 0, s, a, dz, partial, ceil_div(a.N, runs));
+    hipLaunchKernelGGL(few_join_kernel<T>, dim3((unsigned)std::min<int64_t>(ceil_div(a.M * a.K, 256), 1 << 20)), dim3(256), 0, s, a,
+                       partial, (int)runs);
+  }
+  if (a.dw && a.K > 0)
+    hipLaunchKernelGGL((few_dw_kernel<T, MM>), dim3((unsigned)across, (unsigned)runs), dim3(256), 0, s, a, dz, ceil_div(a.N, runs));
+  KMP_LAUNCH_CHECK();
+  return 0;
+}
+
 // What the workspace holds, each part's rows at multiples of 128 bytes.
 struct Layout {
   int64_t dz, dz_turned, x_turned, w_turned, partial, bytes;   // first bytes
@@ -271,7 +524,7 @@ struct Layout {
     x_turned = dz_turned + N * pm * size;
     w_turned = x_turned + K * pm * size;
     partial = w_turned + K * pn * size;
-    bytes = partial + round_up(ceil_div(M, 64) * N * 4, 256);
+    bytes = std::max(partial + round_up(ceil_div(M, 64) * N * 4, 256), few_bytes(M, N, K));
   }
 };
 
@@ -286,6 +539,12 @@ int turn(hipStream_t s, const TurnArgs& a) {
 template <typename T>
 int backward_as(hipStream_t s, const DenseBackArgs& a) {
   constexpr int SIZE = (int)sizeof(T);
+  if (a.M > 0 && a.N > 0 && a.M <= kFew) {
+    if (a.M == 1) return few_backward<T, 1>(s, a);
+    if (a.M <= 4) return few_backward<T, 4>(s, a);
+    if (a.M <= 8) return few_backward<T, 8>(s, a);
+    return few_backward<T, 16>(s, a);
+  }
   const Layout at(SIZE, a.M, a.N, a.K);
   char* ws = static_cast<char*>(a.workspace);
   float* partial = reinterpret_cast<float*>(ws + at.partial);
