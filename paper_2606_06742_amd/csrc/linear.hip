@@ -237,11 +237,17 @@ int product_as(hipStream_t s, const TileArgs& a, const OutArgs& out) {
   typedef DenseTile<E, O> S;
   const auto tiles = [&](int tm, int tn) { return ceil_div(a.M, tm) * ceil_div(a.N, tn); };
   if (a.M <= 16 && (a.N <= 6144 || a.M <= 4)) return few_as<E, O>(s, a, out);
+  // the fewest tiles: eight groups over k (32x64 above; us: 77 x 2051 x 8192 17.8 / 20.9,
+  // 64 x 1000 x 8192 13.8 / 19.7, 128 x 2048 x 4096 11.0 / 12.5; f32 77 x 2051 x 4096 27.9
+  // / 44.4; rows not aligned 77 x 2051 x 8191 29.9 / 39.2, 32 x 4096 x 4097 17.5 / 22.8)
+  const bool least = tiles(32, 32) <= 256;
   if (!aligned_rows(a)) {
+    if (least) return tiles_as<E, S, 32, 32, 1, 1, 8, 2, false>(s, a, out);
     if (tiles(32, 64) <= 256) return tiles_as<E, S, 32, 64, 1, 2, 4, 2, false>(s, a, out);
     if (tiles(64, 64) <= 512) return tiles_as<E, S, 64, 64, 2, 2, 1, 2, false>(s, a, out);
     return tiles_as<E, S, 128, 128, 2, 4, 1, 2, false>(s, a, out);
   }
+  if (least) return tiles_as<E, S, 32, 32, 1, 1, 8, 2, true>(s, a, out);
   if (tiles(32, 64) <= 256) return tiles_as<E, S, 32, 64, 1, 2, 4, 3, true>(s, a, out);
   if constexpr (sizeof(E) == 4) {
     if (tiles(64, 64) <= 512) return tiles_as<E, S, 64, 64, 2, 2, 2, 2, true>(s, a, out);
@@ -268,14 +274,17 @@ struct TurnArgs {
   void* turned; int64_t ldt;           // cols x rows, may be null
   float* partial;                      // [row tiles][cols], may be null
 };
+struct TurnsArgs { TurnArgs each[3]; int64_t tiles[3]; };   // up to three in one launch
 template <typename T>
-__global__ __launch_bounds__(256) void turn_kernel(TurnArgs a) {
+__global__ __launch_bounds__(256) void turn_kernel(TurnsArgs all) {
   constexpr int S = 64, VEC = vec_of<T>(), PER = S / VEC, RPI = 256 / PER;
   __shared__ T tile[S][S + 2];
   __shared__ float sums[RPI][S];
   const int lr = threadIdx.x / PER, c = threadIdx.x % PER * VEC;
-  const int64_t across = ceil_div(a.cols, S), tiles = ceil_div(a.rows, S) * across;
-  for (int64_t at = blockIdx.x; at < tiles; at += gridDim.x) {
+  for (int64_t job = blockIdx.x; job < all.tiles[0] + all.tiles[1] + all.tiles[2]; job += gridDim.x) {
+    const int which = job < all.tiles[0] ? 0 : job < all.tiles[0] + all.tiles[1] ? 1 : 2;
+    const TurnArgs a = all.each[which];
+    const int64_t at = job - (which > 0 ? all.tiles[0] : 0) - (which > 1 ? all.tiles[1] : 0), across = ceil_div(a.cols, S);
     const int64_t r0 = at / across * S, c0 = at % across * S;
     float sum[VEC] = {};
 #pragma unroll
@@ -403,7 +412,7 @@ template <typename T, int MM>
 __global__ __launch_bounds__(256) void few_dx_kernel(DenseBackArgs a, const float* dz, float* partial, int64_t run) {
   constexpr int VEC = vec_of<T>(), U = 4;
   __shared__ float sums[3][MM][VEC][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t k = ((int64_t)blockIdx.x * 64 + lane) * VEC, from = blockIdx.y * run, to = min(a.N, from + run);
   float acc[MM][VEC] = {};
   for (int64_t n0 = from + w; n0 < to; n0 += 4 * U) {
@@ -456,7 +465,7 @@ __global__ __launch_bounds__(256) void few_join_kernel(DenseBackArgs a, const fl
 template <typename T, int MM>
 __global__ __launch_bounds__(256) void few_dw_kernel(DenseBackArgs a, const float* dz, int64_t run) {
   constexpr int VEC = vec_of<T>();
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t k = ((int64_t)blockIdx.x * 64 + lane) * VEC, from = blockIdx.y * run, to = min(a.N, from + run);
   float x[MM][VEC];
 #pragma unroll
@@ -529,14 +538,6 @@ struct Layout {
 };
 
 template <typename T>
-int turn(hipStream_t s, const TurnArgs& a) {
-  const int64_t tiles = ceil_div(a.rows, 64) * ceil_div(a.cols, 64);
-  hipLaunchKernelGGL(turn_kernel<T>, dim3((unsigned)std::min<int64_t>(tiles, 1 << 20)), dim3(256), 0, s, a);
-  KMP_LAUNCH_CHECK();
-  return 0;
-}
-
-template <typename T>
 int backward_as(hipStream_t s, const DenseBackArgs& a) {
   constexpr int SIZE = (int)sizeof(T);
   if (a.M > 0 && a.N > 0 && a.M <= kFew) {
@@ -550,9 +551,19 @@ int backward_as(hipStream_t s, const DenseBackArgs& a) {
   float* partial = reinterpret_cast<float*>(ws + at.partial);
   const bool some = a.M > 0 && a.N > 0;
   if (some) {
-    TurnArgs t{a.dout, a.lddo, a.act == KMP_ACT_NONE ? nullptr : a.z, a.ldz, a.act, a.M, a.N, a.dx ? ws + at.dz : nullptr, at.pn,
-               a.dw ? ws + at.dz_turned : nullptr, at.pm, a.dbias ? partial : nullptr};
-    if (int e = turn<T>(s, t)) return e;
+    TurnsArgs all{};
+    int n = 0;
+    const auto add = [&](const TurnArgs& t) {
+      all.each[n] = t;
+      all.tiles[n++] = ceil_div(t.rows, 64) * ceil_div(t.cols, 64);
+    };
+    add(TurnArgs{a.dout, a.lddo, a.act == KMP_ACT_NONE ? nullptr : a.z, a.ldz, a.act, a.M, a.N, a.dx ? ws + at.dz : nullptr, at.pn,
+                 a.dw ? ws + at.dz_turned : nullptr, at.pm, a.dbias ? partial : nullptr});
+    if (a.dx && a.K > 0) add(TurnArgs{a.w, a.ldw, nullptr, 0, 0, a.N, a.K, nullptr, 0, ws + at.w_turned, at.pn, nullptr});
+    if (a.dw && a.K > 0) add(TurnArgs{a.x, a.ldx, nullptr, 0, 0, a.M, a.K, nullptr, 0, ws + at.x_turned, at.pm, nullptr});
+    const int64_t jobs = all.tiles[0] + all.tiles[1] + all.tiles[2];
+    hipLaunchKernelGGL(turn_kernel<T>, dim3((unsigned)std::min<int64_t>(jobs, 1 << 20)), dim3(256), 0, s, all);
+    KMP_LAUNCH_CHECK();
   }
   if (a.dbias && a.N > 0) {
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.N, 64), 1 << 20));
@@ -570,16 +581,10 @@ int backward_as(hipStream_t s, const DenseBackArgs& a) {
     const OutArgs o{M, N, KMP_ACT_NONE, false, nullptr, nullptr, 0, out, ldo, nullptr, 0};
     return product_as<T, T>(s, t, o);
   };
-  if (a.dx && a.M > 0) {
-    if (some)
-      if (int e = turn<T>(s, TurnArgs{a.w, a.ldw, nullptr, 0, 0, a.N, a.K, nullptr, 0, ws + at.w_turned, at.pn, nullptr})) return e;
+  if (a.dx && a.M > 0)
     if (int e = product(at.dz, at.pn, at.w_turned, at.pn, a.M, a.K, a.N, a.dx, a.lddx)) return e;
-  }
-  if (a.dw && a.N > 0) {
-    if (some)
-      if (int e = turn<T>(s, TurnArgs{a.x, a.ldx, nullptr, 0, 0, a.M, a.K, nullptr, 0, ws + at.x_turned, at.pm, nullptr})) return e;
+  if (a.dw && a.N > 0)
     if (int e = product(at.dz_turned, at.pm, at.x_turned, at.pm, a.N, a.K, a.M, a.dw, a.lddw)) return e;
-  }
   return 0;
 }
 
