@@ -44,6 +44,8 @@ struct PickShared : Common {           // with the histograms of its segments
   double weight[GRID];                 // running sums of the bins, relative to the row's maximum
   double tokens[GRID];
   double before[kMostSegs];
+  double base[kMostSegs];              // a segment's first bin's border; -INFINITY: it has no bins
+  int offset[kMostSegs];               // its place on the row's grid; GRID: none of it is there
 };
 
 // f(j, x_j) for the row's elements [from, to): wavefront w takes the w-th of WAVES
@@ -178,7 +180,7 @@ struct Row {
   // The first of the elements [from, to) at which `before` and the running sum of the
   // weights from the key `cut` up exceed `goal`, or the last that has a weight.
   __device__ int64_t pass(key_t cut, int64_t from, int64_t to, double before, double goal, double& weight_of) {
-    while (to - from > 32 * NT) {                 // the wavefront's run in which the sum passes
+    while (to - from > 4 * NT) {                  // the wavefront's run in which the sum passes
       double s = 0.0;
       visit<1>(x, from, to, [&](int64_t j, float v) { s += kept(cut, j, v); });
       s = wave_sum(s);
@@ -196,7 +198,7 @@ struct Row {
       from += max(at, 0) * run;
       to = min(to, from + run);
     }
-    // 32 neighbouring elements a thread at most
+    // four neighbouring elements a thread at most
     const int per = (int)ceil_div(to - from, NT);
     const int64_t j0 = from + threadIdx.x * per;
     const int n = (int)max((int64_t)0, min((int64_t)per, to - j0));
@@ -575,35 +577,28 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
 }
 
 // ---- The draw, one workgroup per row
-// The first n keys of sh.listed in descending order (n <= LISTED; the rest up to the next
-// power of two is cleared). Bitonic merges: up to 64 keys by one wavefront's shuffles.
+// The first n keys of sh.listed (all different; n <= LISTED) in descending order: a key's
+// place is the number of larger ones where they are few, else by bitonic merges (the rest
+// up to the next power of two is cleared). 50 keys: 0.8 us, by shuffles of one wavefront
+// 3.2.
 __device__ __forceinline__ void sort_list(PickShared& sh, int n) {
-  int size = 64;
-  while (size < n) size *= 2;
-  for (int i = n + threadIdx.x; i < size; i += NT) sh.listed[i] = 0;
-  __syncthreads();
   const int t = threadIdx.x;
-  if (size <= NT) {
-    key_t mine = t < size ? sh.listed[t] : 0;
-    for (int k = 2; k <= size; k <<= 1)
-      for (int s = k >> 1; s > 0; s >>= 1) {
-        key_t other;
-        if (s >= 64) {
-          __syncthreads();
-          if (t < size) sh.listed[t] = mine;
-          __syncthreads();
-          other = sh.listed[t & (size - 1) ^ s];
-        } else {
-          if (t >= size) continue;
-          other = __shfl_xor(mine, s, kWave);
-        }
-        mine = ((t & k) == 0) == ((t & s) == 0) ? max(mine, other) : min(mine, other);
-      }
+  if (n <= NT) {
+    const key_t mine = t < n ? sh.listed[t] : 0;
+    int rank = 0;
+    if ((t & ~63) < n) {
+#pragma unroll 8
+      for (int j = 0; j < n; ++j) rank += sh.listed[j] > mine;
+    }
     __syncthreads();
-    if (t < size) sh.listed[t] = mine;
+    if (t < n) sh.listed[rank] = mine;
     __syncthreads();
     return;
   }
+  int size = 2 * NT;
+  while (size < n) size *= 2;
+  for (int i = n + t; i < size; i += NT) sh.listed[i] = 0;
+  __syncthreads();
   for (int k = 2; k <= size; k <<= 1)
     for (int s = k >> 1; s > 0; s >>= 1) {
       for (int i = t; i < size / 2; i += NT) {
@@ -650,6 +645,8 @@ __device__ __forceinline__ int first_of(PickShared& sh, int n, F is) {
   return sh.n;
 }
 
+static_assert(GRID == NT, "a bin a thread");
+
 // A row's token by its segments' histograms, or -1 where its cuts are not in them (below
 // 32 e-foldings, or with more than LISTED tokens in their bins). The bins that hold the
 // cuts are known from running sums over the bins; only their tokens are looked for in
@@ -661,35 +658,30 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
   const int g = threadIdx.x;
   // a bin's weights relative to the row's maximum, from those relative to its border
   const auto border_weight = [&](double bin) { return exp(-(first - bin + f0) * (1.0 / kFine)); };
-  const auto offset = [&](int s) {                // of segment s's first bin; GRID: none of it is on the row's grid
-    const float m = key_value((uint32_t)(seg[s].top >> 32));
-    const double d = m > -INFINITY ? first - floor((double)m * scale) : (double)GRID;
-    return d < (double)GRID ? (int)d : GRID;
-  };
-  // running counts and weights over the row's bins; what lies below them
-  double w = 0.0, n = 0.0, below = 0.0;
-  if (g < GRID) {
-    for (int s = 0; s < segs; ++s) {
-      const int off = offset(s);
-      if (g >= off) {
-        w += seg[s].weight[g - off];
-        n += (double)seg[s].count[g - off];
-      }
-      if (off > 0) {                              // thread g: the segment's bin g, if that is below
-        const float m = key_value((uint32_t)(seg[s].top >> 32));
-        if (m > -INFINITY && g + off >= GRID) below += seg[s].weight[g] * border_weight(floor((double)m * scale) - g);
-      }
-      if (g == 0) {
-        const float m = key_value((uint32_t)(seg[s].top >> 32));
-        if (m > -INFINITY) below += seg[s].tail * row.weight(m);
-      }
-    }
-    w *= border_weight(first - g);
+  if (g < segs) {
+    const float m = key_value((uint32_t)(seg[g].top >> 32));
+    const double base = m > -INFINITY ? floor((double)m * scale) : -INFINITY, d = first - base;
+    sh.base[g] = base;
+    sh.offset[g] = d < (double)GRID ? (int)d : GRID;
+    sh.before[g] = m > -INFINITY ? seg[g].tail * row.weight(m) : 0.0;
   }
+  __syncthreads();
+  // running counts and weights over the row's bins; what lies below them
+  double w = 0.0, n = 0.0, below = g < segs ? sh.before[g] : 0.0;
+#pragma unroll 4
+  for (int s = 0; s < segs; ++s) {
+    const int off = sh.offset[s];
+    // (thread g: the row's bin g, and the segment's bin g where that is below the grid)
+    const double here = g >= off ? seg[s].weight[g - off] : 0.0, under = g + off >= GRID ? seg[s].weight[g] : 0.0;
+    w += here;
+    n += g >= off ? (double)seg[s].count[g - off] : 0.0;
+    if (under > 0.0) below += under * border_weight(sh.base[s] - g);
+  }
+  w *= border_weight(first - g);
   below = block_sum<NW>(below, sh.red);
   double total, tokens;
   const double runw = block_running(sh, w, total), runn = block_running(sh, n, tokens);
-  if (g < GRID) sh.weight[g] = runw, sh.tokens[g] = runn;
+  sh.weight[g] = runw, sh.tokens[g] = runn;
   __syncthreads();
   const auto weight_to = [&](int b) { return b >= 0 ? sh.weight[b] : 0.0; };   // of the bins up to b
   const auto count_to = [&](int b) { return b >= 0 ? (int64_t)sh.tokens[b] : 0; };
@@ -723,7 +715,8 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
   if (by_k || by_p || by_m) {
     lo = min(lo, first_of(sh, GRID, [&](int b) { return sh.tokens[b] >= sh.tokens[hi]; }));   // (a bin that has tokens)
     const bool far = by_k && by_p && kb > hi;     // the k-th token's bin as well, for the weight of the first k
-    if (count_to(hi) + (far ? count_to(kb) - count_to(kb - 1) : 0) <= LISTED) lo = 0;
+    // (all that may be kept where that is few: a longer list is not put in order as fast)
+    if (count_to(hi) + (far ? count_to(kb) - count_to(kb - 1) : 0) <= NT) lo = 0;
     const int64_t near = count_to(hi) - count_to(lo - 1), more = far ? count_to(kb) - count_to(kb - 1) : 0;
     if (near + more > LISTED) return -1;
     // list them: logits below `low` are of later bins (a little lower than the border, for
@@ -738,12 +731,18 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
       const double d = first - floor((double)v * scale);
       return d < (double)GRID ? (int)d : GRID;
     };
-    visit<4>(row.x, 0, row.V, [&](int64_t j, float v) {
-      if (!(v >= low) || v == -INFINITY) return;
+    visit<8>(row.x, 0, row.V, [&](int64_t j, float v) {
+      bool is = v >= low && v > -INFINITY;
+      if (!__any(is)) return;
       const int b = bin_of(v);
-      if (!((b >= lo && b <= hi) || (far && b == kb))) return;
-      const int at = atomicAdd(&sh.n, 1);
-      if (at < LISTED) sh.listed[at] = key_of(v, (uint32_t)j);
+      is = is && ((b >= lo && b <= hi) || (far && b == kb));
+      const unsigned long long which = __ballot(is);
+      if (which == 0) return;
+      int at = 0;                                 // (one atomic a wavefront)
+      const int leader = __ffsll(which) - 1;
+      if ((int)(threadIdx.x & 63) == leader) at = atomicAdd(&sh.n, __popcll(which));
+      at = __shfl(at, leader, kWave) + __popcll(which & (((unsigned long long)1 << (threadIdx.x & 63)) - 1));
+      if (is && at < LISTED) sh.listed[at] = key_of(v, (uint32_t)j);
     });
     __syncthreads();
     const int size = min(sh.n, LISTED);
@@ -795,14 +794,16 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
   // and its listed tokens
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   for (int s = wave; s < segs; s += NW) {
-    const int off = offset(s), bins = cut != 0 ? lo : GRID;
-    const float m = key_value((uint32_t)(seg[s].top >> 32));
+    const int off = sh.offset[s], bins = cut != 0 ? lo : GRID;
+    const double base = sh.base[s], tail = sh.before[s];
     double sum = 0.0;
-    if (m > -INFINITY) {
-      const double base = floor((double)m * scale);
-      for (int i = lane; i < GRID; i += 64)
-        if (cut == 0 || i + off < bins) sum += seg[s].weight[i] * border_weight(base - i);
-      if (lane == 0 && cut == 0) sum += seg[s].tail * row.weight(m);
+    if (base > -INFINITY) {
+#pragma unroll 4
+      for (int i = lane; i < GRID; i += 64) {
+        const double own = cut == 0 || i + off < bins ? seg[s].weight[i] : 0.0;
+        if (own > 0.0) sum += own * border_weight(base - i);
+      }
+      if (lane == 0 && cut == 0) sum += tail;
     }
     sum = wave_sum(sum);
     if (lane == 0) sh.before[s] = sum;
@@ -850,15 +851,39 @@ __device__ __forceinline__ void put_token(const SampleArgs& a, int64_t t, int64_
   if (a.logp) a.logp[t] = (float)logp;
 }
 
+// The rows whose cuts the histograms do not see: by passes over the row alone.
 template <typename T>
+__device__ __forceinline__ int64_t draw_aside(Shared& sh, const SampleArgs& a, const Choice& choice, const T* x, key_t top, double& logp) {
+  Passes<T> row(sh, choice.row(sh, x, a.V, key_value((uint32_t)(top >> 32))));
+  key_t cut = 0;
+  if (choice.k < a.V) cut = row.kth(choice.k, top | UINT32_MAX);
+  if (choice.p < 1.0f) cut = row.reach_p((double)choice.p, cut);
+  double share;
+  const int64_t token = row.draw(cut, max((double)choice.u, 0.0), share);
+  logp = log(share);
+  return token;
+}
+
+// ASIDE: those rows in the same launch, for no more rows than the chip has compute units
+// (the registers and LDS of both allow one workgroup each there, of the draw alone two;
+// a launch costs 4 us).
+template <typename T, bool ASIDE>
 __global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs) {
-  __shared__ PickShared sh;
+  union All {
+    PickShared pick;
+    Shared aside;
+    __device__ All() {}
+  };
+  __shared__ __align__(16) char memory[ASIDE ? sizeof(All) : sizeof(PickShared)];
+  PickShared& sh = *reinterpret_cast<PickShared*>(memory);
   const int64_t length = segment_length(a.V);
   for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
     const T* x = static_cast<const T*>(a.logits) + t * a.ld;
     const Segment* seg = static_cast<const Segment*>(a.workspace) + t * segs;
     key_t top = 0;
-    for (int s = 0; s < segs; ++s) top = max(top, seg[s].top);
+    for (int s = threadIdx.x & 63; s < segs; s += 64) top = max(top, seg[s].top);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) top = max(top, (key_t)__shfl_xor(top, off, kWave));
     const float m = key_value((uint32_t)(top >> 32));
     const Choice choice(a, t);
     const bool nan = choice.nan || m != m || m == INFINITY;
@@ -873,32 +898,32 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs)
       Row<T> row = choice.row(sh, x, a.V, m);
       double share;
       token = pick(sh, row, seg, segs, length, choice.k, (double)choice.p, max((double)choice.u, 0.0), share);
-      if (token < 0) token = kAside;
       logp = log(share);
+      if (token < 0) {
+        if constexpr (ASIDE) {
+          __syncthreads();
+          token = draw_aside(*reinterpret_cast<Shared*>(memory), a, choice, x, top, logp);
+        } else {
+          token = kAside;
+        }
+      }
     }
     put_token(a, t, token, logp);
     __syncthreads();
   }
 }
-
-// The rows whose cuts the histograms do not see: by passes over the row alone.
 template <typename T>
-__global__ __launch_bounds__(NT) void sample_aside_kernel(SampleArgs a) {
+__global__ __launch_bounds__(NT) void sample_aside_kernel(SampleArgs a, int segs) {
   __shared__ Shared sh;
   for (int64_t t = blockIdx.x; t < a.T; t += gridDim.x) {
     const int64_t mark = a.wide ? static_cast<const int64_t*>(a.tokens)[t] : static_cast<const int32_t*>(a.tokens)[t];
     if (mark != kAside) continue;
-    const T* x = static_cast<const T*>(a.logits) + t * a.ld;
-    const Segment* seg = static_cast<const Segment*>(a.workspace) + t * segments(a.V);
-    key_t top = 0, cut = 0;
-    for (int s = 0; s < (int)segments(a.V); ++s) top = max(top, seg[s].top);
-    const Choice choice(a, t);
-    Passes<T> row(sh, choice.row(sh, x, a.V, key_value((uint32_t)(top >> 32))));
-    if (choice.k < a.V) cut = row.kth(choice.k, top | UINT32_MAX);
-    if (choice.p < 1.0f) cut = row.reach_p((double)choice.p, cut);
-    double share;
-    const int64_t token = row.draw(cut, max((double)choice.u, 0.0), share);
-    put_token(a, t, token, log(share));
+    const Segment* seg = static_cast<const Segment*>(a.workspace) + t * segs;
+    key_t top = 0;
+    for (int s = 0; s < segs; ++s) top = max(top, seg[s].top);
+    double logp;
+    const int64_t token = draw_aside(sh, a, Choice(a, t), static_cast<const T*>(a.logits) + t * a.ld, top, logp);
+    put_token(a, t, token, logp);
     __syncthreads();
   }
 }
@@ -907,8 +932,13 @@ template <typename T>
 int sample_as(hipStream_t s, const SampleArgs& a) {
   const int segs = (int)segments(a.V);
   hipLaunchKernelGGL(sample_count_kernel<T>, dim3(segs, (unsigned)std::min<int64_t>(a.T, 65535)), dim3(CT), 0, s, a);
-  hipLaunchKernelGGL(sample_pick_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T, 65535)), dim3(NT), 0, s, a, segs);
-  hipLaunchKernelGGL(sample_aside_kernel<T>, dim3((unsigned)std::min<int64_t>(a.T, 256)), dim3(NT), 0, s, a);
+  const dim3 rows((unsigned)std::min<int64_t>(a.T, 65535));
+  if (a.T <= 256) {
+    hipLaunchKernelGGL((sample_pick_kernel<T, true>), rows, dim3(NT), 0, s, a, segs);
+  } else {
+    hipLaunchKernelGGL((sample_pick_kernel<T, false>), rows, dim3(NT), 0, s, a, segs);
+    hipLaunchKernelGGL(sample_aside_kernel<T>, dim3(256), dim3(NT), 0, s, a, segs);
+  }
   KMP_LAUNCH_CHECK();
   return 0;
 }
