@@ -103,3 +103,13 @@ def test_oracle_gradients_against_differences(after, rms, gate):
                         for s in (1, -1))
             want = (loss(up) - loss(down)) / 2e-5
             assert abs(got[i] - want) <= 1e-6 * (1 + abs(want)), (k, i, got[i], want)
+
+
+def test_largest_arguments(km):  # noqa: F811
+    """Sizes up to the largest accepted ones have a workspace; pointers and pitches there
+    are refused or taken without overflow."""
+    most = (1 << 31) - 1
+    size = km.lib().kmp_block_norm_workspace_bytes
+    for t in (1, 2, 3):
+        for r, d in ((most, most), (most, 1), (0, most), (1, most)):
+            assert size(t, r, d) >= 4 * 4 * d and size(t, r, d) < 1 << 62

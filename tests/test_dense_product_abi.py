@@ -81,3 +81,12 @@ def test_oracle_gradients_against_differences(act):
             args = [[x, w, b], [x, w, b]]
             args[0][k], args[1][k] = p + step, p - step
             assert abs((loss(*args[0]) - loss(*args[1])) / 2e-6 - g[i]) <= 1e-6 * (1 + abs(g[i]))
+
+
+def test_largest_arguments(km):  # noqa: F811
+    """Workspaces of the largest accepted sizes do not overflow."""
+    most = 1 << 28
+    size = km.lib().kmp_dense_product_workspace_bytes
+    for t in (1, 2, 3):
+        for m, n, k in ((most, most, most), (most, 1, 1), (1, most, 1), (1, 1, most), (16, most, most), (0, most, most)):
+            assert 256 <= size(t, m, n, k) < 1 << 62

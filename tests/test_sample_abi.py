@@ -52,3 +52,10 @@ def test_oracle_by_hand():
     assert [draw(u, temperature=0.5) for u in (0.02, 0.04, 0.5, 0.6, 0.8)] == [0, 1, 1, 2, 3]   # 1, 16, 4, 9 of 30
     _, logp, _ = OO.sample_tokens(x, [0.5], top_k=[2])
     assert abs(logp[0] - np.log(4 / 7)) < 1e-12
+
+
+def test_largest_arguments(km):  # noqa: F811
+    """Workspaces of the largest accepted sizes do not overflow."""
+    most = (1 << 31) - 1
+    for T, V in ((most, most), (most, 1), (1, most), (0, most)):
+        assert 256 <= km.kmp_sample_tokens_workspace_bytes(T, V) < 1 << 62
