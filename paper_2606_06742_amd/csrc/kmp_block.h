@@ -1,5 +1,5 @@
-// The norms around a model's block (block.hip, block_back.hip), fused with the block's gate and the residual
-// stream, forward and backward. With N(x) = (x - mu) r g + c (mu = 0 and r from the
+// The norms around a model's block (block.hip, block_back.hip), fused with the block's
+// gate and the residual stream, forward and backward. With N(x) = (x - mu) r g + c (mu = 0 and r from the
 // mean square for the norm by the root mean square):
 //   n = N(b) or b,  h = rscale res + gate n,  y = N(h)
 //   s = dh + r2 (w - mean(w) - xh2 mean(w xh2)),  w = dy g2,  xh2 = (h - mu2) r2

@@ -292,12 +292,12 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void tile_kernel(TileArgs a, typ
 // the operands of every 32 bytes of k are read from LDS while the 32 before them are
 // multiplied: reads and loads are issued between the products, whose issue takes an
 // eighth of the time that the matrix cores need for one (all of them ahead of a group of
-// products left the cores idle: 4096 x 8192 x 4096 in 16 bits @BEFORE / @AFTER us). The
-// barrier of slice s stands within its last products: their operands are in registers,
-// so that the stage is free for slice s + NS, and slice s + 1 has landed, so that its
-// first operands can be read behind them. A slice past the end is the last one again,
-// unused, which keeps the number of loads under way the same. (Slices of 64 bytes
-// through four or five stages: 4 % slower.)
+// products left the cores idle: 4096 x 8192 x 4096 in 16 bits 276 / 263 us, 8192 x 8192 x
+// 8192 923 / 876, in 8 bits 536 / 462). The barrier of slice s stands within its last
+// products: their operands are in registers, so that the stage is free for slice s + NS,
+// and slice s + 1 has landed, so that its first operands can be read behind them. A slice
+// past the end is the last one again, unused, which keeps the number of loads under way
+// the same. (Slices of 64 bytes through four or five stages: 4 % slower.)
 template <typename E, typename Epi, int TM, int TN, int WR, int WC, int NS>
 __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typename Epi::Args out, int tm, int tn) {
   constexpr int NW = WR * WC, MB = TM / WR / 32, NB = TN / WC / 32, QA = TM / 8 / NW, QB = TN / 8 / NW;

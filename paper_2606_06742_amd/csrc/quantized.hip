@@ -148,57 +148,58 @@ struct ScaledTile {
 // N x K, w from HBM: few tokens; tiles of 32 x 64 (four groups over k, ring of 3), 64
 // x 64 (two groups, ring of 3, or of 2 and so two workgroups a compute unit); operands
 // ahead in tiles of 128 and 256; the floor, the larger of the bytes at a copy's 4.82
-// TB/s and the products at the 2040 TOP/s of the library's 8-bit product of order 8192:
+// TB/s and the products at 2040 TOP/s (what the 8-bit product of order 8192 reached before
+// its reads were dealt out between the products; 2380 since):
 //                      few  32x64  64,3  64,2   128   256  floor
-//   1 x 4096 x 4096    6.0   7.5   9.7  12.0  20.9  48.7   3.5
-//   16 x 8192 x 4096  11.6  10.4  11.4  16.6  30.0  51.2   7.0
-//   16 x 32000 x 2048 21.2  18.2  18.5  15.6  20.3  30.4  13.8
-//   64 x 1000 x 8192        11.8  15.8  21.6  39.6  91.8   1.8
-//   64 x 4096 x 4096         8.1  10.1  12.9  22.2  49.2   3.6
-//   128 x 4096 x 4096        8.7  10.7  12.8  23.4  50.2   3.8
-//   256 x 4096 x 4096       14.6  11.7  13.2  23.5  52.2   4.2
-//   64 x 12288 x 4096       20.8  16.5  19.8  32.3  52.6  10.8
-//   64 x 32000 x 2048       27.5  21.3  18.0  21.2  31.4  14.5
-//   512 x 4096 x 4096       27.0  19.6  16.6  24.0  52.0   8.4
-//   2048 x 2048 x 2048      35.9  24.6  18.4  16.6  31.7   8.4
-//   1024 x 8192 x 4096       132    89    74  45.6  60.5  33.7
-//   3000 x 5000 x 1000       159    83    63  36.4  32.6  14.7
-//   4096 x 4096 x 4096       224   169   135  87.0  71.0  67.4
-//   4096 x 16384 x 4096      850   632   534   364   293   269
+//   1 x 4096 x 4096    6.0   7.5   9.7  12.0  21.0  40.2   3.5
+//   16 x 8192 x 4096  11.6  10.4  11.4  16.6  21.8  40.6   7.0
+//   16 x 32000 x 2048 21.2  18.2  18.5  15.6  19.4  28.9  13.8
+//   64 x 1000 x 8192        11.8  15.8  21.6  39.6  76.2   1.8
+//   64 x 4096 x 4096         8.1  10.1  12.9  22.2  40.7   3.6
+//   128 x 4096 x 4096        8.7  10.7  12.8  23.3  42.1   3.8
+//   256 x 4096 x 4096       14.6  11.7  13.2  23.5  43.4   4.2
+//   64 x 12288 x 4096       20.8  16.5  19.8  32.7  47.5  10.8
+//   64 x 32000 x 2048       27.5  21.3  18.0  20.8  29.4  14.5
+//   512 x 4096 x 4096       27.0  19.6  16.6  24.1  43.7   8.4
+//   2048 x 2048 x 2048      35.9  24.6  18.4  16.3  27.6   8.4
+//   1024 x 8192 x 4096       132    89    74  42.6  50.6  33.7
+//   3000 x 5000 x 1000       159    83    63  36.9  31.4  14.7
+//   4096 x 4096 x 4096       224   169   135  85.7  64.1  67.4
+//   4096 x 16384 x 4096      850   632   534   328   256   269
 // Between 512 and 768 tiles of 64 those of 128 leave compute units idle: one group a
 // tile of 64 and a ring of 2, up to five workgroups a compute unit (64,1; here and
 // below in a recorded graph, 1 to 2 us more a launch):
 //                       64,2  64,1   128  floor
-//   600 x 4500 x 700    13.0   9.9  11.0   1.9
-//   1500 x 1500 x 1500  17.3  12.7  14.5   3.3
-//   1244 x 1824 x 10909 74.2  61.7  84.4  24.3
-//   1000 x 3000 x 4096  34.1  28.7  32.5  12.0
-//   768 x 4096 x 8192   51.1  50.6  59.5  25.3
-//   1024 x 3584 x 4096  35.2  34.2  32.6  14.7
-//   2048 x 2048 x 2048  18.3  18.8  16.0   8.4
+//   600 x 4500 x 700    13.0   9.9  11.9   1.9
+//   1500 x 1500 x 1500  17.3  12.7  15.7   3.3
+//   1244 x 1824 x 10909 74.2  61.7  68.9  24.3
+//   1000 x 3000 x 4096  34.1  28.7  26.1  12.0
+//   768 x 4096 x 8192   51.1  50.6  44.4  25.3
+//   1024 x 3584 x 4096  35.2  34.2  26.2  14.7
+//   2048 x 2048 x 2048  18.3  18.8  16.8   8.4
 // Up to 256 tiles of 128 have a compute unit each and room for a ring of 4 there,
 // which hides more of the loads than a ring of 2 (128,4; in a recorded graph, both
 // sides in turn):
 //                       64,1   128  128,4
-//   600 x 4500 x 700    10.7         11.4
-//   1500 x 1500 x 1500  13.9         14.4
-//   1244 x 1824 x 10909 63.6         48.4
-//   4138 x 534 x 7988   44.9         39.0
-//   1000 x 3000 x 4096  24.9         23.7
-//   768 x 4096 x 8192   44.1         39.3
-//   1024 x 3584 x 4096        26.7   23.9
-//   2000 x 2000 x 8192        47.6   43.5
-//   2048 x 2048 x 2048        17.1   16.1
+//   600 x 4500 x 700    10.7         11.8
+//   1500 x 1500 x 1500  13.9         14.3
+//   1244 x 1824 x 10909 63.6         52.7
+//   4138 x 534 x 7988   44.9         43.6
+//   1000 x 3000 x 4096  24.9         22.8
+//   768 x 4096 x 8192   44.1         36.3
+//   1024 x 3584 x 4096        26.2   24.0
+//   2000 x 2000 x 8192        47.4   43.4
+//   2048 x 2048 x 2048        16.8   16.7
 // Few tokens with more channels than the first table's have 192 tiles of 256 and take
 // them (in a recorded graph, w from HBM), though smaller ones are ahead (reading alone
 // is a little faster than the copy that the floor's rate is of):
 //                        few  32x64  64,3  64,2  64,1   128   256  floor
 //   1 x 50257 x 2048    19.4  28.0  28.3  24.6  21.4  22.8  31.6  21.4
-//   64 x 50257 x 2048         43.2  34.6  30.2  30.3  29.0  34.6  22.8
+//   64 x 50257 x 2048         43.2  34.6  30.2  30.3  28.5  33.9  22.8
 //   16 x 128256 x 4096   141   105   108   107   108   109   133   110
-//   64 x 128256 x 4096         164   128   122   123   121   138   113
+//   64 x 128256 x 4096         164   128   122   123   127   138   113
 //   1 x 151936 x 4096    103   126   134   139   152   155   180   129
-//   64 x 151936 x 4096         191   159   152   152   162   187   133
+//   64 x 151936 x 4096         191   159   152   152   172   188   133
 // Rows that are not aligned: few tokens; tiles of 32 x 64 (four groups), 64 and 128
 // (one; 128 with eight wavefronts, with four 97 for 87 at 1244 x 1824 x 10909):
 //                        few  32x64    64   128  floor

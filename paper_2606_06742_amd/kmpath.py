@@ -447,8 +447,11 @@ def _gate(t, name, rows, d, xdtype, wdtype, on):
 
 
 def _block_weights(x, *weights):
-    """The weights' type: the first given one's, else x's."""
-    return next((t.dtype for t in weights if t is not None and t.dim() == 1), x.dtype)
+    """The weights' type: the first given vector's, else x's."""
+    for t in weights:
+        if t is not None and t.dim() == 1:
+            return t.dtype
+    return x.dtype
 
 
 def kmp_block_norm(b, res, h, y, eps, gamma_after=None, beta_after=None, gate=None, gamma=None, beta=None,
@@ -473,14 +476,18 @@ def kmp_block_norm(b, res, h, y, eps, gamma_after=None, beta_after=None, gate=No
         yt = _type(y.dtype, "y")
     wd = _block_weights(b, gamma_after, beta_after, gamma, beta, gate)
     gp, ldg = _gate(gate, "gate", rows, d, b.dtype, wd, on)
-    import torch
-    f = torch.float32
+    bt = _type(b.dtype, "b")
+    st = sc = None
+    if stats is not None or scale is not None:
+        import torch
+        st, sc = _vector(stats, "stats", 4 * rows, torch.float32, on), _vector(scale, "scale", rows, torch.float32, on)
     _check(lib().kmp_block_norm(
-        sp, _type(b.dtype, "b"), (KMP_NORM_RMS if rms else 0) | (KMP_NORM_AFTER if after else 0), bp, ldb, rp, ldr,
-        rows, d, _type(wd, "gamma"), _vector(gamma_after, "gamma_after", d, wd, on),
-        _vector(beta_after, "beta_after", d, wd, on), gp, ldg, float(rscale), _vector(gamma, "gamma", d, wd, on),
-        _vector(beta, "beta", d, wd, on), float(eps), hp, ldh, yt, yp, ldy,
-        _vector(stats, "stats", 4 * rows, f, on), _vector(scale, "scale", rows, f, on)), allow_maxiter=False)
+        sp, bt, (KMP_NORM_RMS if rms else 0) | (KMP_NORM_AFTER if after else 0), bp, ldb, rp, ldr, rows, d,
+        bt if wd is b.dtype else _type(wd, "gamma"),
+        None if gamma_after is None else _vector(gamma_after, "gamma_after", d, wd, on),
+        None if beta_after is None else _vector(beta_after, "beta_after", d, wd, on), gp, ldg, rscale,
+        None if gamma is None else _vector(gamma, "gamma", d, wd, on),
+        None if beta is None else _vector(beta, "beta", d, wd, on), eps, hp, ldh, yt, yp, ldy, st, sc), allow_maxiter=False)
 
 
 def kmp_block_norm_workspace_bytes(rows: int, d: int, dtype) -> int:
