@@ -288,6 +288,21 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void tile_kernel(TileArgs a, typ
   Epi::template store<MB, NB>(out, acc, m0 + wr * MB * 32, n0 + wc * NB * 32, lane, lds + SUMS + wg * REGION);
 }
 
+// Columns 32 b to 32 b + 31 of rows 16 h to 16 h + 15 of a turned slice of T columns, as
+// an operand of Blocks::multiply (below).
+typedef short short4v __attribute__((ext_vector_type(4)));
+template <int T>
+__device__ __forceinline__ int4v read_turned(const int8_t* slice, int b, int h, int lane) {
+  const int l = lane & 15, group = lane >> 4;     // (16 lanes: 16 columns; groups 2 and 3: rows 8 on)
+  const int at = (16 * h + 8 * (group >> 1) + (l >> 2)) * (T * 2) + ((b ^ (l >> 2)) * 4 + 2 * (group & 1) + (l >> 1 & 1)) * 16 + (l & 1) * 8;
+  typedef __attribute__((address_space(3))) short4v* lds_t;
+  union { short4v v[2]; int4v all; } u;
+  u.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(uint32_t)(uintptr_t)(slice + at));
+  u.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(uint32_t)(uintptr_t)(slice + at + 4 * (T * 2)));
+  return u.all;
+}
+__device__ __forceinline__ int64_t round_up_to(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+
 // The larger forms, aligned rows: slices as in tile_kernel in a ring of NS stages, and
 // the operands of every 32 bytes of k are read from LDS while the 32 before them are
 // multiplied: reads and loads are issued between the products, whose issue takes an
@@ -298,7 +313,14 @@ __global__ __launch_bounds__(64 * WR * WC * WK) void tile_kernel(TileArgs a, typ
 // and slice s + 1 has landed, so that its first operands can be read behind them. A slice
 // past the end is the last one again, unused, which keeps the number of loads under way
 // the same. (Slices of 64 bytes through four or five stages: 4 % slower.)
-template <typename E, typename Epi, int TM, int TN, int WR, int WC, int NS>
+//
+// XT, WT: that operand is given the other way round, K rows of M or of N elements (of two
+// bytes, rows at multiples of 16 bytes), whose slice is 64 of these rows. Blocks of 4 rows
+// by 16 columns come out of LDS turned by the hardware: of 16 lanes, lane l names the place
+// of row l / 4, columns 4 (l % 4) on, and gets column l of the four rows. A row's 16-byte
+// chunk c lies at place c ^ 4 (row % 4), so that the 32 bytes of each of four rows that 16
+// lanes read, and those beside them that the next 16 read, lie on different banks.
+template <typename E, typename Epi, int TM, int TN, int WR, int WC, int NS, bool XT = false, bool WT = false>
 __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typename Epi::Args out, int tm, int tn) {
   constexpr int NW = WR * WC, MB = TM / WR / 32, NB = TN / WC / 32, QA = TM / 8 / NW, QB = TN / 8 / NW;
   constexpr int SL = 128, STAGE = (TM + TN) * SL;
@@ -312,19 +334,29 @@ __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typenam
   const int wr = w / WC, wc = w % WC;
   const int lr = lane >> 3;                                           // loads: row of eight, byte of the slice
   const int lc[2] = {((lane & 7) ^ (lr >> 1)) * 16, ((lane & 7) ^ (4 + (lr >> 1))) * 16};
+  static_assert(!(XT || WT) || (sizeof(E) == 2 && TM % 128 == 0 && TN % 128 == 0), "turned operands");
   const int8_t* pa[QA];
   const int8_t* pb[QB];
+  // a turned operand's load q of width T from column c0 of C: its row of the slice, and the
+  // address there (columns past the end: the last ones again)
+  const auto turned_row = [&](int q, int Q, int T) { return (w * Q + q) * (512 / T) + lane / (T / 8); };
+  const auto turned = [&](const int8_t* p, int64_t ld, int64_t c0, int64_t C, int q, int Q, int T) {
+    const int r = turned_row(q, Q, T), c = ((lane & (T / 8 - 1)) ^ 4 * (r & 3)) * 8;
+    return p + r * ld + min(c0 + c, round_up_to(C, 8) - 8) * 2;
+  };
 #pragma unroll
-  for (int q = 0; q < QA; ++q) pa[q] = a.x + min(m0 + (w * QA + q) * 8 + lr, a.M - 1) * a.ldx + lc[q & 1];
+  for (int q = 0; q < QA; ++q)
+    pa[q] = XT ? turned(a.x, a.ldx, m0, a.M, q, QA, TM) : a.x + min(m0 + (w * QA + q) * 8 + lr, a.M - 1) * a.ldx + lc[q & 1];
 #pragma unroll
-  for (int q = 0; q < QB; ++q) pb[q] = a.w + min(n0 + (w * QB + q) * 8 + lr, a.N - 1) * a.ldw + lc[q & 1];
+  for (int q = 0; q < QB; ++q)
+    pb[q] = WT ? turned(a.w, a.ldw, n0, a.N, q, QB, TN) : a.w + min(n0 + (w * QB + q) * 8 + lr, a.N - 1) * a.ldw + lc[q & 1];
   const uint32_t base = (uint32_t)(uintptr_t)lds;                     // LDS addresses have 32 bits
   const int whole = (int)a.K / SL, tail = (int)a.K % SL;
   const auto fetch_one = [&](int s, int i) {                          // load i of LOADS of slice s
     const uint32_t at = base + s % NS * STAGE;
-    const int k = min(s, whole - 1) * SL;
-    if (i < QA) load_to_lds(pa[i < QA ? i : 0] + k, at + (w * QA + i) * 1024);
-    else load_to_lds(pb[i < QA ? 0 : i - QA] + k, at + TM * SL + (w * QB + i - QA) * 1024);
+    const int k = min(s, whole - 1);
+    if (i < QA) load_to_lds(pa[i < QA ? i : 0] + (XT ? k * 64 * a.ldx : k * SL), at + (w * QA + i) * 1024);
+    else load_to_lds(pb[i < QA ? 0 : i - QA] + (WT ? k * 64 * a.ldw : k * SL), at + TM * SL + (w * QB + i - QA) * 1024);
   };
   typename Blocks<E>::acc_t acc[MB][NB] = {};
   const int row = lane & 31, half = lane >> 5;
@@ -333,8 +365,9 @@ __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typenam
   int4v fa[2][MB], fb[2][NB];
   const auto read_one = [&](int s, int h, int i) {                    // operand i of READS: bytes 32 h .. of slice s
     const int c = ((2 * h + half) ^ (row >> 1 & 7)) * 16 + s % NS * STAGE;
-    if (i < NB) fb[h & 1][i < NB ? i : 0] = *reinterpret_cast<const int4v*>(lb + i * 32 * SL + c);
-    else fa[h & 1][i < NB ? 0 : i - NB] = *reinterpret_cast<const int4v*>(la + (i - NB) * 32 * SL + c);
+    const int8_t* st = lds + s % NS * STAGE;
+    if (i < NB) fb[h & 1][i < NB ? i : 0] = WT ? read_turned<TN>(st + TM * SL, wc * NB + i, h, lane) : *reinterpret_cast<const int4v*>(lb + i * 32 * SL + c);
+    else fa[h & 1][i < NB ? 0 : i - NB] = XT ? read_turned<TM>(st, wr * MB + i - NB, h, lane) : *reinterpret_cast<const int4v*>(la + (i - NB) * 32 * SL + c);
   };
   const auto multiply_one = [&](int h, int i) {
     acc[i / NB][i % NB] = Blocks<E>::multiply(fb[h & 1][i % NB], fa[h & 1][i / NB], acc[i / NB][i % NB]);
@@ -378,14 +411,19 @@ __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typenam
   }
   if (tail > 0) {                                                     // zeros past K
     __syncthreads();
+    const auto rest = [&](const int8_t* p, int64_t ld, int r) {       // of a turned operand: rows past K are zeros
+      int4v v = {0, 0, 0, 0};
+      if (2 * r < tail) __builtin_memcpy(&v, p + whole * 64 * ld, 16);
+      return v;
+    };
 #pragma unroll
     for (int q = 0; q < QA; ++q)
       *reinterpret_cast<int4v*>(lds + (w * QA + q) * 1024 + lane * 16) =
-          chunk16(pa[q] - lc[q & 1], whole * SL + lc[q & 1], a.K);
+          XT ? rest(pa[q], a.ldx, turned_row(q, QA, TM)) : chunk16(pa[q] - lc[q & 1], whole * SL + lc[q & 1], a.K);
 #pragma unroll
     for (int q = 0; q < QB; ++q)
       *reinterpret_cast<int4v*>(lds + TM * SL + (w * QB + q) * 1024 + lane * 16) =
-          chunk16(pb[q] - lc[q & 1], whole * SL + lc[q & 1], a.K);
+          WT ? rest(pb[q], a.ldw, turned_row(q, QB, TN)) : chunk16(pb[q] - lc[q & 1], whole * SL + lc[q & 1], a.K);
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
@@ -416,9 +454,9 @@ template <typename E, typename Epi, int TM, int TN, int WR, int WC, int WK, int 
 int tiles_as(hipStream_t s, const TileArgs& a, const typename Epi::Args& out) {
   return launch_tiles<TM, TN>(s, a, out, tile_kernel<E, Epi, TM, TN, WR, WC, WK, NS, ALIGNED>, 64 * WR * WC * WK);
 }
-template <typename E, typename Epi, int TM, int TN, int WR, int WC, int NS>
+template <typename E, typename Epi, int TM, int TN, int WR, int WC, int NS, bool XT = false, bool WT = false>
 int ahead_as(hipStream_t s, const TileArgs& a, const typename Epi::Args& out) {
-  return launch_tiles<TM, TN>(s, a, out, ahead_kernel<E, Epi, TM, TN, WR, WC, NS>, 64 * WR * WC);
+  return launch_tiles<TM, TN>(s, a, out, ahead_kernel<E, Epi, TM, TN, WR, WC, NS, XT, WT>, 64 * WR * WC);
 }
 
 }  // namespace kmp

@@ -380,18 +380,23 @@ __global__ __launch_bounds__(1024) void bias_join_kernel(const float* partial, i
   }
 }
 
-// Few tokens (M <= MM <= 16) take no part of the above: reading w once for dx and
+// Few tokens (M <= MM <= kFew) take no part of the above: reading w once for dx and
 // writing dw once is all that counts, and dz stays in 32 bits.
-// dz [M][N] and its column sums, a thread per column.
-template <typename T, typename W>
+// dz [N][MM], zeros from M on, so that a channel's are one load for a whole wavefront;
+// and its sums over the tokens. A thread per channel.
+template <typename T, typename W, int MM>
 __global__ __launch_bounds__(256) void few_dz_kernel(DenseBackArgs a, float* dz) {
   for (int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x; n < a.N; n += (int64_t)gridDim.x * 256) {
     float sum = 0.0f;
-    for (int64_t m = 0; m < a.M; ++m) {
-      float v = (float)static_cast<const T*>(a.dout)[m * a.lddo + n];
-      if (a.act != KMP_ACT_NONE) v *= slope(a.act, (float)static_cast<const T*>(a.z)[m * a.ldz + n]);
-      dz[m * a.N + n] = v;
-      sum += v;
+#pragma unroll
+    for (int m = 0; m < MM; ++m) {
+      float v = 0.0f;
+      if (m < a.M) {
+        v = (float)static_cast<const T*>(a.dout)[m * a.lddo + n];
+        if (a.act != KMP_ACT_NONE) v *= slope(a.act, (float)static_cast<const T*>(a.z)[m * a.ldz + n]);
+        sum += v;
+      }
+      dz[n * MM + m] = v;
     }
     if (a.dbias) static_cast<W*>(a.dbias)[n] = (W)sum;
   }
@@ -422,7 +427,7 @@ __global__ __launch_bounds__(256) void few_dx_kernel(DenseBackArgs a, const floa
       const int64_t n = min(n0 + 4 * i, to - 1);
       load_part(static_cast<const T*>(a.w) + n * a.ldw, k, a.K, v[i]);
 #pragma unroll
-      for (int m = 0; m < MM; ++m) f[i][m] = m < a.M && n0 + 4 * i < to ? dz[m * a.N + n] : 0.0f;
+      for (int m = 0; m < MM; ++m) f[i][m] = dz[n * MM + m];
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -469,15 +474,20 @@ __global__ __launch_bounds__(256) void few_dw_kernel(DenseBackArgs a, const floa
   const int64_t k = ((int64_t)blockIdx.x * 64 + lane) * VEC, from = blockIdx.y * run, to = min(a.N, from + run);
   float x[MM][VEC];
 #pragma unroll
-  for (int m = 0; m < MM; ++m) load_part(static_cast<const T*>(a.x) + min((int64_t)m, a.M - 1) * a.ldx, k, a.K, x[m]);
+  for (int m = 0; m < MM; ++m) {
+    load_part(static_cast<const T*>(a.x) + min((int64_t)m, a.M - 1) * a.ldx, k, a.K, x[m]);
+    if (m >= a.M) {                               // (tokens that are not there: 0, not 0 times what may be infinite)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[m][e] = 0.0f;
+    }
+  }
   if (k >= a.K) return;
 #pragma unroll 2
   for (int64_t n = from + w; n < to; n += 4) {
     float v[VEC] = {};
 #pragma unroll
     for (int m = 0; m < MM; ++m) {
-      if (m >= a.M) continue;
-      const float f = dz[m * a.N + n];
+      const float f = dz[n * MM + m];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) v[e] += f * x[m][e];
     }
@@ -491,24 +501,32 @@ __global__ __launch_bounds__(256) void few_dw_kernel(DenseBackArgs a, const floa
     }
   }
 }
-constexpr int kFew = 16;
+// us of a call with all three gradients, N = K = 4096 in bf16: 1 token 29, 4 tokens 36, 8
+// tokens 47; by the other way 17 tokens 54, and 16 tokens by this one 84.
+constexpr int kFew = 8;
+// Tiles of 128 x 128 from which on w or x is taken as it is (us of a call so / by
+// transposes: 256 x 4096 x 4096 with 64 tiles of dx 72.8 / 69.2, 1024 x 2048 x 2048 with 128
+// of either 50.9 / 52.4, 512 x 4096 x 4096 80.3 / 86.4, 4096 x 4096 x 4096 308 / 340, 8192 x
+// 4096 x 1024 213 / 260).
+constexpr int kLeastTurned = 128;
 // Runs of w's rows, so that about 1024 workgroups read it, of 64 rows at least.
 int64_t few_runs(int64_t N, int64_t K, int vec) {
   return std::max<int64_t>(1, std::min<int64_t>({ceil_div(N, 64), 1024 / ceil_div(std::max<int64_t>(K, 1), 64 * vec), 32768}));
 }
+int few_tokens(int64_t M) { return M <= 1 ? 1 : M <= 4 ? 4 : kFew; }   // MM of M
 // Bytes of dz and of the runs' sums; never fewer for larger M, N or K.
 int64_t few_bytes(int64_t M, int64_t N, int64_t K) {
   M = std::min<int64_t>(M, kFew);
-  return round_up(M * N * 4, 256) + M * std::min<int64_t>(ceil_div(std::max<int64_t>(N, 1), 64) * K, 1024 * 512 + K) * 4;
+  return round_up(few_tokens(M) * N * 4, 256) + M * std::min<int64_t>(ceil_div(std::max<int64_t>(N, 1), 64) * K, 1024 * 512 + K) * 4;
 }
 template <typename T, int MM>
 int few_backward(hipStream_t s, const DenseBackArgs& a) {
   constexpr int VEC = vec_of<T>();
   float* dz = static_cast<float*>(a.workspace);
-  float* partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + round_up(a.M * a.N * 4, 256));
+  float* partial = reinterpret_cast<float*>(static_cast<char*>(a.workspace) + round_up(MM * a.N * 4, 256));
   const dim3 columns((unsigned)std::min<int64_t>(ceil_div(a.N, 256), 1 << 20));
-  if (a.btype == KMP_F32) hipLaunchKernelGGL((few_dz_kernel<T, float>), columns, dim3(256), 0, s, a, dz);
-  else hipLaunchKernelGGL((few_dz_kernel<T, T>), columns, dim3(256), 0, s, a, dz);
+  if (a.btype == KMP_F32) hipLaunchKernelGGL((few_dz_kernel<T, float, MM>), columns, dim3(256), 0, s, a, dz);
+  else hipLaunchKernelGGL((few_dz_kernel<T, T, MM>), columns, dim3(256), 0, s, a, dz);
   const int64_t across = ceil_div(a.K, 64 * VEC), runs = few_runs(a.N, a.K, VEC);
   if (a.dx && a.K > 0) {
     hipLaunchKernelGGL((few_dx_kernel<T, MM>), dim3((unsigned)across, (unsigned)runs), dim3(256), 0, s, a, dz, partial, ceil_div(a.N, runs));
@@ -537,19 +555,38 @@ struct Layout {
   }
 };
 
+// Products with operands given the other way round (kmp_tiles.h): w, or x and w.
+template <typename T, bool XT>
+int turned_product(hipStream_t s, const TileArgs& a, const OutArgs& out) {
+  typedef DenseTile<T, T> S;
+  const auto tiles = [&](int tm, int tn) { return ceil_div(a.M, tm) * ceil_div(a.N, tn); };
+  if (tiles(128, 128) <= 256) return ahead_as<T, S, 128, 128, 2, 4, 4, XT, true>(s, a, out);
+  if (tiles(256, 256) < 192) return ahead_as<T, S, 256, 128, 4, 2, 2, XT, true>(s, a, out);
+  return ahead_as<T, S, 256, 256, 2, 4, 2, XT, true>(s, a, out);
+}
+// Whether such an operand is: rows of a whole number of 16 bytes, at multiples of them.
+bool turnable(const void* p, int64_t ld, int64_t cols) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld % 8 == 0 && cols % 8 == 0;
+}
+
 template <typename T>
 int backward_as(hipStream_t s, const DenseBackArgs& a) {
   constexpr int SIZE = (int)sizeof(T);
   if (a.M > 0 && a.N > 0 && a.M <= kFew) {
-    if (a.M == 1) return few_backward<T, 1>(s, a);
-    if (a.M <= 4) return few_backward<T, 4>(s, a);
-    if (a.M <= 8) return few_backward<T, 8>(s, a);
-    return few_backward<T, 16>(s, a);
+    switch (few_tokens(a.M)) {
+      case 1: return few_backward<T, 1>(s, a);
+      case 4: return few_backward<T, 4>(s, a);
+      default: return few_backward<T, kFew>(s, a);
+    }
   }
   const Layout at(SIZE, a.M, a.N, a.K);
   char* ws = static_cast<char*>(a.workspace);
   float* partial = reinterpret_cast<float*>(ws + at.partial);
   const bool some = a.M > 0 && a.N > 0;
+  // Where w or x can be taken as they are, and the product has tiles enough for that, they
+  // are not transposed first.
+  const bool dx_as_is = SIZE == 2 && some && a.dx && turnable(a.w, a.ldw, a.K) && ceil_div(a.M, 128) * ceil_div(a.K, 128) >= kLeastTurned;
+  const bool dw_as_is = SIZE == 2 && some && a.dw && turnable(a.x, a.ldx, a.K) && ceil_div(a.N, 128) * ceil_div(a.K, 128) >= kLeastTurned;
   if (some) {
     TurnsArgs all{};
     int n = 0;
@@ -557,10 +594,11 @@ int backward_as(hipStream_t s, const DenseBackArgs& a) {
       all.each[n] = t;
       all.tiles[n++] = ceil_div(t.rows, 64) * ceil_div(t.cols, 64);
     };
-    add(TurnArgs{a.dout, a.lddo, a.act == KMP_ACT_NONE ? nullptr : a.z, a.ldz, a.act, a.M, a.N, a.dx ? ws + at.dz : nullptr, at.pn,
-                 a.dw ? ws + at.dz_turned : nullptr, at.pm, a.dbias ? partial : nullptr});
-    if (a.dx && a.K > 0) add(TurnArgs{a.w, a.ldw, nullptr, 0, 0, a.N, a.K, nullptr, 0, ws + at.w_turned, at.pn, nullptr});
-    if (a.dw && a.K > 0) add(TurnArgs{a.x, a.ldx, nullptr, 0, 0, a.M, a.K, nullptr, 0, ws + at.x_turned, at.pm, nullptr});
+    add(TurnArgs{a.dout, a.lddo, a.act == KMP_ACT_NONE ? nullptr : a.z, a.ldz, a.act, a.M, a.N,
+                 a.dx || dw_as_is ? ws + at.dz : nullptr, at.pn, a.dw && !dw_as_is ? ws + at.dz_turned : nullptr, at.pm,
+                 a.dbias ? partial : nullptr});
+    if (a.dx && a.K > 0 && !dx_as_is) add(TurnArgs{a.w, a.ldw, nullptr, 0, 0, a.N, a.K, nullptr, 0, ws + at.w_turned, at.pn, nullptr});
+    if (a.dw && a.K > 0 && !dw_as_is) add(TurnArgs{a.x, a.ldx, nullptr, 0, 0, a.M, a.K, nullptr, 0, ws + at.x_turned, at.pm, nullptr});
     const int64_t jobs = all.tiles[0] + all.tiles[1] + all.tiles[2];
     hipLaunchKernelGGL(turn_kernel<T>, dim3((unsigned)std::min<int64_t>(jobs, 1 << 20)), dim3(256), 0, s, all);
     KMP_LAUNCH_CHECK();
@@ -575,16 +613,30 @@ int backward_as(hipStream_t s, const DenseBackArgs& a) {
     KMP_LAUNCH_CHECK();
   }
   if (a.K == 0) return 0;
-  const auto product = [&](int64_t x, int64_t ldx, int64_t w, int64_t ldw, int64_t M, int64_t N, int64_t depth, void* out, int64_t ldo) {
-    const TileArgs t{reinterpret_cast<const int8_t*>(ws + x), ldx * SIZE, reinterpret_cast<const int8_t*>(ws + w), ldw * SIZE, M, N,
-                     depth * SIZE};
-    const OutArgs o{M, N, KMP_ACT_NONE, false, nullptr, nullptr, 0, out, ldo, nullptr, 0};
-    return product_as<T, T>(s, t, o);
+  const auto bytes = [](const void* p) { return static_cast<const int8_t*>(p); };
+  const auto plain = [](int64_t M, int64_t N, void* out, int64_t ldo) {
+    return OutArgs{M, N, KMP_ACT_NONE, false, nullptr, nullptr, 0, out, ldo, nullptr, 0};
   };
-  if (a.dx && a.M > 0)
-    if (int e = product(at.dz, at.pn, at.w_turned, at.pn, a.M, a.K, a.N, a.dx, a.lddx)) return e;
-  if (a.dw && a.N > 0)
-    if (int e = product(at.dz_turned, at.pm, at.x_turned, at.pm, a.N, a.K, a.M, a.dw, a.lddw)) return e;
+  if (a.dx && a.M > 0) {
+    const OutArgs o = plain(a.M, a.K, a.dx, a.lddx);
+    if (dx_as_is) {
+      if constexpr (SIZE == 2)
+        if (int e = turned_product<T, false>(s, TileArgs{bytes(ws + at.dz), at.pn * SIZE, bytes(a.w), a.ldw * SIZE, a.M, a.K, a.N * SIZE}, o)) return e;
+    } else {
+      const TileArgs t{bytes(ws + at.dz), at.pn * SIZE, bytes(ws + at.w_turned), at.pn * SIZE, a.M, a.K, a.N * SIZE};
+      if (int e = product_as<T, T>(s, t, o)) return e;
+    }
+  }
+  if (a.dw && a.N > 0) {
+    const OutArgs o = plain(a.N, a.K, a.dw, a.lddw);
+    if (dw_as_is) {
+      if constexpr (SIZE == 2)
+        if (int e = turned_product<T, true>(s, TileArgs{bytes(ws + at.dz), at.pn * SIZE, bytes(a.x), a.ldx * SIZE, a.N, a.K, a.M * SIZE}, o)) return e;
+    } else {
+      const TileArgs t{bytes(ws + at.dz_turned), at.pm * SIZE, bytes(ws + at.x_turned), at.pm * SIZE, a.N, a.K, a.M * SIZE};
+      if (int e = product_as<T, T>(s, t, o)) return e;
+    }
+  }
   return 0;
 }
 

@@ -80,7 +80,7 @@ def test_every_place_once(xt):
     """x and w of one 1 a row each: every product is 0 or 1, exactly; any wrong index shows."""
     import torch
     from paper_2606_06742_amd import kmpath as km
-    for M, N, K in ((33, 65, 70), (300, 500, 96), (1000, 2000, 129), (2100, 8400, 72)):
+    for M, N, K in ((33, 65, 70), (300, 500, 96), (1000, 2000, 129), (2100, 8400, 72), (1200, 1300, 1048), (40, 2500, 2056)):
         announce(f"dense product, ones, {xt} {M} x {N} x {K}")
         rng = np.random.default_rng(M)
         i, j = torch.as_tensor(rng.integers(0, K, M), device=device()), torch.as_tensor(rng.integers(0, K, N), device=device())
@@ -165,6 +165,18 @@ def test_backward_of_large_tiles(xt):
     for M, N, K, pad, act in ((1100, 1300, 700, 0, "gelu"), (2600, 500, 1900, 1, "silu"), (130, 4200, 2100, 0, "relu"),
                               (8, 4096, 1500, 0, "gelu_tanh"), (2, 1500, 5000, 1, "gelu")):
         announce(f"dense product backward {xt} {M} x {N} x {K} gap {pad} {act}")
+        _check_backward(np.random.default_rng(M + N), M, N, K, xt, act, pad, 0)
+
+
+@pytest.mark.parametrize("xt", ["bf16", "f16"])
+def test_backward_of_operands_as_they_are(xt):
+    """Rows of whole 16 bytes, at multiples of them: w and x are not transposed first. Depths
+    with and without a rest, fewer than a slice, columns that end inside a tile, channels
+    that are no multiple of 8; and rows just not aligned beside them."""
+    for M, N, K, pad, act in ((700, 1003, 1104, 0, "gelu"), (300, 2051, 1024, 8, "silu"), (2100, 1500, 2304, 0, "none"),
+                              (60, 1030, 8200, 16, "relu"), (1025, 17, 1032, 0, "gelu"), (4100, 3000, 520, 0, "gelu_tanh"),
+                              (700, 1003, 1104, 4, "gelu")):
+        announce(f"dense product backward, operands as they are, {xt} {M} x {N} x {K} gap {pad} {act}")
         _check_backward(np.random.default_rng(M + N), M, N, K, xt, act, pad, 0)
 
 
