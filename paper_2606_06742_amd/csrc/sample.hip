@@ -446,10 +446,9 @@ __host__ __device__ constexpr int64_t segment_length(int64_t V) {
 }
 __host__ __device__ constexpr int64_t segments(int64_t V) { return ceil_div(V, segment_length(V)); }
 
-// exp(f / 16) - 1 for f in [0, 1]: Taylor's terms up to (f / 16)^7, the next is below
+// exp(r) - 1 for r = f / 16 in [0, 1 / 16]: Taylor's terms up to r^7, the next is below
 // 2^-47.
-__device__ __forceinline__ double grow(double f) {
-  const double r = f * (1.0 / kFine);
+__device__ __forceinline__ double grow(double r) {
   double p = 1.0 / 5040.0;
   p = fma(p, r, 1.0 / 720.0);
   p = fma(p, r, 1.0 / 120.0);
@@ -459,6 +458,12 @@ __device__ __forceinline__ double grow(double f) {
   p = fma(p, r, 1.0);
   return p * r;
 }
+
+// f / 16 = (v scale - bin) step. The product's rounding may have taken it up to a bin's
+// border, from below: f is then below 0 by that much, and kept so. From 2^40 on f is 0:
+// different logits are 2^-24 of them apart or more, so that only equal ones share a grid
+// from 2^33 on, and from 2^53 on f is rounding alone.
+__device__ __forceinline__ double step_of(double first) { return fabs(first) < 0x1p40 ? 1.0 / kFine : 0.0; }
 
 // A row's choices.
 struct Choice {
@@ -491,11 +496,14 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
   __shared__ uint32_t counts[CW];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t length = segment_length(a.V), from = blockIdx.x * length, to = min(a.V, from + length);
-  const int c = 64 - __clzll((unsigned long long)ceil_div(min(length, a.V), COLUMNS)) + 1, q = min(67 - 2 * c, 51);
+  // a column's elements are whole vectors
+  const int64_t most = vec_of<T>() * ceil_div(min(length, a.V), (int64_t)COLUMNS * vec_of<T>());
+  const int c = 64 - __clzll((unsigned long long)most) + 1, q = min(67 - 2 * c, 51);
+  const unsigned long long half = (unsigned long long)1 << (63 - c);   // a sum of 0: a little below it takes none off the count
   for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
     const T* x = static_cast<const T*>(a.logits) + t * a.ld;
     Segment* out = static_cast<Segment*>(a.workspace) + t * gridDim.x + blockIdx.x;
-    for (int i = threadIdx.x; i < GRID * COLUMNS; i += CT) (&bins[0][0])[i] = 0;
+    for (int i = threadIdx.x; i < GRID * COLUMNS; i += CT) (&bins[0][0])[i] = half;
     float m = -INFINITY;
     visit<4, CW>(x, from, to, [&](int64_t, float v) { m = __builtin_elementwise_maximum(m, v); });   // NaN where one is
 #pragma unroll
@@ -524,15 +532,15 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
     const bool some = m > -INFINITY && m < INFINITY && !choice.greedy;
     const double it = 1.0 / (double)choice.temperature, scale = kFine * it, first = floor((double)m * scale);
     if (some) {
-      // p + 2^(52 - q) holds p in steps of 2^-q in its last bits; the count's one is added
-      // and the sum's exponent taken off at once
-      const double magic = ldexp(1.0, 52 - q);
+      // p + 1.5 2^(52 - q) holds p in steps of 2^-q in its last bits; the count's one is
+      // added and the constant's bits taken off at once
+      const double magic = ldexp(1.5, 52 - q), step = step_of(first);
       const unsigned long long one = ((unsigned long long)1 << (64 - c)) - (unsigned long long)__double_as_longlong(magic);
       unsigned long long* column = &bins[0][lane & (COLUMNS - 1)];
       visit<1, CW>(x, from, to, [&](int64_t, float v) {
         const double bin = floor((double)v * scale), place = first - bin;
         if (place < (double)GRID) {
-          const double p = grow(fma((double)v, scale, -bin));
+          const double p = grow(fma((double)v, scale, -bin) * step);
           atomicAdd(column + (int)place * COLUMNS, (unsigned long long)__double_as_longlong(p + magic) + one);
         } else if (v > -INFINITY) {
           ++tail_count;
@@ -556,13 +564,13 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
       tail = block_sum<CW>(tail, red);
     }
     for (int g = threadIdx.x; g < GRID; g += CT) {
-      unsigned long long sum = 0;
+      int64_t sum = 0;
       uint32_t n = 0;
       const unsigned long long low = ((unsigned long long)1 << (64 - c)) - 1;
 #pragma unroll 4
       for (int k = 0; k < COLUMNS; ++k) {         // (staggered over the banks)
         const unsigned long long b = bins[g][(k + g) & (COLUMNS - 1)];
-        sum += b & low;
+        sum += (int64_t)(b & low) - (int64_t)half;
         n += (uint32_t)(b >> (64 - c));
       }
       out->weight[g] = (double)n + ldexp((double)sum, -q);
@@ -654,7 +662,7 @@ static_assert(GRID == NT, "a bin a thread");
 template <typename T>
 __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segment* seg, int segs, int64_t length, int64_t k, double p,
                         double u, double& share) {
-  const double scale = kFine * row.it, y = (double)row.m * scale, first = floor(y), f0 = fma((double)row.m, scale, -first);
+  const double scale = kFine * row.it, y = (double)row.m * scale, first = floor(y), f0 = kFine * step_of(first) * fma((double)row.m, scale, -first);
   const int g = threadIdx.x;
   // a bin's weights relative to the row's maximum, from those relative to its border
   const auto border_weight = [&](double bin) { return exp(-(first - bin + f0) * (1.0 / kFine)); };

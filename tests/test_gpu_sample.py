@@ -95,7 +95,7 @@ def test_choices_of_their_own():
     assert tokens[11] == V - 1 and tokens[3] == 0 and tokens[15] == 0
 
 
-@pytest.mark.parametrize("V", [3, 1000, 5000, 70001])
+@pytest.mark.parametrize("V", [3, 4, 8, 17, 32, 48, 1000, 5000, 70001])
 def test_equal_logits(V):
     """Ties: weights of 1, whose sums are exact, so that every border is; the lowest
     indices are kept."""
@@ -147,6 +147,46 @@ def test_masks():
     for rule in (dict(temperature=nan), dict(top_p=nan), dict(min_p=nan)):
         assert _check(x, values, good, **rule)[1] == -1
     assert _check(x, values, nan)[1] == -1
+
+
+@pytest.mark.parametrize("V", [1, 20, 300, 2000, 20001, 70001])
+def test_whole_multiples_of_the_temperature(V):
+    """Logits k times the temperature, exactly: their quotients round up to whole numbers
+    as often as down. Few in a row, so that each counts; large ones, near and far from
+    each other; every weight is known by k alone."""
+    rng = np.random.default_rng(V)
+    T = 128 if V <= 2000 else 12
+    temperature = rng.uniform(0.02, 3.0, T).astype(np.float32).astype(np.float64)
+    for scale in (1, 2 ** 12, 2 ** 30):
+        k = (rng.integers(-3, 4, (T, V)) + 8) * scale
+        x = (temperature[:, None] * 2.0 ** rng.integers(0, 3, (T, V)) * scale).astype(np.float32)
+        x[::2] = (temperature[::2, None] * k[::2]).astype(np.float32)
+        logits, values = _put(x.astype(np.float64), _dtype("f32"))
+        for rule in (dict(), dict(top_p=[0.8] * T), dict(top_k=[max(1, V // 3)] * T), dict(min_p=[0.01] * T)):
+            announce(f"sample, multiples of the temperature, {V}, times {scale}, {rule}")
+            _check(logits, values, rng.random(T), temperature=temperature, exact=True, **rule)
+
+
+@pytest.mark.parametrize("V", [5, 300, 3001, 40000])
+def test_lowest_values_at_other_temperatures(V):
+    """Rows of the type's lowest value alone (weights of 1 each) and rows masked by it, at
+    temperatures whose inverse is rounded, down to the smallest and up to the largest."""
+    rng = np.random.default_rng(V + 1)
+    for xt, low in (("f32", np.finfo(np.float32).min), ("bf16", -3.3895e38), ("f16", -65504.0)):
+        announce(f"sample, lowest values, {xt} {V}")
+        temperature = np.array([0.7, 0.3, 1.3, 1e-3, 1e-30, 1e-44, 3e38, 11.0])
+        T = len(temperature)
+        x = np.full((T, V), low)
+        for rows in ("all", "one", "some", "highest"):
+            if rows == "one":
+                x[:, V // 2] = 1.25
+            if rows == "some":
+                x[:, ::4] = 1.25
+            if rows == "highest":
+                x = -x
+            logits, values = _put(x, _dtype(xt), 1, 1)
+            for rule in (dict(), dict(top_k=[max(1, V // 8)] * T), dict(top_p=[0.3] * T), dict(min_p=[0.5] * T)):
+                _check(logits, values, rng.random(T), temperature=temperature, exact=True, **rule)
 
 
 def test_wide_ranges():
