@@ -329,10 +329,11 @@ int kmp_dgemm_grouped(void* stream, int32_t G, int32_t M, int32_t N, int32_t K,
 
 /* ------------------------------------------------------------------------
  * Operators at a language model's end: the layer norm of its hidden states,
- * the norms around its blocks, the 8-bit product with its vocabulary head, the log
- * probabilities of its tokens and their choice. A kernel machine's features often come from there (hidden states;
- * log probability and entropy of an answer's tokens). Their gradients train the
- * model's end itself: the path above gives none with respect to its features.
+ * the norms around its blocks, products with an activation, the 8-bit product with
+ * its vocabulary head, the log probabilities of its tokens and their choice. A kernel
+ * machine's features often come from there (hidden states; log probability and entropy
+ * of an answer's tokens). Their gradients train the model's end itself: the path above
+ * gives none with respect to its features.
  * Unlike the entry points above they work in 16 or 32 bits (sums and statistics
  * in 32, or 64 for doubles, which the layer norm takes), never allocate, never
  * wait for the device and may be captured into a HIP graph. Element types:  */
@@ -390,7 +391,8 @@ int kmp_layer_norm_backward(void* stream, int32_t xtype, const void* dy, int64_t
  *              KMP_F32 for 16-bit x), each may be NULL (ones, zeros)
  *   gate       NULL (ones); with ldg = 0 DEVICE [d] of wtype, for every row; with
  *              ldg >= d DEVICE, rows x d of xtype
- *   h          DEVICE, xtype; may be NULL; h == res with ldh == ldr is allowed
+ *   h          DEVICE, xtype; may be NULL; h == res with ldh == ldr is allowed; no
+ *              output overlaps an input otherwise, or another output
  *   y          DEVICE, of type ytype = xtype or KMP_I8 (as by kmp_quantize_rows,
  *              scales in scale [rows]); may be NULL: no norm of h. h or y
  *   stats      DEVICE [rows][4]: mu and r of b's norm, mu and r of h's (0 and 1
@@ -466,8 +468,9 @@ int kmp_quantized_product(void* stream, const int8_t* x, int64_t ldx, const floa
  * KMP_F32) or NULL; out and residual (NULL: none) DEVICE M x N of type otype (x's
  * type or KMP_F32); zout DEVICE M x N of x's type or NULL: z, which the backward
  * pass reads. Sums and epilogue are in 32 bits, out and zout are each rounded once.
- * out may be residual with the same leading dimension. Rows that start at multiples
- * of 16 bytes are read fastest. K = 0 gives act(bias) + residual. K <= 2^28; at
+ * out may be residual with the same leading dimension; no output overlaps an input
+ * otherwise, or another output. Rows that start at multiples of 16 bytes are read
+ * fastest. K = 0 gives act(bias) + residual. K <= 2^28; at
  * most 2^23 tiles of 64 x 64 (KMP_EINVAL above).                              */
 int kmp_dense_product(void* stream, int32_t type, const void* x, int64_t ldx, int64_t M, const void* w,
                       int64_t ldw, int64_t N, int64_t K, int32_t btype, const void* bias, int32_t act,
@@ -488,7 +491,8 @@ size_t kmp_dense_product_workspace_bytes(int32_t type, int64_t M, int64_t N, int
  * without dx. In 16 bits dz is rounded to type for the products, as their operands
  * are, but not for dbias. Sums are in 32 bits and in a fixed order: the same call
  * gives the same bits. M = 0 gives dw = dbias = 0, N = 0 dx = 0. M, N and K <= 2^28.
- * The workspace is aligned to 16 bytes.                                       */
+ * No output overlaps an input or another output. The workspace is aligned to 16
+ * bytes.                                                                      */
 int kmp_dense_product_backward(void* stream, int32_t type, const void* dout, int64_t lddo, int64_t M, int64_t N,
                                int64_t K, int32_t act, const void* z, int64_t ldz, const void* x, int64_t ldx,
                                const void* w, int64_t ldw, void* dx, int64_t lddx, void* dw, int64_t lddw,

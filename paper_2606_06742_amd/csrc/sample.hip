@@ -9,6 +9,12 @@
 // comparisons of sums over the vocabulary, whose neighbours differ by one weight (1e-6
 // of the sum and less): weights and sums are in 64 bits, where a wrong side is a matter
 // of 1e-10, and every sum has a fixed order, or is one of whole numbers.
+// Two launches: segments of rows are read once for histograms of their weights, on one
+// grid, so that a row's bins are sums of its segments'; then a workgroup per row finds the
+// bins that hold its cuts, and lists and orders only their tokens. Bound by the 64-bit
+// work on each logit (1024 x 128000 bf16: 176 us at 37 instructions a logit, where the
+// reads take 53 at a copy's rate) and by reading the row again for the list (129 us);
+// by sorting rows, 16.4 ms. One row: by two dependent launches (9 and 15 us).
 #include "kmp_keys.h"
 
 namespace kmp {
@@ -904,7 +910,7 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs)
       logp = 0.0;
     } else if (!nan) {
       Row<T> row = choice.row(sh, x, a.V, m);
-      double share;
+      double share = 0.0;
       token = pick(sh, row, seg, segs, length, choice.k, (double)choice.p, max((double)choice.u, 0.0), share);
       logp = log(share);
       if (token < 0) {
