@@ -13,7 +13,7 @@
 // grid, so that a row's bins are sums of its segments'; then a workgroup per row finds the
 // bins that hold its cuts, and lists and orders only their tokens. Bound by the 64-bit
 // work on each logit (1024 x 128000 bf16: 176 us at 37 instructions a logit, where the
-// reads take 53 at a copy's rate) and by reading the row again for the list (129 us);
+// reads take 53 at a copy's rate) and by reading the row again for the list (about 100 us);
 // by sorting rows, 16.4 ms. One row: by two dependent launches (9 and 15 us).
 #include "kmp_keys.h"
 
@@ -46,7 +46,11 @@ struct Shared : Common {               // of passes over a row alone
 };
 struct PickShared : Common {           // with the histograms of its segments
   key_t listed[LISTED];
-  double sums[LISTED];                 // running sums of their weights
+  union {
+    double sums[LISTED];               // running sums of their weights
+    key_t turned[LISTED];              // while they are put in order: by buckets
+  };
+  int filled[NT], most;                // keys of a bucket, its end
   double weight[GRID];                 // running sums of the bins, relative to the row's maximum
   double tokens[GRID];
   double before[kMostSegs];
@@ -591,13 +595,18 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
 }
 
 // ---- The draw, one workgroup per row
-// The first n keys of sh.listed (all different; n <= LISTED) in descending order: a key's
-// place is the number of larger ones where they are few, else by bitonic merges (the rest
-// up to the next power of two is cleared). 50 keys: 0.8 us, by shuffles of one wavefront
-// 3.2.
-__device__ __forceinline__ void sort_list(PickShared& sh, int n) {
+// The first n keys of sh.listed (all different; n <= LISTED) in descending order. Few: a
+// key's place is the number of larger ones (50 keys: 0.8 us, by shuffles of one wavefront
+// 3.2). Else by buckets, bucket_of(key) in [0, NT), of which none has a larger key than the
+// one before it: a key's place is its bucket's plus the number of larger ones in that; where
+// one has more than kCrowded keys, by bitonic merges (the rest up to the next power of two
+// is cleared). 45 rows with 600 keys or so: 54.2 us by merges, 50 by buckets, 57 by counting
+// up to 512.
+constexpr int kCounted = 128, kCrowded = 256;
+template <typename F>
+__device__ __forceinline__ void sort_list(PickShared& sh, int n, F bucket_of) {
   const int t = threadIdx.x;
-  if (n <= NT) {
+  if (n <= kCounted) {
     const key_t mine = t < n ? sh.listed[t] : 0;
     int rank = 0;
     if ((t & ~63) < n) {
@@ -609,7 +618,35 @@ __device__ __forceinline__ void sort_list(PickShared& sh, int n) {
     __syncthreads();
     return;
   }
-  int size = 2 * NT;
+  sh.filled[t] = 0;
+  if (t == 0) sh.most = 0;
+  __syncthreads();
+  for (int i = t; i < n; i += NT) atomicAdd(&sh.filled[bucket_of(sh.listed[i])], 1);
+  __syncthreads();
+  const int own = sh.filled[t];
+  double all;
+  const int end = (int)block_running(sh, (double)own, all);   // (whole numbers: exact)
+  if (own > kCrowded) sh.most = own;
+  __syncthreads();
+  if (sh.most == 0) {
+    sh.filled[t] = end - own;
+    __syncthreads();
+    for (int i = t; i < n; i += NT) {
+      const key_t key = sh.listed[i];
+      sh.turned[atomicAdd(&sh.filled[bucket_of(key)], 1)] = key;
+    }
+    __syncthreads();
+    for (int i = t; i < n; i += NT) {             // (filled: the bucket's end)
+      const key_t key = sh.turned[i];
+      const int b = bucket_of(key), from = b > 0 ? sh.filled[b - 1] : 0, to = sh.filled[b];
+      int rank = from;
+      for (int j = from; j < to; ++j) rank += sh.turned[j] > key;
+      sh.listed[rank] = key;
+    }
+    __syncthreads();
+    return;
+  }
+  int size = 2 * kCounted;
   while (size < n) size *= 2;
   for (int i = n + t; i < size; i += NT) sh.listed[i] = 0;
   __syncthreads();
@@ -665,7 +702,7 @@ static_assert(GRID == NT, "a bin a thread");
 // 32 e-foldings, or with more than LISTED tokens in their bins). The bins that hold the
 // cuts are known from running sums over the bins; only their tokens are looked for in
 // the row and put in order, and where all that is kept is few, these, too.
-template <typename T>
+template <int WHOLE, typename T>
 __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segment* seg, int segs, int64_t length, int64_t k, double p,
                         double u, double& share) {
   const double scale = kFine * row.it, y = (double)row.m * scale, first = floor(y), f0 = kFine * step_of(first) * fma((double)row.m, scale, -first);
@@ -702,7 +739,10 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
   // the bins in which the cuts lie: the k-th token's, those where the sum may reach p of
   // the first k tokens' (their weight is not known before they are in order), those
   // around min_p
-  const bool by_k = k < row.V, by_p = p < 1.0, by_m = row.min_p > 0.0;
+  const bool by_p = p < 1.0, by_m = row.min_p > 0.0;
+  // (where k is not below the number of tokens that have a weight, most others being ruled
+  // out, it leaves none out: 300 x 50000 with 500 left and k = 1000 384 / 64 us)
+  const bool by_k = k < row.V && (below > 0.0 || (double)k < tokens);
   int kb = GRID, lo = GRID, hi = GRID - 1;
   double least = total + below, most = least;
   if (by_k) {
@@ -729,8 +769,10 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
   if (by_k || by_p || by_m) {
     lo = min(lo, first_of(sh, GRID, [&](int b) { return sh.tokens[b] >= sh.tokens[hi]; }));   // (a bin that has tokens)
     const bool far = by_k && by_p && kb > hi;     // the k-th token's bin as well, for the weight of the first k
-    // (all that may be kept where that is few: a longer list is not put in order as fast)
-    if (count_to(hi) + (far ? count_to(kb) - count_to(kb - 1) : 0) <= NT) lo = 0;
+    // (all that may be kept where that is few, WHOLE at most: then no run of the row has to
+    // be passed through for the draw. us with 512 / 2048: 1024 rows with 1280 tokens that
+    // are not ruled out 517 / 394, one such row 52.9 / 55.9, so that few rows take 512)
+    if (count_to(hi) + (far ? count_to(kb) - count_to(kb - 1) : 0) <= WHOLE) lo = 0;
     const int64_t near = count_to(hi) - count_to(lo - 1), more = far ? count_to(kb) - count_to(kb - 1) : 0;
     if (near + more > LISTED) return -1;
     // list them: logits below `low` are of later bins (a little lower than the border, for
@@ -745,7 +787,7 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
       const double d = first - floor((double)v * scale);
       return d < (double)GRID ? (int)d : GRID;
     };
-    visit<8>(row.x, 0, row.V, [&](int64_t j, float v) {
+    visit<4>(row.x, 0, row.V, [&](int64_t j, float v) {
       bool is = v >= low && v > -INFINITY;
       if (!__any(is)) return;
       const int b = bin_of(v);
@@ -761,7 +803,11 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
     __syncthreads();
     const int size = min(sh.n, LISTED);
     __syncthreads();
-    sort_list(sh, size);
+    const double edge = first - lo + 1.0, finer = (double)NT / (last - lo + 1);
+    sort_list(sh, size, [&](key_t key) {
+      const double d = edge - (double)key_value((uint32_t)(key >> 32)) * scale;
+      return (int)min(max(d * finer, 0.0), (double)(NT - 1));
+    });
     const auto weight = [&](key_t key) { return row.weight(key_value((uint32_t)(key >> 32))); };
     sum_list(sh, size, weight);
     const int run = (int)near;                    // the first of them, bins lo to hi
@@ -793,7 +839,8 @@ __device__ __forceinline__ int64_t pick(PickShared& sh, Row<T>& row, const Segme
   if (listed > 0) {                               // by index: the complemented index above the value's bits
     for (int i = threadIdx.x; i < listed; i += NT) sh.listed[i] = sh.listed[i] << 32 | sh.listed[i] >> 32;
     __syncthreads();
-    sort_list(sh, listed);
+    const double finer = (double)NT / (double)row.V;
+    sort_list(sh, listed, [&](key_t key) { return min((int)((double)(uint32_t)~(uint32_t)(key >> 32) * finer), NT - 1); });
     sum_list(sh, listed, [&](key_t key) { return row.weight(key_value((uint32_t)key)); });
     if (lo == 0) {                                // all that is kept
       int i = first_of(sh, listed, [&](int i) { return sh.sums[i] > goal; });
@@ -880,9 +927,10 @@ __device__ __forceinline__ int64_t draw_aside(Shared& sh, const SampleArgs& a, c
 
 // ASIDE: those rows in the same launch, for no more rows than the chip has compute units
 // (the registers and LDS of both allow one workgroup each there, of the draw alone two;
-// a launch costs 4 us).
+// a launch costs 4 us). Two need 128 registers, of which a few spill: us for one / two
+// workgroups 1024 x 128000 bf16 286 / 268, 300 x 50000 f32 128 / 99, 2000 x 4000 f16 129 / 98.
 template <typename T, bool ASIDE>
-__global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs) {
+__global__ __launch_bounds__(NT, ASIDE ? 2 : 4) void sample_pick_kernel(SampleArgs a, int segs) {
   union All {
     PickShared pick;
     Shared aside;
@@ -911,7 +959,7 @@ __global__ __launch_bounds__(NT) void sample_pick_kernel(SampleArgs a, int segs)
     } else if (!nan) {
       Row<T> row = choice.row(sh, x, a.V, m);
       double share = 0.0;
-      token = pick(sh, row, seg, segs, length, choice.k, (double)choice.p, max((double)choice.u, 0.0), share);
+      token = pick<ASIDE ? NT : 2048>(sh, row, seg, segs, length, choice.k, (double)choice.p, max((double)choice.u, 0.0), share);
       logp = log(share);
       if (token < 0) {
         if constexpr (ASIDE) {

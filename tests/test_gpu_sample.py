@@ -149,6 +149,27 @@ def test_masks():
     assert _check(x, values, nan)[1] == -1
 
 
+@pytest.mark.parametrize("T", [40, 300])
+@pytest.mark.parametrize("xt", ["f32", "bf16"])
+def test_lists_of_every_length(T, xt):
+    """Lists of tens to thousands of tokens near the cuts, spread, close together and with
+    many equal ones, in few and in many rows; the allowed ones at one end, scattered, and
+    fewer than top_k, with others so far below that they have hardly a weight, or none."""
+    rng = np.random.default_rng(T)
+    V = 6000
+    for spread in (0.01, 0.3, 2.0):
+        x = spread * rng.standard_normal((T, V))
+        x[1::4] = np.round(x[1::4] * 8) / 8
+        x[2::4, 1500:] -= rng.choice([40.0, 300.0, 2000.0, np.inf], (len(x[2::4]), 1))
+        x[3::4, rng.random(V) < 0.7] = -np.inf
+        logits, values = _put(x, _dtype(xt))
+        for rule in (dict(top_p=rng.uniform(0.02, 0.999, T)), dict(top_k=rng.integers(1, V, T)), dict(min_p=rng.uniform(0.01, 0.99, T)),
+                     dict(top_k=rng.integers(100, 4000, T), top_p=rng.uniform(0.1, 0.99, T)), dict(top_k=np.full(T, 1600)),
+                     dict(top_k=np.full(T, 5000), top_p=rng.uniform(0.5, 0.99, T))):
+            announce(f"sample, lists, {T} rows {xt} spread {spread} {list(rule)}")
+            _check(logits, values, rng.random(T), exact=True, **rule)
+
+
 @pytest.mark.parametrize("V", [1, 20, 300, 2000, 20001, 70001])
 def test_whole_multiples_of_the_temperature(V):
     """Logits k times the temperature, exactly: their quotients round up to whole numbers
