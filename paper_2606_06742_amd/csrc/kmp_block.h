@@ -11,7 +11,8 @@
 // of t, and dgate = s n has no sum). Bound by memory: b and res are read, h and y
 // written, and the backward pass reads dy, dh, h and b and writes db and dres, each
 // once. y is formed from h in 32 bits; the backward pass reads h as it was rounded, as
-// 32 bits of it would double that read.
+// 32 bits of it would double that read: dg2 has that rounding beside its own, 1.4 (up to
+// 1.53 seen) times the error of one.
 #pragma once
 
 #include "kmp_rows.h"
