@@ -389,8 +389,8 @@ int kmp_layer_norm_backward(void* stream, int32_t xtype, const void* dy, int64_t
  *   res        NULL: no residual
  *   gamma_after, beta_after, gamma, beta  DEVICE [d] of type wtype (xtype, or
  *              KMP_F32 for 16-bit x), each may be NULL (ones, zeros)
- *   gate       NULL (ones); with ldg = 0 DEVICE [d] of wtype, for every row; with
- *              ldg >= d DEVICE, rows x d of xtype
+ *   gate       NULL (ones, whatever ldg is); with ldg = 0 DEVICE [d] of wtype, for
+ *              every row; with ldg >= d DEVICE, rows x d of xtype
  *   h          DEVICE, xtype; may be NULL; h == res with ldh == ldr is allowed; no
  *              output overlaps an input otherwise, or another output
  *   y          DEVICE, of type ytype = xtype or KMP_I8 (as by kmp_quantize_rows,

@@ -108,6 +108,7 @@ int kmp_block_norm(void* stream, int32_t xtype, int32_t flags, const void* b, in
     if (!h && !y) return refuse(name, "h or y must be given");
     if (h && h == res && ldh != ldr) return refuse(name, "h may be res with the same leading dimension only");
     if (!b || (y && ytype == KMP_I8 && !scale)) return refuse(name, "null pointer");
+    if (!gate) ldg = 0;                           // (the kernels take a gate per row by it)
     BlockArgs a{xtype, wtype, (flags & KMP_NORM_RMS) != 0, (flags & KMP_NORM_AFTER) != 0, b, ldb, res, ldr, rows, d,
                 gamma_after, beta_after, gate, ldg, (float)rscale, gamma, beta, (float)eps, h, ldh,
                 y && ytype == KMP_I8, y, ldy, stats, scale};
@@ -150,6 +151,7 @@ int kmp_block_norm_backward(void* stream, int32_t xtype, int32_t flags, const vo
       if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15))
         return refuse(name, "the workspace is missing, too small or not aligned to 16 bytes", KMP_EWORKSPACE);
     }
+    if (!gate) ldg = 0;                           // (the kernels take a gate per row by it)
     const int64_t at = round_up(block_partials(xtype, rows, d) * 4 * d * 4, 16) / 4;
     BlockBackArgs a{xtype, wtype, (flags & KMP_NORM_RMS) != 0, after, dy, lddy, dh, lddh, b, ldb, h, ldh, rows, d,
                     gamma_after, beta_after, gate, ldg, (float)rscale, gamma, stats, db, lddb, dres, lddres, dgate, lddg,
