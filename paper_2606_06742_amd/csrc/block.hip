@@ -131,11 +131,15 @@ __global__ __launch_bounds__(threads_of(TPR)) void block_reg_kernel(BlockArgs a)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) v[i][e] = fmaf(v[i][e] * r2, g2[i][e], c2[i][e]);
       if (BYTES) {
+        // (not of what another thread has, too: where h is written over res, that may have
+        // been read after that thread's store)
         float most = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+          const int skip = place(i).skip;
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) most = larger(most, fabsf(v[i][e]));
+          for (int e = 0; e < VEC; ++e) most = e < skip ? most : larger(most, fabsf(v[i][e]));
+        }
         const ByteScale bs(row_most<TPR>(most, fred, fslot));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {

@@ -36,3 +36,26 @@ def test_no_gate_with_a_leading_dimension(d):
     for other in outs[1:]:
         for a, b in zip(outs[0], other):
             assert not a.isnan().any() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("xt", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [7, 333, 1025, 1031, 4160, 8190, 16391, 17001])
+def test_rows_in_8_bits_in_place(xt, d):
+    """h over res with y in 8 bits, with and without a norm of b (no barrier then stands
+    between a wavefront's first reads of res and another's writes of h): widths that are
+    no whole number of vectors, whose last ones overlap their neighbours."""
+    import torch
+    from tests.test_gpu_operators import _put
+    import numpy as np
+    rows = 600
+    for after, rms in ((False, False), (False, True), (True, False)):
+        announce(f"block norm to 8 bits in place {xt} {rows} x {d}, norm of b {after}, root mean square {rms}")
+        c = Case(rows, d, xt, xt, after, rms, "vector", rscale=3.0)
+        outs = []
+        for h in (c.matrix(), c.t["res"]):
+            q, _ = _put(np.zeros((rows, d), np.int8), torch.int8)
+            scale = torch.full((rows,), float("nan"), device=device())
+            c.forward(h, q, scale)
+            outs.append((h, q, scale, c.stats.clone()))
+        for a, b in zip(*outs):
+            assert torch.equal(a, b)
