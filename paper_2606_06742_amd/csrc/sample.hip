@@ -282,15 +282,18 @@ struct Passes : Row<T> {
     atomicAdd(&sh.h.sum[bin][c], w);
     atomicAdd(&sh.h.count[bin][c], 1u);
   }
-  __device__ void read_bins(unsigned long long& w, uint32_t& n) {
+  __device__ void read_bins(double& w, uint32_t& n) {
     __syncthreads();
-    w = 0, n = 0;
+    unsigned long long low = 0, high = 0;         // (a column has up to 64 bits)
+    n = 0;
     if (threadIdx.x < BINS)
       for (int c = 0; c < COLS; ++c) {            // (staggered over the banks)
         const int at = (c + threadIdx.x) & (COLS - 1);
-        w += sh.h.sum[threadIdx.x][at];
+        low += (uint32_t)sh.h.sum[threadIdx.x][at];
+        high += sh.h.sum[threadIdx.x][at] >> 32;
         n += sh.h.count[threadIdx.x][at];
       }
+    w = ldexp((double)high, 32) + (double)low;
     __syncthreads();
   }
 
@@ -308,10 +311,10 @@ struct Passes : Row<T> {
         if (key < lo || key > hi || !is(key, v)) return;
         add((int)((hi - key) >> shift), WEIGHED ? (unsigned long long)rint(ldexp(scaled(v), q)) : 1ull);
       });
-      unsigned long long w;
+      double w;
       uint32_t count;
       read_bins(w, count);
-      const double own = WEIGHED ? ldexp((double)w, -q) * unit : (double)count;
+      const double own = WEIGHED ? ldexp(w, -q) * unit : (double)count;
       double total;
       const double running = block_running(sh, threadIdx.x < BINS ? own : 0.0, total);
       int b = block_first(sh, threadIdx.x < BINS && count > 0 && reach(above + running));
@@ -346,7 +349,9 @@ struct Passes : Row<T> {
   // each an eighth: a bin's weights are summed as whole numbers, scaled by its top. What
   // lies below (2^-46 and less of the top's weight each) is the next window's.
   __device__ key_t reach_p(double p, key_t cut) {
-    const int q = 62 - (64 - __clzll((unsigned long long)V));
+    // (a column's elements, those of 16 threads, are V / 32 and 256 at most: 2^-47 up to 2^20
+    // tokens, 2^-36 for the longest rows)
+    const int q = min(52, __clzll((unsigned long long)(V / 32 + 256)) - 1);
     const double fine = 8.0 * it;
     float top = m;
     double above = 0.0, goal = -1.0;
@@ -365,11 +370,11 @@ struct Passes : Row<T> {
           if (goal < 0.0) tail += weight(v);
         }
       });
-      unsigned long long w;
+      double w;
       uint32_t count;
       read_bins(w, count);
       const double scale = weight(top), unit = scale * exp(-0.125 * (threadIdx.x & (BINS - 1)));
-      const double own = threadIdx.x < BINS ? ldexp((double)w, -q) * unit : 0.0;
+      const double own = threadIdx.x < BINS ? ldexp(w, -q) * unit : 0.0;
       double total;
       const double running = block_running(sh, own, total);
       if (goal < 0.0) goal = p * (total + block_sum<NW>(tail, sh.red));
@@ -438,10 +443,12 @@ struct Passes : Row<T> {
 // exp(f / 16), f = y - floor(y); 512 bins down from the segment's largest logit's span 32
 // e-foldings. A bin's count and the sum of its exp(f / 16) - 1 are one 64-bit whole
 // number, added to by one LDS atomic: the sum in steps of 2^-q below, the count from bit
-// 64 - c up, c bits being enough for a column's elements (each four lanes' own).
+// 64 - c up, c bits being enough for a column's elements (each four lanes' own) of SEG
+// neighbouring ones, after which the columns are summed: q is 43 or more, so that a weight
+// is within 2^-44 of its size in rows of any length.
 constexpr int COLUMNS = 16;
 constexpr int CT = 512, CW = CT / 64;  // threads and wavefronts that count one
-constexpr int SEG = 16384;             // elements of a segment of rows that are not longer than 64 such
+constexpr int SEG = 16384;             // elements of a segment of rows that are not longer than 64 such, and of a round of longer ones
 constexpr double kFine = 16.0;
 
 struct Segment {
@@ -495,6 +502,8 @@ struct Choice {
   }
 };
 
+static_assert(GRID == CT, "a bin a thread");
+
 // One workgroup per segment of a row: a pass for the maximum, one for the histogram, one
 // for what lies below it where there is any; all but the first find the segment in the
 // cache.
@@ -507,7 +516,7 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int64_t length = segment_length(a.V), from = blockIdx.x * length, to = min(a.V, from + length);
   // a column's elements are whole vectors
-  const int64_t most = vec_of<T>() * ceil_div(min(length, a.V), (int64_t)COLUMNS * vec_of<T>());
+  const int64_t most = vec_of<T>() * ceil_div(min((int64_t)SEG, a.V), (int64_t)COLUMNS * vec_of<T>());
   const int c = 64 - __clzll((unsigned long long)most) + 1, q = min(67 - 2 * c, 51);
   const unsigned long long half = (unsigned long long)1 << (63 - c);   // a sum of 0: a little below it takes none off the count
   for (int64_t t = blockIdx.y; t < a.T; t += gridDim.y) {
@@ -541,22 +550,44 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
     // (rows that are greedy, not finite or have no choice need no more than the maximum)
     const bool some = m > -INFINITY && m < INFINITY && !choice.greedy;
     const double it = 1.0 / (double)choice.temperature, scale = kFine * it, first = floor((double)m * scale);
-    if (some) {
-      // p + 1.5 2^(52 - q) holds p in steps of 2^-q in its last bits; the count's one is
-      // added and the constant's bits taken off at once
-      const double magic = ldexp(1.5, 52 - q), step = step_of(first);
-      const unsigned long long one = ((unsigned long long)1 << (64 - c)) - (unsigned long long)__double_as_longlong(magic);
-      unsigned long long* column = &bins[0][lane & (COLUMNS - 1)];
-      visit<1, CW>(x, from, to, [&](int64_t, float v) {
-        const double bin = floor((double)v * scale), place = first - bin;
-        if (place < (double)GRID) {
-          const double p = grow(fma((double)v, scale, -bin) * step);
-          atomicAdd(column + (int)place * COLUMNS, (unsigned long long)__double_as_longlong(p + magic) + one);
-        } else if (v > -INFINITY) {
-          ++tail_count;
-        }
-      });
+    // p + 1.5 2^(52 - q) holds p in steps of 2^-q in its last bits; the count's one is
+    // added and the constant's bits taken off at once
+    const double magic = ldexp(1.5, 52 - q), step = step_of(first);
+    const unsigned long long one = ((unsigned long long)1 << (64 - c)) - (unsigned long long)__double_as_longlong(magic);
+    unsigned long long* column = &bins[0][lane & (COLUMNS - 1)];
+    const int g = threadIdx.x;                    // thread g sums bin g
+    double above = 0.0;                           // of exp(f / 16) - 1
+    uint32_t number = 0;
+    for (int64_t round = from; round < to; round += SEG) {
+      if (some) {
+        visit<1, CW>(x, round, min(to, round + SEG), [&](int64_t, float v) {
+          const double bin = floor((double)v * scale), place = first - bin;
+          if (place < (double)GRID) {
+            const double p = grow(fma((double)v, scale, -bin) * step);
+            atomicAdd(column + (int)place * COLUMNS, (unsigned long long)__double_as_longlong(p + magic) + one);
+          } else if (v > -INFINITY) {
+            ++tail_count;
+          }
+        });
+      }
+      __syncthreads();
+      int64_t sum = 0;
+      const unsigned long long low = ((unsigned long long)1 << (64 - c)) - 1;
+#pragma unroll 4
+      for (int k = 0; k < COLUMNS; ++k) {         // (staggered over the banks)
+        const unsigned long long b = bins[g][(k + g) & (COLUMNS - 1)];
+        sum += (int64_t)(b & low) - (int64_t)half;
+        number += (uint32_t)(b >> (64 - c));
+      }
+      above += ldexp((double)sum, -q);
+      if (round + SEG < to) {                     // (of a segment of more than a round's elements)
+        __syncthreads();
+        for (int i = threadIdx.x; i < GRID * COLUMNS; i += CT) (&bins[0][0])[i] = half;
+        __syncthreads();
+      }
     }
+    out->weight[g] = (double)number + above;
+    out->count[g] = number;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) tail_count += __shfl_xor(tail_count, off, kWave);
     if (lane == 0) counts[w] = tail_count;
@@ -572,19 +603,6 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
         if (v > -INFINITY && !(first - floor((double)v * scale) < (double)GRID)) tail += exp(((double)v - (double)m) * it);
       }
       tail = block_sum<CW>(tail, red);
-    }
-    for (int g = threadIdx.x; g < GRID; g += CT) {
-      int64_t sum = 0;
-      uint32_t n = 0;
-      const unsigned long long low = ((unsigned long long)1 << (64 - c)) - 1;
-#pragma unroll 4
-      for (int k = 0; k < COLUMNS; ++k) {         // (staggered over the banks)
-        const unsigned long long b = bins[g][(k + g) & (COLUMNS - 1)];
-        sum += (int64_t)(b & low) - (int64_t)half;
-        n += (uint32_t)(b >> (64 - c));
-      }
-      out->weight[g] = (double)n + ldexp((double)sum, -q);
-      out->count[g] = n;
     }
     if (threadIdx.x == 0) {
       out->tail = tail;
