@@ -1026,7 +1026,8 @@ int sample_as(hipStream_t s, const SampleArgs& a) {
 }  // namespace
 
 size_t sample_workspace(int64_t T, int64_t V) {
-  return std::max<int64_t>(256, T * segments(V) * (int64_t)sizeof(Segment));
+  // (a bound of the segments that does not fall: there are 64 up to 2^20 tokens, 33 from there on)
+  return std::max<int64_t>(256, T * std::min<int64_t>(ceil_div(V, SEG), kMostSegs) * (int64_t)sizeof(Segment));
 }
 
 int sample_tokens(hipStream_t s, const SampleArgs& a) {
