@@ -236,7 +236,8 @@ template <typename E, typename O>
 int product_as(hipStream_t s, const TileArgs& a, const OutArgs& out) {
   typedef DenseTile<E, O> S;
   const auto tiles = [&](int tm, int tn) { return ceil_div(a.M, tm) * ceil_div(a.N, tn); };
-  if (a.M <= 16 && (a.N <= 6144 || a.M <= 4)) return few_as<E, O>(s, a, out);
+  // (a launch has fewer than 2^32 threads: few_as takes 256 for 16 channels)
+  if (a.M <= 16 && (a.N <= 6144 || (a.M <= 4 && a.N <= ((int64_t)1 << 28) - 16))) return few_as<E, O>(s, a, out);
   // the fewest tiles: eight groups over k (32x64 above; us: 77 x 2051 x 8192 17.8 / 20.9,
   // 64 x 1000 x 8192 13.8 / 19.7, 128 x 2048 x 4096 11.0 / 12.5; f32 77 x 2051 x 4096 27.9
   // / 44.4; rows not aligned 77 x 2051 x 8191 29.9 / 39.2, 32 x 4096 x 4097 17.5 / 22.8)
