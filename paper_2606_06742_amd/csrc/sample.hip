@@ -506,8 +506,9 @@ static_assert(GRID == CT, "a bin a thread");
 
 // One workgroup per segment of a row: a pass for the maximum, one for the histogram, one
 // for what lies below it where there is any; all but the first find the segment in the
-// cache.
-template <typename T>
+// cache. LONG: segments of more than SEG elements, in rounds of that many (as one kernel 1
+// to 2 % slower where there is one round).
+template <typename T, bool LONG>
 __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
   __shared__ unsigned long long bins[GRID][COLUMNS];
   __shared__ float tops[CW];
@@ -550,27 +551,10 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
     // (rows that are greedy, not finite or have no choice need no more than the maximum)
     const bool some = m > -INFINITY && m < INFINITY && !choice.greedy;
     const double it = 1.0 / (double)choice.temperature, scale = kFine * it, first = floor((double)m * scale);
-    // p + 1.5 2^(52 - q) holds p in steps of 2^-q in its last bits; the count's one is
-    // added and the constant's bits taken off at once
-    const double magic = ldexp(1.5, 52 - q), step = step_of(first);
-    const unsigned long long one = ((unsigned long long)1 << (64 - c)) - (unsigned long long)__double_as_longlong(magic);
-    unsigned long long* column = &bins[0][lane & (COLUMNS - 1)];
     const int g = threadIdx.x;                    // thread g sums bin g
     double above = 0.0;                           // of exp(f / 16) - 1
     uint32_t number = 0;
-    for (int64_t round = from; round < to; round += SEG) {
-      if (some) {
-        visit<1, CW>(x, round, min(to, round + SEG), [&](int64_t, float v) {
-          const double bin = floor((double)v * scale), place = first - bin;
-          if (place < (double)GRID) {
-            const double p = grow(fma((double)v, scale, -bin) * step);
-            atomicAdd(column + (int)place * COLUMNS, (unsigned long long)__double_as_longlong(p + magic) + one);
-          } else if (v > -INFINITY) {
-            ++tail_count;
-          }
-        });
-      }
-      __syncthreads();
+    const auto sum_bin = [&] {
       int64_t sum = 0;
       const unsigned long long low = ((unsigned long long)1 << (64 - c)) - 1;
 #pragma unroll 4
@@ -580,14 +564,33 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
         number += (uint32_t)(b >> (64 - c));
       }
       above += ldexp((double)sum, -q);
-      if (round + SEG < to) {                     // (of a segment of more than a round's elements)
+    };
+    if (some) {
+      // p + 1.5 2^(52 - q) holds p in steps of 2^-q in its last bits; the count's one is
+      // added and the constant's bits taken off at once
+      const double magic = ldexp(1.5, 52 - q), step = step_of(first);
+      const unsigned long long one = ((unsigned long long)1 << (64 - c)) - (unsigned long long)__double_as_longlong(magic);
+      unsigned long long* column = &bins[0][lane & (COLUMNS - 1)];
+      for (int64_t round = from;;) {
+        const int64_t next = LONG ? min(to, round + SEG) : to;
+        visit<1, CW>(x, round, next, [&](int64_t, float v) {
+          const double bin = floor((double)v * scale), place = first - bin;
+          if (place < (double)GRID) {
+            const double p = grow(fma((double)v, scale, -bin) * step);
+            atomicAdd(column + (int)place * COLUMNS, (unsigned long long)__double_as_longlong(p + magic) + one);
+          } else if (v > -INFINITY) {
+            ++tail_count;
+          }
+        });
+        if (!LONG || next == to) break;
+        round = next;
+        __syncthreads();
+        sum_bin();
         __syncthreads();
         for (int i = threadIdx.x; i < GRID * COLUMNS; i += CT) (&bins[0][0])[i] = half;
         __syncthreads();
       }
     }
-    out->weight[g] = (double)number + above;
-    out->count[g] = number;
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) tail_count += __shfl_xor(tail_count, off, kWave);
     if (lane == 0) counts[w] = tail_count;
@@ -604,6 +607,9 @@ __global__ __launch_bounds__(CT, 4) void sample_count_kernel(SampleArgs a) {
       }
       tail = block_sum<CW>(tail, red);
     }
+    sum_bin();
+    out->weight[g] = (double)number + above;
+    out->count[g] = number;
     if (threadIdx.x == 0) {
       out->tail = tail;
       out->top = choice.greedy ? key_of(m, at) : key_of(m, 0);
@@ -1011,7 +1017,9 @@ __global__ __launch_bounds__(NT) void sample_aside_kernel(SampleArgs a, int segs
 template <typename T>
 int sample_as(hipStream_t s, const SampleArgs& a) {
   const int segs = (int)segments(a.V);
-  hipLaunchKernelGGL(sample_count_kernel<T>, dim3(segs, (unsigned)std::min<int64_t>(a.T, 65535)), dim3(CT), 0, s, a);
+  const dim3 grid((unsigned)segs, (unsigned)std::min<int64_t>(a.T, 65535));
+  if (segment_length(a.V) == SEG) hipLaunchKernelGGL((sample_count_kernel<T, false>), grid, dim3(CT), 0, s, a);
+  else hipLaunchKernelGGL((sample_count_kernel<T, true>), grid, dim3(CT), 0, s, a);
   const dim3 rows((unsigned)std::min<int64_t>(a.T, 65535));
   if (a.T <= 256) {
     hipLaunchKernelGGL((sample_pick_kernel<T, true>), rows, dim3(NT), 0, s, a, segs);
