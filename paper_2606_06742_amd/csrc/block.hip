@@ -28,14 +28,10 @@ __global__ __launch_bounds__(threads_of(TPR)) void block_reg_kernel(BlockArgs a)
   __syncthreads();
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR, d = (int)a.d;
   const int stride = RPB > 1 ? TPR : (int)blockDim.x;
-  constexpr bool KNOWN = (FORM & kKnown) != 0, WHOLE = KNOWN && !(FORM & kRagged);
+  constexpr bool KNOWN = (FORM & kKnown) != 0;
   const bool BYTES = KNOWN ? (FORM & kOther) != 0 : a.bytes;
   const bool each = KNOWN ? (FORM & kGates) != 0 : a.ldg != 0;         // a gate per row
-  const auto place = [&](int i) {
-    Place<VEC> q((t + i * stride) * VEC, d);
-    if (WHOLE) q.at = (t + i * stride) * VEC, q.skip = 0;
-    return q;
-  };
+  const auto place = [&](int i) { return Place<VEC>((t + i * stride) * VEC, d); };
   const auto put = [&](auto* p, int i, const auto& v, bool live) {     // a row's vector i
     if (KNOWN) store_n(p + place(i).at, v);
     else if (live) store_at(p, place(i), v);
