@@ -21,6 +21,9 @@ template <> struct acc_of<double> { typedef double type; };
 // Elements of one 16-byte access.
 template <typename T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
 
+// A number as a type.
+template <int N> struct Count { static constexpr int n = N; };
+
 // N consecutive elements from any address that is aligned to one element (the
 // hardware takes 16-byte accesses at such addresses, aligned ones are faster).
 // Conversion to Acc is exact; to T it rounds to the nearest, ties to even.

@@ -37,7 +37,6 @@ __device__ __forceinline__ float block_most(float v, float* red) {
 }
 // f(j, N elements) over a row of d by a workgroup of BIG threads: whole vectors of
 // 16 bytes, then single elements.
-template <int N> struct Count { static constexpr int n = N; };
 template <int VEC, typename F>
 __device__ __forceinline__ void over_row(int64_t d, F f) {
   const int64_t whole = d / VEC;

@@ -310,9 +310,8 @@ __device__ __forceinline__ int64_t round_up_to(int64_t a, int64_t b) { return (a
 // products left the cores idle: 4096 x 8192 x 4096 in 16 bits 276 / 263 us, 8192 x 8192 x
 // 8192 923 / 876, in 8 bits 536 / 462). The barrier of slice s stands within its last
 // products: their operands are in registers, so that the stage is free for slice s + NS,
-// and slice s + 1 has landed, so that its first operands can be read behind them. A slice
-// past the end is the last one again, unused, which keeps the number of loads under way
-// the same. (Slices of 64 bytes through four or five stages: 4 % slower.)
+// and slice s + 1 has landed, so that its first operands can be read behind them. The last
+// slices, behind which fewer than NS loads are under way, have their own waits. (Slices of 64 bytes through four or five stages: 4 % slower.)
 //
 // XT, WT: that operand is given the other way round, K rows of M or of N elements (of two
 // bytes, rows at multiples of 16 bytes), whose slice is 64 of these rows. Blocks of 4 rows
@@ -354,9 +353,8 @@ __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typenam
   const int whole = (int)a.K / SL, tail = (int)a.K % SL;
   const auto fetch_one = [&](int s, int i) {                          // load i of LOADS of slice s
     const uint32_t at = base + s % NS * STAGE;
-    const int k = min(s, whole - 1);
-    if (i < QA) load_to_lds(pa[i < QA ? i : 0] + (XT ? k * 64 * a.ldx : k * SL), at + (w * QA + i) * 1024);
-    else load_to_lds(pb[i < QA ? 0 : i - QA] + (WT ? k * 64 * a.ldw : k * SL), at + TM * SL + (w * QB + i - QA) * 1024);
+    if (i < QA) load_to_lds(pa[i < QA ? i : 0] + (XT ? s * 64 * a.ldx : s * SL), at + (w * QA + i) * 1024);
+    else load_to_lds(pb[i < QA ? 0 : i - QA] + (WT ? s * 64 * a.ldw : s * SL), at + TM * SL + (w * QB + i - QA) * 1024);
   };
   typename Blocks<E>::acc_t acc[MB][NB] = {};
   const int row = lane & 31, half = lane >> 5;
@@ -386,28 +384,42 @@ __global__ __launch_bounds__(64 * WR * WC) void ahead_kernel(TileArgs a, typenam
   if (whole > 0) {
 #pragma unroll
     for (int s = 0; s < NS; ++s)
+      if (s < whole) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) fetch_one(s, i);
-    wait_loads<(NS - 1) * LOADS>();
+        for (int i = 0; i < LOADS; ++i) fetch_one(s, i);
+      }
+    if (whole >= NS) wait_loads<(NS - 1) * LOADS>();
+    else wait_loads<0>();
     barrier();
 #pragma unroll
     for (int i = 0; i < READS; ++i) read_one(0, 0, i);
-    for (int s = 0; s + 1 < whole; ++s) {
+    // slice s with `behind` slices behind it, NS or more as NS
+    const auto slice = [&](int s, auto behind) {
+      constexpr int BEHIND = behind.n;
 #pragma unroll
       for (int h = 0; h < 3; ++h) multiply(h, 0, MULS, READS, [&](int i) { read_one(s, h + 1, i); });
-      multiply(3, 0, MULS / 2, 0, [](int) {});
-      wait_loads<(NS - 2) * LOADS>();                                 // s + 1 has landed, the later ones may not have
-      wait_lds();                                                     // the last operands of s are here
-      barrier();
-      multiply(3, MULS / 2, MULS, READS + LOADS, [&](int i) {
-        if (i < READS) read_one(s + 1, 0, i);
-        else fetch_one(s + NS, i - READS);
-      });
+      if constexpr (BEHIND == 0) {
+        multiply(3, 0, MULS, 0, [](int) {});
+      } else {
+        multiply(3, 0, MULS / 2, 0, [](int) {});
+        wait_loads<((BEHIND < NS ? BEHIND : NS - 1) - 1) * LOADS>();  // s + 1 has landed, the later ones may not have
+        wait_lds();                                                   // the last operands of s are here
+        barrier();
+        multiply(3, MULS / 2, MULS, READS + (BEHIND == NS ? LOADS : 0), [&](int i) {
+          if (i < READS) read_one(s + 1, 0, i);
+          else fetch_one(s + NS, i - READS);
+        });
+      }
+    };
+    int s = 0;
+    for (; s + NS < whole; ++s) slice(s, Count<NS>());
+    static_assert(NS == 2 || NS == 4, "the last slices");
+    if constexpr (NS == 4) {
+      if (whole - s > 3) slice(s++, Count<3>());
+      if (whole - s > 2) slice(s++, Count<2>());
     }
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-      multiply(h, 0, MULS, h < 3 ? READS : 0, [&](int i) { read_one(whole - 1, h + 1, i); });
-    wait_loads<0>();                                                  // (what was fetched past the end)
+    if (whole - s > 1) slice(s++, Count<1>());
+    slice(s, Count<0>());
   }
   if (tail > 0) {                                                     // zeros past K
     __syncthreads();
