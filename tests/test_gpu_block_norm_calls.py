@@ -59,3 +59,47 @@ def test_rows_in_8_bits_in_place(xt, d):
             outs.append((h, q, scale, c.stats.clone()))
         for a, b in zip(*outs):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("gate", [None, "vector", "matrix"])
+def test_rows_of_2_28_columns(gate):
+    """Columns beyond 2^28: more than a launch has threads. Without a norm of b every
+    element of h, db and dres has two roundings; a thread adds d / 1024 terms of a sum of a
+    row one after another, each within 2^-24 of it: y, db and dres by 2^-6 of the largest."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    rows, d, t = 2, 2 ** 28 + 65, torch.bfloat16
+    g = torch.Generator(device=device()).manual_seed(7)
+    rand = lambda *n: torch.randn(*n, generator=g, device=device(), dtype=t)
+    b, res, dy, dh, gamma = rand(rows, d), rand(rows, d), rand(rows, d), rand(rows, d), rand(d)
+    w = None if gate is None else rand(d) if gate == "vector" else rand(rows, d)
+    new = lambda *n: torch.full(n, float("nan"), dtype=t, device=device())
+    h, y, db, dres, dgamma, dbeta = new(rows, d), new(rows, d), new(rows, d), new(rows, d), new(d), new(d)
+    dw = None if w is None else torch.full_like(w, float("nan"))
+    stats = torch.full((rows, 4), float("nan"), device=device())
+    ws = torch.empty(km.kmp_block_norm_workspace_bytes(rows, d, t), dtype=torch.uint8, device=device())
+    form = dict(gate=w, gamma=gamma, rscale=0.5, after=False, rms=True)
+    announce(f"block norm {rows} x {d}, gate {gate}")
+    km.kmp_block_norm(b, res, h, y, EPS, stats=stats, **form)
+    km.kmp_block_norm_backward(dy, dh, b, h, stats, db, dres, dgate=dw, dgamma=dgamma, dbeta=dbeta, workspace=ws, **form)
+    one = torch.ones((), device=device())
+    near = lambda got, want, off: bool(((got.float() - want).abs() <= off + 2.0 ** -8 * (want.abs() + off)).all())
+    sums = [torch.zeros(d, device=device()) for _ in range(3)]
+    for r in range(rows):
+        wr = one if w is None else (w if w.dim() == 1 else w[r]).float()
+        he = 0.5 * res[r].float() + wr * b[r].float()
+        assert near(h[r], he, 2.0 ** -22 * 16)
+        rs = float(1 / torch.sqrt((he.double() ** 2).mean() + EPS))
+        assert abs(float(stats[r, 3]) / rs - 1) < 2.0 ** -6
+        assert near(y[r], he * rs * gamma.float(), 2.0 ** -6 * float(he.abs().max()) * rs * float(gamma.abs().max()))
+        xh, v = h[r].float() * float(stats[r, 3]), dy[r].float() * gamma.float()
+        s = dh[r].float() + float(stats[r, 3]) * (v - xh * float((v.double() * xh.double()).mean()))
+        most = 2.0 ** -6 * float(s.abs().max())
+        assert near(dres[r], 0.5 * s, most) and near(db[r], wr * s, most * float(wr.abs().max()))
+        if gate == "matrix":
+            assert near(dw[r], s * b[r].float(), most * float(b.float().abs().max()))
+        sums[0] += s * b[r].float()
+        sums[1] += dy[r].float() * xh
+        sums[2] += dy[r].float()
+    assert near(dgamma, sums[1], 2.0 ** -18) and near(dbeta, sums[2], 2.0 ** -20)
+    assert gate != "vector" or near(dw, sums[0], 2 * most * float(b.float().abs().max()))
