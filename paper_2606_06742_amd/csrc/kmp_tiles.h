@@ -307,11 +307,12 @@ __device__ __forceinline__ int64_t round_up_to(int64_t a, int64_t b) { return (a
 // the operands of every 32 bytes of k are read from LDS while the 32 before them are
 // multiplied: reads and loads are issued between the products, whose issue takes an
 // eighth of the time that the matrix cores need for one (all of them ahead of a group of
-// products left the cores idle: 4096 x 8192 x 4096 in 16 bits 276 / 263 us, 8192 x 8192 x
-// 8192 923 / 876, in 8 bits 536 / 462). The barrier of slice s stands within its last
-// products: their operands are in registers, so that the stage is free for slice s + NS,
-// and slice s + 1 has landed, so that its first operands can be read behind them. The last
-// slices, behind which fewer than NS loads are under way, have their own waits. (Slices of 64 bytes through four or five stages: 4 % slower.)
+// products left the cores idle: 8-bit 8192 x 8192 x 8192 523 / 479 us, 4096 x 16384 x 4096
+// 279 / 262). The barrier of slice s stands within its last products: their operands are in
+// registers, so that the stage is free for slice s + NS, and slice s + 1 has landed, so that
+// its first operands can be read behind them. The last slices, behind which fewer than NS
+// loads are under way, have waits of their own. (Slices of 64 bytes through four or five
+// stages: 4 % slower.)
 //
 // XT, WT: that operand is given the other way round, K rows of M or of N elements (of two
 // bytes, rows at multiples of 16 bytes), whose slice is 64 of these rows. Blocks of 4 rows

@@ -194,36 +194,37 @@ int few_as(hipStream_t s, const TileArgs& a, const OutArgs& out) {
 }
 
 // Which form, by what keeps the chip's 256 compute units busy. us per launch at M x N x
-// K, operands from HBM: few tokens; tiles of 32 x 64 (four groups over k, ring of 3), 64 x
-// 64 (two groups, ring of 3, or of 2; one group, ring of 2), operands ahead in tiles of
-// 128 (ring of 4, or of 2), 256 x 128 and 256 x 256; the floor, the larger of the bytes
-// at a copy's 4.93 TB/s and the products at the 1574 TFLOP/s (bf16; f32: 155) of the
-// library's product of order 8192. In bf16:
-//                      few  32x64  64,3  64,2  64,1 128,4 128,2 256,128 256  floor
-//   1 x 4096 x 4096    9.0  11.8  16.5  21.1  30.9  31.7  38.9  47.7  75.4   6.8
-//   1 x 16384 x 4096  24.6  29.8  30.9  37.1  52.4  38.0  61.7  70.0  90.9  27.2
-//   16 x 8192 x 4096  18.9  16.3  18.2  29.3  45.6  32.3  54.9  64.3  80.0  13.7
-//   16 x 32000 x 2048 39.0  34.2  34.8  33.2  34.8  33.9  38.7  43.9  54.6  26.8
-//   64 x 4096 x 4096        14.1  17.5  23.4  31.8  34.5  42.5  53.0  79.8   7.0
-//   64 x 12288 x 4096       37.1  28.0  36.3  51.1  39.3  63.3  73.9  94.2  20.8
-//   256 x 4096 x 4096       26.6  19.6  25.0  33.3  35.7  43.3  57.6  87.5   7.7
-//   512 x 4096 x 4096       51.4  38.1  30.7  37.7  38.0  44.3  57.1  86.8  10.9
-//   600 x 4500 x 704        30.3  19.4  16.0  12.7  14.1  14.8  20.6  35.0   2.6
-//   1000 x 3000 x 4096      71.4  51.6  50.6  43.9  39.5  45.1  57.6  87.2  15.6
-//   1024 x 4096 x 4096      99.3  69.1  56.4  61.8  45.5  48.1  59.0  88.7  21.8
-//   2048 x 2048 x 2048      61.2  41.4  32.7  33.2  26.9  28.9  35.4  53.1  10.9
-//   1024 x 8192 x 4096       236   155   129   126  89.0  79.0  78.8   104  43.7
-//   2048 x 4096 x 4096       182   132   107   113  85.0  78.5  71.3  98.4  43.7
-//   3000 x 5000 x 1000       197   118  87.3  73.2  70.1  58.2  58.5  48.2  19.1
-//   4096 x 4096 x 4096       368   276   225   224   171   154   155   124  87.3
-//   4096 x 8192 x 4096             574   471   462   342   304   313   242   175
+// K, in a recorded graph, the forms in turn, operands from HBM: few tokens; tiles of 32 x 64
+// (four groups over k, ring of 3), 64 x 64 (two groups, ring of 3, or of 2; one group, ring
+// of 2), operands ahead in tiles of 128 (ring of 4, or of 2), 256 x 128 and 256 x 256; the
+// floor, the larger of the bytes at a copy's 4.93 TB/s and the products at the 1574 TFLOP/s
+// (bf16; f32: 155) of the library's product of order 8192. In bf16:
+//                        few  32x64  64,3  64,2  64,1 128,4 128,2 256,128  256  floor
+//   1 x 4096 x 4096      8.9   15.7  18.5  30.4  47.4  31.2  56.2    65.8 83.6    6.8
+//   1 x 16384 x 4096    24.6   29.7  30.7  35.9  51.4  37.8  61.4    70.7 89.4   27.2
+//   16 x 8192 x 4096    20.4   18.4  20.3  31.5  48.3  31.8  57.6    67.3 85.3   13.7
+//   16 x 32000 x 2048   38.6   31.1  31.6  29.2  32.2  33.4  36.8    42.4 51.2   26.8
+//   64 x 4096 x 4096           18.6  23.5  33.1  48.5  35.6  60.2    71.1 89.7    7.0
+//   64 x 12288 x 4096          35.5  26.5  34.9  49.3  37.7  60.7    71.8 90.1   20.8
+//   256 x 4096 x 4096          32.7  22.7  32.1  48.4  40.7  60.2    84.2  108    7.7
+//   512 x 4096 x 4096          62.5  41.6  36.3  47.9  40.3  58.2    81.2  106   10.9
+//   600 x 4500 x 704           30.2  19.3  16.1  12.2  13.6  14.4    21.0 35.2    2.6
+//   1000 x 3000 x 4096         86.3  58.8  64.7  52.9  39.9  58.2    78.2  105   15.6
+//   1024 x 4096 x 4096          117  80.2  68.8  67.1  44.0  57.7    79.4  106   21.8
+//   2048 x 2048 x 2048         63.8  44.7  36.4  34.3  26.1  32.3    41.6 58.3   10.9
+//   1024 x 8192 x 4096          236   158   132   128  88.0  78.3    86.8  108   43.7
+//   2048 x 4096 x 4096          210   155   130   125  86.2  77.8    84.1  105   43.7
+//   3000 x 5000 x 1000          198   122  91.6  82.2  69.4  57.7    60.5 49.9   19.1
+//   4096 x 4096 x 4096          394   288   239   233   168   151     159  121   87.3
+//   4096 x 8192 x 4096          777   568   463   449   332   296     308  237  174.6
+//   8192 x 8192 x 8192         2546  1949  1642  1673  1216  1119    1090  881  698.5
 // In f32 (128: of four wavefronts, ring of 2):
-//                      few  32x64  64,2   128  floor
-//   1 x 4096 x 4096   14.1  42.5  76.2   251  13.6
-//   128 x 4096 x 1000       19.0  25.5  75.1   6.8
-//   1024 x 1024 x 1024      31.7  26.4  73.2  13.9
-//   2048 x 2048 x 2048       205   156   137   111
-//   4096 x 4096 x 1024       435   303   274   222
+//                        few  32x64  64,2   128  floor
+//   1 x 4096 x 4096     16.1   44.3  77.2   253   13.6
+//   128 x 4096 x 1000          19.6  25.8  74.5    6.8
+//   1024 x 1024 x 1024         31.0  25.6  72.4   13.9
+//   2048 x 2048 x 2048          189   154   138  110.8
+//   4096 x 4096 x 1024          431   304   274  221.7
 // Rows that are not aligned, f16: few tokens; tiles of 32 x 64 (four groups), 64 and 128:
 //                      few  32x64    64   128  floor
 //   16 x 4096 x 4097  11.5  17.8  22.1  36.3   6.9
@@ -238,9 +239,9 @@ int product_as(hipStream_t s, const TileArgs& a, const OutArgs& out) {
   const auto tiles = [&](int tm, int tn) { return ceil_div(a.M, tm) * ceil_div(a.N, tn); };
   // (a launch has fewer than 2^32 threads: few_as takes 256 for 16 channels)
   if (a.M <= 16 && (a.N <= 6144 || (a.M <= 4 && a.N <= ((int64_t)1 << 28) - 16))) return few_as<E, O>(s, a, out);
-  // the fewest tiles: eight groups over k (32x64 above; us: 77 x 2051 x 8192 17.8 / 20.9,
-  // 64 x 1000 x 8192 13.8 / 19.7, 128 x 2048 x 4096 11.0 / 12.5; f32 77 x 2051 x 4096 27.9
-  // / 44.4; rows not aligned 77 x 2051 x 8191 29.9 / 39.2, 32 x 4096 x 4097 17.5 / 22.8)
+  // the fewest tiles: eight groups over k (32x64 above; us: 77 x 2051 x 8192 23.9 / 26.8,
+  // 64 x 1000 x 8192 24.2 / 27.8, 128 x 2048 x 4096 15.2 / 17.2; f32 77 x 2051 x 4096 28.6
+  // / 45.0; rows not aligned 77 x 2051 x 8191 29.9 / 39.2, 32 x 4096 x 4097 17.5 / 22.8)
   const bool least = tiles(32, 32) <= 256;
   if (!aligned_rows(a)) {
     if (least) return tiles_as<E, S, 32, 32, 1, 1, 8, 2, false>(s, a, out);

@@ -145,61 +145,60 @@ struct ScaledTile {
 };
 
 // Which form, by what keeps the chip's 256 compute units busy. us per launch at M x
-// N x K, w from HBM: few tokens; tiles of 32 x 64 (four groups over k, ring of 3), 64
-// x 64 (two groups, ring of 3, or of 2 and so two workgroups a compute unit); operands
-// ahead in tiles of 128 and 256; the floor, the larger of the bytes at a copy's 4.82
-// TB/s and the products at 2040 TOP/s (what the 8-bit product of order 8192 reached before
-// its reads were dealt out between the products; 2380 since):
-//                      few  32x64  64,3  64,2   128   256  floor
-//   1 x 4096 x 4096    6.0   7.5   9.7  12.0  21.0  40.2   3.5
-//   16 x 8192 x 4096  11.6  10.4  11.4  16.6  21.8  40.6   7.0
-//   16 x 32000 x 2048 21.2  18.2  18.5  15.6  19.4  28.9  13.8
-//   64 x 1000 x 8192        11.8  15.8  21.6  39.6  76.2   1.8
-//   64 x 4096 x 4096         8.1  10.1  12.9  22.2  40.7   3.6
-//   128 x 4096 x 4096        8.7  10.7  12.8  23.3  42.1   3.8
-//   256 x 4096 x 4096       14.6  11.7  13.2  23.5  43.4   4.2
-//   64 x 12288 x 4096       20.8  16.5  19.8  32.7  47.5  10.8
-//   64 x 32000 x 2048       27.5  21.3  18.0  20.8  29.4  14.5
-//   512 x 4096 x 4096       27.0  19.6  16.6  24.1  43.7   8.4
-//   2048 x 2048 x 2048      35.9  24.6  18.4  16.3  27.6   8.4
-//   1024 x 8192 x 4096       132    89    74  42.6  50.6  33.7
-//   3000 x 5000 x 1000       159    83    63  36.9  31.4  14.7
-//   4096 x 4096 x 4096       224   169   135  85.7  64.1  67.4
-//   4096 x 16384 x 4096      850   632   534   328   256   269
+// N x K (here and up to the rows that are not aligned: in a recorded graph, the forms in
+// turn, operands from HBM): few tokens; tiles of 32 x 64 (four groups over k, ring of 3), 64 x 64 (two groups, ring
+// of 3, or of 2 and so two workgroups a compute unit); operands ahead in tiles of 128 and
+// 256; the floor, the larger of the bytes at a copy's 4.93 TB/s and the products at the
+// 2380 TOP/s that the 8-bit product of order 8192 has reached:
+//                         few  32x64  64,3  64,2   128   256  floor
+//   1 x 4096 x 4096       6.1    8.4  10.2  14.8  25.5  41.3    3.4
+//   16 x 8192 x 4096     11.7   11.4  12.2  17.5  30.7  46.4    6.9
+//   16 x 32000 x 2048    21.6   18.7  19.0  15.6  19.7  28.2   13.5
+//   64 x 1000 x 8192            11.8  16.4  21.9  40.1  77.3    1.8
+//   64 x 4096 x 4096            10.5  13.0  17.3  30.9  45.6    3.6
+//   128 x 4096 x 4096           10.4  12.7  17.1  32.3  47.2    3.7
+//   256 x 4096 x 4096           18.4  13.0  17.2  31.8  53.2    4.0
+//   64 x 12288 x 4096           21.1  15.5  19.7  32.9  47.8   10.6
+//   64 x 32000 x 2048           27.5  20.7  17.2  20.8  29.0   14.2
+//   512 x 4096 x 4096           35.1  23.3  20.6  31.5  52.3    7.2
+//   2048 x 2048 x 2048          37.4  25.8  19.8  16.6  28.6    7.2
+//   1024 x 8192 x 4096           129  86.9  73.1  45.6  58.2   28.9
+//   3000 x 5000 x 1000           149  84.6  59.7  37.0  31.7   12.6
+//   4096 x 4096 x 4096           222   161   134  85.7  68.3   57.7
+//   4096 x 16384 x 4096          859   658   521   331   262  231.0
+//   8192 x 8192 x 8192          1428  1094   906   610   476  462.0
 // Between 512 and 768 tiles of 64 those of 128 leave compute units idle: one group a
-// tile of 64 and a ring of 2, up to five workgroups a compute unit (64,1; here and
-// below in a recorded graph, 1 to 2 us more a launch):
-//                       64,2  64,1   128  floor
-//   600 x 4500 x 700    13.0   9.9  11.9   1.9
-//   1500 x 1500 x 1500  17.3  12.7  15.7   3.3
-//   1244 x 1824 x 10909 74.2  61.7  68.9  24.3
-//   1000 x 3000 x 4096  34.1  28.7  26.1  12.0
-//   768 x 4096 x 8192   51.1  50.6  44.4  25.3
-//   1024 x 3584 x 4096  35.2  34.2  26.2  14.7
-//   2048 x 2048 x 2048  18.3  18.8  16.8   8.4
+// tile of 64 and a ring of 2, up to five workgroups a compute unit (64,1):
+//                        64,2  64,1   128  floor
+//   600 x 4500 x 700     13.4  10.4  11.1    1.8
+//   1500 x 1500 x 1500   18.2  14.7  15.1    2.8
+//   1244 x 1824 x 10909  86.8  71.6  83.2   20.8
+//   1000 x 3000 x 4096   33.3  28.8  30.4   10.3
+//   768 x 4096 x 8192    55.8  52.0  56.8   21.7
+//   1024 x 3584 x 4096   37.2  35.9  32.1   12.6
+//   2048 x 2048 x 2048   19.8  19.6  16.6    7.2
 // Up to 256 tiles of 128 have a compute unit each and room for a ring of 4 there,
-// which hides more of the loads than a ring of 2 (128,4; in a recorded graph, both
-// sides in turn):
-//                       64,1   128  128,4
-//   600 x 4500 x 700    10.7         11.8
-//   1500 x 1500 x 1500  13.9         14.3
-//   1244 x 1824 x 10909 63.6         52.7
-//   4138 x 534 x 7988   44.9         43.6
-//   1000 x 3000 x 4096  24.9         22.8
-//   768 x 4096 x 8192   44.1         36.3
-//   1024 x 3584 x 4096        26.2   24.0
-//   2000 x 2000 x 8192        47.4   43.4
-//   2048 x 2048 x 2048        16.8   16.7
+// which hides more of the loads than a ring of 2 (128,4):
+//                        64,1   128  128,4
+//   600 x 4500 x 700     10.4  11.1   10.8
+//   1500 x 1500 x 1500   14.7  15.1   13.5
+//   1244 x 1824 x 10909  71.6  83.2   66.4
+//   4138 x 534 x 7988    53.6  58.5   44.2
+//   1000 x 3000 x 4096   28.8  30.4   23.1
+//   768 x 4096 x 8192    52.0  56.8   40.2
+//   1024 x 3584 x 4096   35.9  32.1   25.0
+//   2000 x 2000 x 8192   65.2  58.8   45.0
+//   2048 x 2048 x 2048   19.6  16.6   15.6
 // Few tokens with more channels than the first table's have 192 tiles of 256 and take
-// them (in a recorded graph, w from HBM), though smaller ones are ahead (reading alone
-// is a little faster than the copy that the floor's rate is of):
-//                        few  32x64  64,3  64,2  64,1   128   256  floor
-//   1 x 50257 x 2048    19.4  28.0  28.3  24.6  21.4  22.8  31.6  21.4
-//   64 x 50257 x 2048         43.2  34.6  30.2  30.3  28.5  33.9  22.8
-//   16 x 128256 x 4096   141   105   108   107   108   109   133   110
-//   64 x 128256 x 4096         164   128   122   123   127   138   113
-//   1 x 151936 x 4096    103   126   134   139   152   155   180   129
-//   64 x 151936 x 4096         191   159   152   152   172   188   133
+// them, though smaller ones are ahead (reading alone is a little faster than the copy that
+// the floor's rate is of):
+//                         few  32x64  64,3  64,2  64,1   128   256  floor
+//   1 x 50257 x 2048     18.4   27.4  27.8  24.2  21.0  26.5  30.9   20.9
+//   64 x 50257 x 2048           42.2  33.3  28.4  27.2  29.9  32.8   22.2
+//   16 x 128256 x 4096    140   98.5   103  98.1  95.1  97.3   126  107.5
+//   64 x 128256 x 4096           159   122   116   113   113   132  110.0
+//   1 x 151936 x 4096    98.6    126   133   135   148   151   174  126.4
+//   64 x 151936 x 4096           192   159   153   153   165   186  130.4
 // Rows that are not aligned: few tokens; tiles of 32 x 64 (four groups), 64 and 128
 // (one; 128 with eight wavefronts, with four 97 for 87 at 1244 x 1824 x 10909):
 //                        few  32x64    64   128  floor
