@@ -485,9 +485,9 @@ def kmp_block_norm(b, res, h, y, eps, gamma_after=None, beta_after=None, gate=No
         sp, bt, (KMP_NORM_RMS if rms else 0) | (KMP_NORM_AFTER if after else 0), bp, ldb, rp, ldr, rows, d,
         bt if wd is b.dtype else _type(wd, "gamma"),
         None if gamma_after is None else _vector(gamma_after, "gamma_after", d, wd, on),
-        None if beta_after is None else _vector(beta_after, "beta_after", d, wd, on), gp, ldg, rscale,
+        None if beta_after is None else _vector(beta_after, "beta_after", d, wd, on), gp, ldg, float(rscale),
         None if gamma is None else _vector(gamma, "gamma", d, wd, on),
-        None if beta is None else _vector(beta, "beta", d, wd, on), eps, hp, ldh, yt, yp, ldy, st, sc), allow_maxiter=False)
+        None if beta is None else _vector(beta, "beta", d, wd, on), float(eps), hp, ldh, yt, yp, ldy, st, sc), allow_maxiter=False)
 
 
 def kmp_block_norm_workspace_bytes(rows: int, d: int, dtype) -> int:

@@ -103,3 +103,20 @@ def test_rows_of_2_28_columns(gate):
         sums[2] += dy[r].float()
     assert near(dgamma, sums[1], 2.0 ** -18) and near(dbeta, sums[2], 2.0 ** -20)
     assert gate != "vector" or near(dw, sums[0], 2 * most * float(b.float().abs().max()))
+
+
+def test_numbers_of_numpy():
+    """The scale and eps of any real type, forward as backward."""
+    import numpy as np
+    import torch
+    c = Case(5, 333, "bf16", "f32", True, False, "vector")
+    outs = []
+    for kind in (float, np.float32, np.float64):
+        from paper_2606_06742_amd import kmpath as km
+        h, y, db, dres = c.matrix(), c.matrix(), c.matrix(), c.matrix()
+        form = dict(c.form(("gamma_after", "beta_after", "gate", "gamma")), rscale=kind(0.75))
+        km.kmp_block_norm(c.t["b"], c.t["res"], h, y, kind(2.0 ** -10), beta=c.t["beta"], stats=c.stats, **form)
+        km.kmp_block_norm_backward(y, h, c.t["b"], h, c.stats, db, dres, **form)
+        outs.append((h, y, db, dres))
+    for other in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(outs[0], other))
