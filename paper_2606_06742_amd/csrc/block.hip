@@ -13,7 +13,7 @@ namespace {
 // weights stay in registers over the rows of a workgroup, and a row's registers take the
 // next one's vectors as soon as they are free: b's behind the first norm, res and the
 // gate behind h, so that the loads are under way during the sums without registers of
-// their own. By HBM: 16384 x 4096 bf16, four arrays, 92 to 100 us (5.4 to 5.8 TB/s), 4096
+// their own. By HBM: 16384 x 4096 bf16, four arrays, 90 to 100 us (5.4 to 6.0 TB/s), 4096
 // x 5120 f16 with a gate per row 53 (3.9); a single row of 4096 3.4, a chain of load, two
 // sums, store.
 template <typename T, typename W, int TPR, int NV, int FORM>

@@ -108,7 +108,7 @@ __global__ __launch_bounds__(BIG) void block_back_row_kernel(BlockBackArgs a) {
 // in registers, adds its RPB row groups in LDS and writes partial[p]. A row's registers
 // take the next one's vectors as soon as they are free: dy, h and dh behind s, whose
 // loads are under way during the second half of the row, b and the gate behind db. By
-// HBM: 16384 x 4096 bf16, six arrays, 185 to 205 us (3.9 to 4.3 TB/s), at two wavefronts a
+// HBM: 16384 x 4096 bf16, six arrays, 184 to 205 us (3.9 to 4.4 TB/s), at two wavefronts a
 // SIMD: its sums and rows fill the registers, and to force more of them in spilled and was
 // slower.
 template <typename T, typename W, int TPR, int NV, int FORM>

@@ -218,6 +218,9 @@ int few_as(hipStream_t s, const TileArgs& a, const OutArgs& out) {
 //   4096 x 4096 x 4096          394   288   239   233   168   151     159  121   87.3
 //   4096 x 8192 x 4096          777   568   463   449   332   296     308  237  174.6
 //   8192 x 8192 x 8192         2546  1949  1642  1673  1216  1119    1090  881  698.5
+// Those of 256 x 128 are ahead of 128,2 where operands come from the last-level cache (2048 x
+// 4096 x 4096 69.4 / 77.0, 1024 x 8192 x 4096 69.5 / 76.8, 1500 x 5000 x 8192 123 / 142),
+// which the rule goes by, and behind it from HBM (84.1 / 77.8, 86.8 / 78.3, 145 / 142).
 // In f32 (128: of four wavefronts, ring of 2):
 //                        few  32x64  64,2   128  floor
 //   1 x 4096 x 4096     16.1   44.3  77.2   253   13.6

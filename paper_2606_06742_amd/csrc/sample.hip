@@ -12,8 +12,8 @@
 // Two launches: segments of rows are read once for histograms of their weights, on one
 // grid, so that a row's bins are sums of its segments'; then a workgroup per row finds the
 // bins that hold its cuts, and lists and orders only their tokens. Bound by the 64-bit
-// work on each logit (1024 x 128000 bf16: 181 us at 37 vector instructions a logit, where
-// the reads take 53 at a copy's rate) and by reading the row again for the list (91 us);
+// work on each logit (1024 x 128000 bf16: 179 us at 37 vector instructions a logit, where
+// the reads take 53 at a copy's rate) and by reading the row again for the list (90 us);
 // by sorting rows, 16.4 ms. One row: by two dependent launches (9 and 15 us).
 #include "kmp_keys.h"
 
