@@ -490,9 +490,9 @@ size_t kmp_dense_product_workspace_bytes(int32_t type, int64_t M, int64_t N, int
  * with KMP_ACT_NONE). dx, dw and dbias may each be NULL, and x without dw, w
  * without dx. In 16 bits and with more than 8 tokens (M) dz is rounded to type for the
  * products, as their operands are; for dbias, and up to 8 tokens, it stays in 32 bits.
- * Sums are in 32 bits and in a fixed order: the same call gives the same bits. M = 0 gives dw = dbias = 0, N = 0 dx = 0. M, N and K <= 2^28.
- * No output overlaps an input or another output. The workspace is aligned to 16
- * bytes.                                                                      */
+ * Sums are in 32 bits and in a fixed order: the same call gives the same bits. M = 0
+ * gives dw = dbias = 0, N = 0 dx = 0. M, N and K <= 2^28. No output overlaps an input or
+ * another output. The workspace is aligned to 16 bytes.                       */
 int kmp_dense_product_backward(void* stream, int32_t type, const void* dout, int64_t lddo, int64_t M, int64_t N,
                                int64_t K, int32_t act, const void* z, int64_t ldz, const void* x, int64_t ldx,
                                const void* w, int64_t ldw, void* dx, int64_t lddx, void* dw, int64_t lddw,

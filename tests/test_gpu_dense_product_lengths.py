@@ -77,3 +77,39 @@ def test_every_number_of_slices_in_8_bits():
             out = torch.full((M, N), float("nan"), device=device())
             km.kmp_quantized_product(x, one[:M], w, one[:N], out)
             assert torch.equal(out, x.float() @ w.float().T)    # (whole numbers below 2^24)
+
+
+@pytest.mark.parametrize("xt", ["f32", "bf16"])
+def test_bias_of_more_channels_than_workgroups(xt):
+    """The sums over the tokens take up to 2^20 workgroups, each then more than one tile."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    M, N, t = 9, 2 ** 27 + 77, _dtype(xt)
+    announce(f"dense product, bias of {M} x {N} {xt}")
+    n = torch.arange(N, device=device(), dtype=torch.int32)
+    dout = torch.empty(M, N, dtype=t, device=device())
+    for m in range(M):
+        dout[m] = ((n + m * 5) % 11 - 5).to(t)
+    db = torch.full((N,), float("nan"), device=device())
+    ws = torch.empty(km.kmp_dense_product_workspace_bytes(M, N, 0, t), dtype=torch.uint8, device=device())
+    km.kmp_dense_product_backward(dout, None, None, None, None, None, db, workspace=ws)
+    assert torch.equal(db, dout.float().sum(dim=0))
+
+
+def test_gradients_of_a_few_tokens_in_long_rows():
+    """8 tokens of 2^26 elements and one channel: the runs' join takes up to 2^20 workgroups,
+    each then more than one part."""
+    import torch
+    from paper_2606_06742_amd import kmpath as km
+    M, N, K, t = 8, 1, 2 ** 26 + 3, torch.bfloat16
+    announce(f"dense product, gradients of {M} x {N} x {K}")
+    k = torch.arange(K, device=device(), dtype=torch.int32)
+    dout = (torch.arange(M, device=device()) - 3).reshape(M, N).to(t)
+    w, x = (k % 13 - 6).to(t).reshape(N, K), torch.empty(M, K, dtype=t, device=device())
+    for m in range(M):
+        x[m] = ((k + m) % 7 - 3).to(t)
+    dx, dw = torch.full((M, K), float("nan"), dtype=t, device=device()), torch.full((N, K), float("nan"), dtype=t, device=device())
+    ws = torch.empty(km.kmp_dense_product_workspace_bytes(M, N, K, t), dtype=torch.uint8, device=device())
+    km.kmp_dense_product_backward(dout, x, w, None, dx, dw, None, workspace=ws)
+    assert torch.equal(dx, dout * w)
+    assert torch.equal(dw[0], (dout.float() * x.float()).sum(dim=0).to(t))     # (whole numbers up to 84)
